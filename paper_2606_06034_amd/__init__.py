@@ -47,3 +47,12 @@ from ._binding import (  # noqa: F401
     gdn_wy_apply,
     lib,
 )
+from ._layer import (  # noqa: F401
+    GDN_NORM_LAYER,
+    GDN_NORM_RMS,
+    gdn_norm_backward,
+    gdn_norm_backward_workspace,
+    gdn_norm_forward,
+    gdn_recurrent_forward,
+    layer_abi_symbols,
+)

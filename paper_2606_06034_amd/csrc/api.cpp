@@ -5,34 +5,21 @@
 
 #include <stdint.h>
 
+#include "checks.hpp"
 #include "launch.hpp"
 
 namespace {
 
-// A 1-D launch of n workgroups of `block` work items fits HIP's grid when
+using namespace gdn::checks;
+
+// grid_ok: a 1-D launch of n workgroups of `block` work items fits HIP's grid when
 // n <= 2^31 - 1 and n * block <= 2^32 - 1.  Every launch here is one
 // workgroup per tile (or per (head, slice) of the state pass), of 64 work
 // items, 128 for the two-wave C = 128 kernels (fused path and integer
 // inverse) and 256 for the C = 128 quantiser and the state pass; the fused
 // kernels that put 2 or 4 tiles in one workgroup launch as many work items
 // per tile in fewer workgroups, so the per-tile check covers them.
-bool grid_ok(int64_t n, int block) {
-  return n >= 0 && n <= 0x7fffffffLL && n * block <= 0xffffffffLL;
-}
 int two_wave(int C) { return C == 128 ? 128 : 64; }
-
-bool valid_C(int C) { return C == 16 || C == 32 || C == 64 || C == 128; }
-bool valid_d(int d) { return d == 64 || d == 128; }
-bool fdtype(int t) { return t == GDN_F32 || t == GDN_BF16; }
-int64_t esize(int t) { return t == GDN_F32 ? 4 : (t == GDN_BF16 ? 2 : 1); }
-bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// [p, p + bytes) and [q, q + qbytes) intersect
-bool overlap(const void* p, int64_t bytes, const void* q, int64_t qbytes) {
-  if (!p || !q || bytes <= 0 || qbytes <= 0) return false;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + (uintptr_t)qbytes && b < a + (uintptr_t)bytes;
-}
 
 // exponents per tile of the integer paths: C = 128 runs three blocks
 int64_t nexp(int C) { return C == 128 ? 3 : 1; }
@@ -56,12 +43,6 @@ int forward_mode_check(int mode, int C, int N, int S, int dk, int dv, bool prep)
 int order_ok(int C, int N, int S) {
   const int lim = (C == 128 ? 64 : C) - 1;  // C = 128 runs 64-blocks
   return N >= 0 && S >= 0 && N <= lim && S <= lim;
-}
-
-int hip_status(hipError_t e) {
-  if (e == hipSuccess) return GDN_OK;
-  if (e == hipErrorNotSupported) return GDN_ERR_UNSUPPORTED;
-  return GDN_ERR_HIP;
 }
 
 // common checks of the [B, L, H, d] entry points (one workgroup of `block`

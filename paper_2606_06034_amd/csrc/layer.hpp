@@ -1,0 +1,25 @@
+// layer.hpp -- host-side launchers of the layer's training and serving
+// operators (internal; arguments validated by api_layer.cpp).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gdn {
+
+hipError_t launch_recurrent(const void* Q, const void* K, const void* V, const float* beta,
+                            const float* g, const float* S0, void* O, float* Sfin,
+                            const int* slots, int n_states, const int* cu, int nseq, int T, int Hk,
+                            int Hv, int dk, int dv, float scale, int dtype, hipStream_t st);
+
+hipError_t launch_norm_forward(const void* x, const void* w, const void* b, const void* z, void* y,
+                               float* mean, float* rstd, int64_t rows, int D, float eps, bool rms,
+                               int dtype, int w_dtype, hipStream_t st);
+hipError_t launch_norm_backward(const void* dy, const void* x, const void* w, const void* b,
+                                const void* z, const float* mean, const float* rstd, void* dx,
+                                float* dw, float* db, void* dz, float* ws, int64_t rows, int D,
+                                bool rms, int dtype, int w_dtype, hipStream_t st);
+// rows of partial sums of dw (and as many of db) that launch_norm_backward writes
+int norm_backward_parts(int64_t rows, int D);
+
+}  // namespace gdn

@@ -1,0 +1,115 @@
+"""The C ABI of gdnlayer.h on the CPU: every declared symbol is exported and
+bound, and bad arguments are refused before anything reaches the GPU (no call
+here passes validation with work to do)."""
+
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import paper_2606_06034_amd as G
+
+HDR = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
+                   "gdnlayer.h")
+OK, NULL, SHAPE, PARAM, DTYPE, ALIGN, ALIAS, UNSUP, WS = 0, -1, -2, -3, -4, -5, -6, -8, -9
+P = [k << 40 for k in range(1, 20)]  # aligned addresses far apart
+L = G.lib
+
+
+def test_exports_every_declared_symbol():
+    names = sorted(set(re.findall(r"^int (gdn_\w+)\s*\(", open(HDR).read(), re.M)))
+    assert names == sorted(G.layer_abi_symbols())
+    for n in names:
+        assert hasattr(L, n), n
+
+
+def call(f, args, **change):
+    a = dict(args, **change)
+    return f(*a.values())
+
+
+REC = dict(Q=P[0], K=P[1], V=P[2], beta=P[3], g=P[4], S0=P[5], O=P[6], S_final=P[7], slots=None,
+           n_states=4, cu=None, nseq=4, T=2, Hk=2, Hv=4, dk=128, dv=64, scale=1.0, dtype=1,
+           stream=None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(nseq=-1), SHAPE), (dict(T=-1), SHAPE), (dict(n_states=-1), SHAPE),
+    (dict(Hk=3), SHAPE), (dict(Hk=0), SHAPE), (dict(Hk=-2), SHAPE), (dict(dk=96), SHAPE),
+    (dict(dv=32), SHAPE), (dict(n_states=3), SHAPE), (dict(nseq=1 << 30, n_states=1 << 30), SHAPE),
+    (dict(dtype=2), DTYPE), (dict(Q=None), NULL), (dict(K=None), NULL), (dict(V=None), NULL),
+    (dict(beta=None), NULL), (dict(g=None), NULL), (dict(O=None), NULL),
+    (dict(Q=P[0] + 8), ALIGN), (dict(S0=P[5] + 4), ALIGN), (dict(slots=P[8] + 4), ALIGN),
+    (dict(cu=P[8] + 4), ALIGN), (dict(O=P[0]), ALIAS), (dict(S_final=P[5] + 16), ALIAS),
+    (dict(S_final=P[6]), ALIAS), (dict(O=P[5]), ALIAS),
+    (dict(nseq=0), OK), (dict(Hk=0, Hv=0), OK),
+])
+def test_recurrent_refusals(change, code):
+    assert call(L.gdn_recurrent_forward, REC, **change) == code
+
+
+NF = dict(x=P[0], w=P[1], b=P[2], z=P[3], y=P[4], mean=P[5], rstd=P[6], rows=8, D=100, eps=1e-6,
+          kind=0, dtype=1, wdt=0, stream=None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(rows=-1), SHAPE), (dict(rows=1 << 31), SHAPE), (dict(D=0), SHAPE),
+    (dict(D=65537), SHAPE), (dict(kind=2), PARAM), (dict(eps=-1.0), PARAM),
+    (dict(eps=float("nan")), PARAM), (dict(dtype=2), DTYPE), (dict(wdt=2), DTYPE),
+    (dict(x=None), NULL), (dict(y=None), NULL), (dict(x=P[0] + 4), ALIGN),
+    (dict(rstd=P[6] + 8), ALIGN), (dict(y=P[0]), ALIAS), (dict(mean=P[6]), ALIAS),
+    (dict(rows=0), OK),
+])
+def test_norm_forward_refusals(change, code):
+    assert call(L.gdn_norm_forward, NF, **change) == code
+
+
+NB = dict(dy=P[0], x=P[1], w=P[2], b=P[3], z=P[4], mean=P[5], rstd=P[6], dx=P[7], dw=P[8],
+          db=P[9], dz=P[10], ws=P[11], wsb=1 << 30, rows=8, D=100, kind=0, dtype=1, wdt=0,
+          stream=None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(rows=-1), SHAPE), (dict(D=0), SHAPE), (dict(kind=-1), PARAM), (dict(dtype=7), DTYPE),
+    (dict(wdt=-1), DTYPE), (dict(dy=None), NULL), (dict(x=None), NULL), (dict(mean=None), NULL),
+    (dict(rstd=None), NULL), (dict(dx=None), NULL), (dict(dz=None), NULL), (dict(ws=None), NULL),
+    (dict(wsb=8 * 100 * 8 - 1), WS), (dict(dw=P[8] + 4), ALIGN), (dict(dx=P[0]), ALIAS),
+    (dict(db=P[8]), ALIAS), (dict(dz=P[4]), ALIAS), (dict(ws=P[1]), ALIAS),
+])
+def test_norm_backward_refusals(change, code):
+    assert call(L.gdn_norm_backward, NB, **change) == code
+
+
+def test_norm_backward_workspace():
+    n = ctypes.c_int64()
+    assert L.gdn_norm_backward_workspace(10, 33, ctypes.byref(n)) == OK
+    assert n.value == 10 * 33 * 8  # a row of sums a workgroup, dw and db
+    assert L.gdn_norm_backward_workspace(10, 33, None) == NULL
+    assert L.gdn_norm_backward_workspace(-1, 33, ctypes.byref(n)) == SHAPE
+    assert G.gdn_norm_backward_workspace(0, 33) == 0
+
+
+def test_binding_refuses_before_the_library():
+    k, v = torch.zeros(2, 1, 2, 64), torch.zeros(2, 1, 4, 64)
+    b = torch.zeros(2, 1, 4)
+    with pytest.raises(ValueError, match="device tensor"):
+        G.gdn_recurrent_forward(k, k, v, b, b)
+    with pytest.raises(ValueError, match="multiple of the key heads"):
+        G.gdn_recurrent_forward(k, k, torch.zeros(2, 1, 3, 64), b, b)
+    with pytest.raises(ValueError, match="B = 1"):
+        G.gdn_recurrent_forward(k, k, v, b, b, cu_seqlens=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="S_final"):
+        G.gdn_recurrent_forward(k, k, v, b, b, slots=torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(TypeError, match="dtype"):
+        G.gdn_recurrent_forward(k, k.half(), v, b, b)
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="kind"):
+        G.gdn_norm_forward(x, kind="batch")
+    with pytest.raises(ValueError, match="device tensor"):
+        G.gdn_norm_forward(x)
+    with pytest.raises(TypeError, match="weight"):
+        G.gdn_norm_forward(x, torch.zeros(8, dtype=torch.float64))
+    with pytest.raises(ValueError, match="mean"):
+        G.gdn_norm_backward(x, x, None, torch.zeros(4), kind="layer")
