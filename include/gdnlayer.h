@@ -1,10 +1,11 @@
 /*
  * gdnlayer.h -- C ABI of the operators that train and serve a Gated DeltaNet
  * layer around the chunk-wise forward of gdninv.h: the recurrent (token by
- * token) form, and the norms of the layer's input and output.  Same library (libgdninv.so), status codes, dtypes and conventions as
- * gdninv.h: device pointers owned by the caller, 16-byte aligned, dense and
- * row-major; work is only enqueued on `stream`; arguments are validated
- * before anything is enqueued; no memory is allocated.
+ * token) form, the chunk-wise backward pass, and the norms of the layer's
+ * input and output.  Same library (libgdninv.so), status codes, dtypes and
+ * conventions as gdninv.h: device pointers owned by the caller, 16-byte
+ * aligned, dense and row-major; work is only enqueued on `stream`; arguments
+ * are validated before anything is enqueued; no memory is allocated.
  *
  * Shared key heads.  Q and K hold Hk heads and V, O, beta, g Hv heads, Hv a
  * multiple of Hk: value head h reads key head h / (Hv / Hk).
@@ -43,6 +44,46 @@ int gdn_recurrent_forward(const void* Q, const void* K, const void* V, const flo
                           const int32_t* slots, int n_states, const int32_t* cu_seqlens, int nseq,
                           int T, int Hk, int Hv, int dk, int dv, float scale, int dtype,
                           void* stream);
+
+/* Gradients of the layer forward gdn_chunk_forward computes with the exact
+ * inverse (exact = 1): from dO and, where given, dS_final (the gradient of
+ * the final state; NULL: zero) those of Q, K, V, beta, g and S0.  Nothing of
+ * the forward pass is kept for it; the states are formed again.
+ * Q, K, dQ, dK [B, L, Hk, dk]; V, dO, dV [B, L, Hv, dv] in dtype (GDN_F32 or
+ * GDN_BF16); beta, g, dbeta, dg [B, L, Hv] fp32; S0 (NULL: zero states),
+ * dS_final, dS0 (nullable: not formed) [B, Hv, dk, dv] fp32.  g is the
+ * cumulative log-decay inside chunks of C tokens (C in {16, 32, 64}) from the
+ * start of each sequence, as for gdn_chunk_forward, and dg the gradient of g
+ * as given; L need not be a multiple of C.  The gradients of a key head sum
+ * over its group of value heads.  Everything is formed in fp32 (bf16 inputs
+ * enter unrounded) and rounded once at the end, in a fixed order: the same
+ * call gives the same bits.
+ * workspace: at least gdn_chunk_backward_workspace() bytes, contents
+ * undefined on return.  dk, dv in {64, 128}.  Four launches on `stream`. */
+int gdn_chunk_backward(const void* Q, const void* K, const void* V, const float* beta,
+                       const float* g, const void* dO, const float* S0, const float* dS_final,
+                       void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS0,
+                       void* workspace, int64_t workspace_bytes, int B, int L, int Hk, int Hv,
+                       int dk, int dv, int C, float scale, int dtype, void* stream);
+
+/* The same over packed sequences, as gdn_chunk_forward_varlen runs them: the
+ * tensors hold T tokens, sequence s those of cu_seqlens[s] .. cu_seqlens[s +
+ * 1] - 1 (nseq + 1 int32 offsets on the device, non-decreasing, within
+ * 0 .. T); the states are [nseq, Hv, dk, dv].  A sequence whose offsets are
+ * out of range is taken as empty (dS0 = dS_final); tokens outside every
+ * sequence get no gradients written. */
+int gdn_chunk_backward_varlen(const void* Q, const void* K, const void* V, const float* beta,
+                              const float* g, const void* dO, const float* S0,
+                              const float* dS_final, void* dQ, void* dK, void* dV, float* dbeta,
+                              float* dg, float* dS0, void* workspace, int64_t workspace_bytes,
+                              const int32_t* cu_seqlens, int nseq, int T, int Hk, int Hv, int dk,
+                              int dv, int C, float scale, int dtype, void* stream);
+
+/* Workspace bytes of gdn_chunk_backward for nseq = B sequences of L tokens
+ * (packed = 0), or of gdn_chunk_backward_varlen for nseq sequences of L = T
+ * tokens in all (packed = 1). */
+int gdn_chunk_backward_workspace(int nseq, int L, int Hv, int dk, int dv, int packed,
+                                 int64_t* bytes);
 
 enum gdn_norm_kind { GDN_NORM_LAYER = 0, GDN_NORM_RMS = 1 };
 

@@ -50,6 +50,9 @@ from ._binding import (  # noqa: F401
 from ._layer import (  # noqa: F401
     GDN_NORM_LAYER,
     GDN_NORM_RMS,
+    gdn_chunk_backward,
+    gdn_chunk_backward_varlen,
+    gdn_chunk_backward_workspace,
     gdn_norm_backward,
     gdn_norm_backward_workspace,
     gdn_norm_forward,

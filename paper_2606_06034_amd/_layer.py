@@ -1,6 +1,6 @@
 """ctypes marshalling for the operators of include/gdnlayer.h (same library
-and manner as _binding.py): the recurrent gated delta rule and the norms of
-the layer."""
+and manner as _binding.py): the recurrent gated delta rule, the chunk-wise
+backward pass and the norms of the layer."""
 
 from __future__ import annotations
 
@@ -17,6 +17,9 @@ _c_int, _c_i64, _c_f, _vp = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes
 
 _SIGS = {
     "gdn_recurrent_forward": [_vp] * 9 + [_c_int, _vp] + [_c_int] * 6 + [_c_f, _c_int, _vp],
+    "gdn_chunk_backward": [_vp] * 15 + [_c_i64] + [_c_int] * 7 + [_c_f, _c_int, _vp],
+    "gdn_chunk_backward_varlen": [_vp] * 15 + [_c_i64, _vp] + [_c_int] * 7 + [_c_f, _c_int, _vp],
+    "gdn_chunk_backward_workspace": [_c_int] * 6 + [ctypes.POINTER(_c_i64)],
     "gdn_norm_forward": [_vp] * 7 + [_c_i64, _c_int, _c_f] + [_c_int] * 3 + [_vp],
     "gdn_norm_backward": [_vp] * 12 + [_c_i64, _c_i64] + [_c_int] * 4 + [_vp],
     "gdn_norm_backward_workspace": [_c_i64, _c_int, ctypes.POINTER(_c_i64)],
@@ -83,6 +86,82 @@ def gdn_recurrent_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, bet
         n, _opt(cu_seqlens, "cu_seqlens", torch.int32), nseq, T, Hk, Hv, dk, dv, scale, dt,
         _stream(stream)))
     return O, S_final
+
+
+def gdn_chunk_backward_workspace(nseq: int, L: int, Hv: int, dk: int, dv: int,
+                                 packed: bool = False) -> int:
+    """Bytes of workspace gdn_chunk_backward needs for nseq sequences of L tokens, or with
+    packed gdn_chunk_backward_varlen for nseq sequences of L tokens in all."""
+    n = _c_i64()
+    _check("gdn_chunk_backward_workspace", lib.gdn_chunk_backward_workspace(
+        nseq, L, Hv, dk, dv, int(packed), ctypes.byref(n)))
+    return n.value
+
+
+def _backward(fn, Q, K, V, beta, g, dO, C, cu, S0, dS_final, scale, want_dS0, out, workspace,
+              stream):
+    B, L, Hk, dk = K.shape
+    Hv, dv = V.shape[-2:]
+    _groups(Hk, Hv)
+    dt = _fdtype(K, "K")
+    nseq = B if cu is None else cu.numel() - 1
+    if nseq < 0:
+        raise ValueError("cu_seqlens must hold nseq + 1 offsets")
+    scale = dk ** -0.5 if scale is None else float(scale)
+    tok, states = B * L, nseq * Hv * dk * dv
+    dQ, dK, dV, dbeta, dg, dS0 = out if out is not None else (None,) * 6
+    dQ = torch.empty_like(K) if dQ is None else dQ
+    dK = torch.empty_like(K) if dK is None else dK
+    dV = torch.empty_like(V) if dV is None else dV
+    dbeta = torch.empty_like(beta) if dbeta is None else dbeta
+    dg = torch.empty_like(g) if dg is None else dg
+    if want_dS0 and dS0 is None:
+        dS0 = torch.empty((nseq, Hv, dk, dv), dtype=torch.float32, device=K.device)
+    if workspace is None:
+        need = gdn_chunk_backward_workspace(nseq, L, Hv, dk, dv, cu is not None)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=K.device)
+    f32 = torch.float32
+    args = [_dev(Q, "Q", K.dtype, tok * Hk * dk), _dev(K, "K"), _dev(V, "V", K.dtype, tok * Hv * dv),
+            _dev(beta, "beta", f32, tok * Hv), _dev(g, "g", f32, tok * Hv),
+            _dev(dO, "dO", K.dtype, tok * Hv * dv), _opt(S0, "S0", f32, states),
+            _opt(dS_final, "dS_final", f32, states), _dev(dQ, "dQ", K.dtype, tok * Hk * dk),
+            _dev(dK, "dK", K.dtype, tok * Hk * dk), _dev(dV, "dV", K.dtype, tok * Hv * dv),
+            _dev(dbeta, "dbeta", f32, tok * Hv), _dev(dg, "dg", f32, tok * Hv),
+            _opt(dS0, "dS0", f32, states), _dev(workspace, "workspace"),
+            workspace.numel() * workspace.element_size()]
+    if cu is not None:
+        args.append(_dev(cu, "cu_seqlens", torch.int32))
+    _check(fn, getattr(lib, fn)(*args, nseq, L, Hk, Hv, dk, dv, C, scale, dt, _stream(stream)))
+    return dQ, dK, dV, dbeta, dg, dS0
+
+
+def gdn_chunk_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, beta: torch.Tensor,
+                       g: torch.Tensor, dO: torch.Tensor, C: int,
+                       S0: Optional[torch.Tensor] = None,
+                       dS_final: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                       want_dS0: bool = False, out=None,
+                       workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of gdn_chunk_forward(..., inverse="exact"): (dQ, dK, dV, dbeta, dg, dS0 or
+    None) from dO and, where given, the gradient of its final state.  Q, K [B, L, Hk, dk], V,
+    dO [B, L, Hv, dv], beta, g [B, L, Hv]; L need not be a multiple of C.  out: the six outputs
+    (None where one is to be allocated).  The workspace (a byte tensor of
+    gdn_chunk_backward_workspace() bytes) is allocated when not given."""
+    return _backward("gdn_chunk_backward", Q, K, V, beta, g, dO, C, None, S0, dS_final, scale,
+                     want_dS0, out, workspace, stream)
+
+
+def gdn_chunk_backward_varlen(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                              beta: torch.Tensor, g: torch.Tensor, dO: torch.Tensor, tables,
+                              C: int, S0: Optional[torch.Tensor] = None,
+                              dS_final: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, want_dS0: bool = False, out=None,
+                              workspace: Optional[torch.Tensor] = None, stream=None):
+    """The same over packed sequences (B = 1): tables = gdn_varlen_tables(cu_seqlens, C), of
+    which the token offsets are read; S0, dS_final, dS0 [nseq, Hv, dk, dv]."""
+    if K.shape[0] != 1:
+        raise ValueError("packed sequences use B = 1")
+    return _backward("gdn_chunk_backward_varlen", Q, K, V, beta, g, dO, C, tables[0], S0,
+                     dS_final, scale, want_dS0, out, workspace, stream)
 
 
 _KINDS = {"layer": GDN_NORM_LAYER, "rms": GDN_NORM_RMS}

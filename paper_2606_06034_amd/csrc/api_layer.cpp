@@ -68,6 +68,72 @@ int gdn_recurrent_forward(const void* Q, const void* K, const void* V, const flo
                                           dk, dv, scale, dtype, (hipStream_t)stream));
 }
 
+int gdn_chunk_backward_workspace(int nseq, int L, int Hv, int dk, int dv, int packed,
+                                 int64_t* bytes) {
+  if (!bytes) return GDN_ERR_NULL;
+  if (nseq < 0 || L < 0 || Hv < 0 || !valid_d(dk) || !valid_d(dv)) return GDN_ERR_SHAPE;
+  const int64_t slots = L > 0 && nseq > 0 ? gdn::backward_slots(nseq, L, packed != 0) : 0;
+  if (Hv > 0 && (!grid_ok(slots, 256) || !grid_ok(slots * Hv, 256))) return GDN_ERR_SHAPE;
+  *bytes = slots * Hv * gdn::backward_tile_bytes(dk, dv);
+  return GDN_OK;
+}
+
+namespace {
+int backward(const void* Q, const void* K, const void* V, const float* beta, const float* g,
+             const void* dO, const float* S0, const float* dS_final, void* dQ, void* dK, void* dV,
+             float* dbeta, float* dg, float* dS0, void* workspace, int64_t workspace_bytes,
+             const int32_t* cu, bool packed, int nseq, int L, int Hk, int Hv, int dk, int dv,
+             int C, float scale, int dtype, void* stream) {
+  if (!valid_heads(Hk, Hv)) return GDN_ERR_SHAPE;
+  if (!(C == 16 || C == 32 || C == 64)) return C == 128 ? GDN_ERR_UNSUPPORTED : GDN_ERR_SHAPE;
+  int64_t need = 0;
+  if (int r = gdn_chunk_backward_workspace(nseq, L, Hv, dk, dv, packed, &need)) return r;
+  if (!grid_ok((int64_t)nseq * Hv * (dv / 16), 256)) return GDN_ERR_SHAPE;
+  if (!fdtype(dtype)) return GDN_ERR_DTYPE;
+  if ((int64_t)nseq * Hv == 0) return GDN_OK;
+  if (packed && !cu) return GDN_ERR_NULL;
+  const int64_t tok = packed ? (int64_t)L : (int64_t)nseq * L, es = esize(dtype);
+  if (tok > 0) {
+    if (!Q || !K || !V || !beta || !g || !dO || !dQ || !dK || !dV || !dbeta || !dg || !workspace)
+      return GDN_ERR_NULL;
+    if (workspace_bytes < need) return GDN_ERR_WORKSPACE;
+  } else {
+    Q = K = V = dO = nullptr, beta = g = nullptr, dQ = dK = dV = workspace = nullptr;
+    dbeta = dg = nullptr;
+  }
+  const int64_t kb = tok * Hk * dk * es, vb = tok * Hv * dv * es, bb = tok * Hv * 4;
+  const int64_t sb = (int64_t)nseq * Hv * dk * dv * 4;
+  const Span in[9] = {{Q, kb},  {K, kb},   {V, vb},         {beta, bb},          {g, bb},
+                      {dO, vb}, {S0, sb}, {dS_final, sb}, {cu, 4ll * (nseq + 1)}};
+  const Span out[7] = {{dQ, kb}, {dK, kb},  {dV, vb},          {dbeta, bb},
+                       {dg, bb}, {dS0, sb}, {workspace, need}};
+  if (int r = check_spans(in, 9, out, 7)) return r;
+  return hip_status(gdn::launch_backward(Q, K, V, beta, g, dO, S0, dS_final, dQ, dK, dV, dbeta, dg,
+                                         dS0, (float*)workspace, cu, nseq, L, Hk, Hv, dk, dv, C,
+                                         scale, dtype, (hipStream_t)stream));
+}
+}  // namespace
+
+int gdn_chunk_backward(const void* Q, const void* K, const void* V, const float* beta,
+                       const float* g, const void* dO, const float* S0, const float* dS_final,
+                       void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS0,
+                       void* workspace, int64_t workspace_bytes, int B, int L, int Hk, int Hv,
+                       int dk, int dv, int C, float scale, int dtype, void* stream) {
+  return backward(Q, K, V, beta, g, dO, S0, dS_final, dQ, dK, dV, dbeta, dg, dS0, workspace,
+                  workspace_bytes, nullptr, false, B, L, Hk, Hv, dk, dv, C, scale, dtype, stream);
+}
+
+int gdn_chunk_backward_varlen(const void* Q, const void* K, const void* V, const float* beta,
+                              const float* g, const void* dO, const float* S0,
+                              const float* dS_final, void* dQ, void* dK, void* dV, float* dbeta,
+                              float* dg, float* dS0, void* workspace, int64_t workspace_bytes,
+                              const int32_t* cu_seqlens, int nseq, int T, int Hk, int Hv, int dk,
+                              int dv, int C, float scale, int dtype, void* stream) {
+  return backward(Q, K, V, beta, g, dO, S0, dS_final, dQ, dK, dV, dbeta, dg, dS0, workspace,
+                  workspace_bytes, cu_seqlens, true, nseq, T, Hk, Hv, dk, dv, C, scale, dtype,
+                  stream);
+}
+
 namespace {
 int check_norm(int64_t rows, int D, int kind, int dtype, int w_dtype) {
   if (rows < 0 || rows > 0x7fffffffLL || D < 1 || D > 65536) return GDN_ERR_SHAPE;

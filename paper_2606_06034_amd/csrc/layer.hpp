@@ -22,4 +22,15 @@ hipError_t launch_norm_backward(const void* dy, const void* x, const void* w, co
 // rows of partial sums of dw (and as many of db) that launch_norm_backward writes
 int norm_backward_parts(int64_t rows, int D);
 
+// Chunk-wise backward pass; ws holds backward_slots() * Hv tiles of
+// backward_tile_bytes().  cu (nullable): nseq + 1 token offsets on the device,
+// then L is the number of all tokens, else of each sequence's.
+int64_t backward_slots(int nseq, int L, bool packed);
+int64_t backward_tile_bytes(int dk, int dv);
+hipError_t launch_backward(const void* Q, const void* K, const void* V, const float* beta,
+                           const float* g, const void* dO, const float* S0, const float* dSf,
+                           void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS0,
+                           float* ws, const int* cu, int nseq, int L, int Hk, int Hv, int dk,
+                           int dv, int C, float scale, int dtype, hipStream_t st);
+
 }  // namespace gdn

@@ -91,6 +91,49 @@ def test_norm_backward_workspace():
     assert G.gdn_norm_backward_workspace(0, 33) == 0
 
 
+BWD = dict(Q=P[0], K=P[1], V=P[2], beta=P[3], g=P[4], dO=P[5], S0=P[6], dSf=P[7], dQ=P[8], dK=P[9],
+           dV=P[10], dbeta=P[11], dg=P[12], dS0=P[13], ws=P[14], wsb=1 << 39, B=2, L=100, Hk=2,
+           Hv=4, dk=128, dv=64, C=64, scale=1.0, dtype=1, stream=None)
+BWD_BAD = [
+    (dict(L=-1), SHAPE), (dict(Hk=3), SHAPE), (dict(Hk=0), SHAPE), (dict(dk=32), SHAPE),
+    (dict(dv=256), SHAPE), (dict(C=48), SHAPE), (dict(C=0), SHAPE), (dict(C=128), UNSUP),
+    (dict(dtype=2), DTYPE), (dict(Q=None), NULL), (dict(K=None), NULL), (dict(V=None), NULL),
+    (dict(beta=None), NULL), (dict(g=None), NULL), (dict(dO=None), NULL), (dict(dQ=None), NULL),
+    (dict(dK=None), NULL), (dict(dV=None), NULL), (dict(dbeta=None), NULL), (dict(dg=None), NULL),
+    (dict(ws=None), NULL), (dict(wsb=1000), WS), (dict(dO=P[5] + 2), ALIGN),
+    (dict(dS0=P[13] + 4), ALIGN), (dict(dQ=P[0]), ALIAS), (dict(dK=P[8]), ALIAS),
+    (dict(dS0=P[7]), ALIAS), (dict(ws=P[2]), ALIAS), (dict(Hk=0, Hv=0), OK)]
+
+
+@pytest.mark.parametrize("change,code", BWD_BAD + [
+    (dict(B=-1), SHAPE), (dict(B=1 << 20, L=1 << 20), SHAPE), (dict(B=0), OK)])
+def test_backward_refusals(change, code):
+    assert call(L.gdn_chunk_backward, BWD, **change) == code
+
+
+@pytest.mark.parametrize("change,code", BWD_BAD + [
+    (dict(nseq=-1), SHAPE), (dict(nseq=0), OK), (dict(cu=None), NULL), (dict(cu=P[15] + 4), ALIGN),
+    (dict(dg=P[15]), ALIAS)])
+def test_packed_backward_refusals(change, code):
+    a = {}
+    for k, v in BWD.items():
+        if k == "B":
+            a.update(cu=P[15], nseq=3)
+        else:
+            a[k] = v
+    assert call(L.gdn_chunk_backward_varlen, a, **change) == code
+
+
+def test_backward_workspace():
+    tile = 4 * (2 * 64 * 64 + 5 * 64 + 2 * 64 * 128 + 2 * 128 * 128)
+    assert G.gdn_chunk_backward_workspace(2, 100, 3, 128, 128) == 2 * 2 * 3 * tile
+    assert G.gdn_chunk_backward_workspace(5, 100, 3, 128, 128, packed=True) == (1 + 5) * 3 * tile
+    assert G.gdn_chunk_backward_workspace(2, 0, 3, 128, 128) == 0
+    assert L.gdn_chunk_backward_workspace(2, 100, 3, 128, 128, 0, None) == NULL
+    with pytest.raises(G.GdnError):
+        G.gdn_chunk_backward_workspace(2, 100, 3, 96, 128)
+
+
 def test_binding_refuses_before_the_library():
     k, v = torch.zeros(2, 1, 2, 64), torch.zeros(2, 1, 4, 64)
     b = torch.zeros(2, 1, 4)
@@ -104,6 +147,10 @@ def test_binding_refuses_before_the_library():
         G.gdn_recurrent_forward(k, k, v, b, b, slots=torch.zeros(2, dtype=torch.int32))
     with pytest.raises(TypeError, match="dtype"):
         G.gdn_recurrent_forward(k, k.half(), v, b, b)
+    with pytest.raises(ValueError, match="B = 1"):
+        G.gdn_chunk_backward_varlen(k, k, v, b, b, v, (None, None, 0), 64)
+    with pytest.raises(ValueError, match="device tensor"):
+        G.gdn_chunk_backward(k, k, v, b, b, v, 64)
     x = torch.zeros(4, 8)
     with pytest.raises(ValueError, match="kind"):
         G.gdn_norm_forward(x, kind="batch")
