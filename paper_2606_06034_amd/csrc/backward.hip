@@ -35,6 +35,7 @@
 #include "engine.hpp"
 #include "launch.hpp"
 #include "layer.hpp"
+#include "split.hpp"
 
 namespace gdn {
 
@@ -42,10 +43,14 @@ namespace {
 
 constexpr int BC = 64;  // tokens a chunk
 
-// workspace of one (chunk, value head), in floats
+// Workspace of one (chunk, value head), in floats.  T and T^T lie as the pair
+// fragments of their row blocks (tile16.hpp), 512 values each: T (I, p) with
+// 2p <= I, T^T (I, p) with 2p + 1 >= I.
+__host__ __device__ constexpr int t_slot(int I, int p) { return (I == 3 ? 4 : I) + p; }
+__host__ __device__ constexpr int tt_slot(int I, int p) { return (I < 2 ? 2 * I : 2 + I) + p - I / 2; }
 __host__ __device__ constexpr int64_t ws_T() { return 0; }
-__host__ __device__ constexpr int64_t ws_Tt() { return BC * BC; }
-__host__ __device__ constexpr int64_t ws_rows() { return 2 * BC * BC; }  // beta e^g e^{gl-g} g off
+__host__ __device__ constexpr int64_t ws_Tt() { return 6 * 512; }
+__host__ __device__ constexpr int64_t ws_rows() { return 12 * 512; }  // beta e^g e^{gl-g} g off
 __host__ __device__ constexpr int64_t ws_R() { return ws_rows() + 5 * BC; }  // P^T dO, then dZ
 __host__ __device__ constexpr int64_t ws_X(int dv) { return ws_R() + BC * dv; }
 __host__ __device__ constexpr int64_t ws_S(int dv) { return ws_X(dv) + BC * dv; }
@@ -139,16 +144,27 @@ __device__ __forceinline__ void rows_to_lds(float* s, const T* __restrict__ x, i
   }
 }
 
-// column-form block of rows r0 .. r0 + 15, columns from p's
+// column-form block of rows r0 .. r0 + 15, columns from p's: as loaded (rows
+// past m repeat the last one, so that no load is behind a branch), and its
+// values (0 past m)
+template <typename T> struct RawBlock { T v[4]; };
+template <typename T>
+__device__ __forceinline__ RawBlock<T> raw_block(const T* __restrict__ p, int64_t ld, int r0, int m) {
+  RawBlock<T> x;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) x.v[v] = p[min(r0 + 4 * lane_g() + v, m - 1) * ld + lane_c()];
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ f32x4 block_of(const RawBlock<T>& x, int r0, int m) {
+  f32x4 r;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) r[v] = r0 + 4 * lane_g() + v < m ? (float)x.v[v] : 0.f;
+  return r;
+}
 template <typename T>
 __device__ __forceinline__ f32x4 col_block(const T* __restrict__ p, int64_t ld, int r0, int m) {
-  f32x4 x;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const int r = r0 + 4 * lane_g() + v;
-    x[v] = r < m ? load1(p + r * ld + lane_c()) : 0.f;
-  }
-  return x;
+  return block_of(raw_block(p, ld, r0, m), r0, m);
 }
 
 template <typename T> struct FragOf { typedef f32x4 type; };
@@ -231,15 +247,25 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
       for (int J = 0; J <= I; ++J)
         Lr.a[bidx(I, J)] = at4(sA + (16 * I + c) * LD + 16 * J + 4 * g);
     blockwise_inverse<4, f32x4>(Lr, Tr);
+    const f32x4 z = zero4();
 #pragma unroll
     for (int I = 0; I < 4; ++I)
 #pragma unroll
-      for (int J = 0; J <= I; ++J) {
-        const f32x4 x = Tr.a[bidx(I, J)];
-        *(f32x4*)(ws + ws_T() + (16 * I + c) * BC + 16 * J + 4 * g) = x;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) ws[ws_Tt() + (16 * J + 4 * g + v) * BC + 16 * I + c] = x[v];
+      for (int J = 0; J < 4; ++J) {
+        // (sA holds nothing that another wave reads)
+        if (J <= I) *(f32x4*)(sA + (16 * I + c) * LD + 16 * J + 4 * g) = Tr.a[bidx(I, J)];
+        if (J / 2 <= I / 2)
+          *(f32x4*)(ws + ws_T() + 512 * t_slot(I, J / 2) + 256 * (J & 1) + 4 * lane_id()) =
+              J <= I ? Tr.a[bidx(I, J)] : z;
       }
+    lds_sync<true>();
+#pragma unroll
+    for (int I = 0; I < 4; ++I)
+#pragma unroll
+      for (int J = 0; J < 4; ++J)
+        if (J / 2 >= I / 2)
+          *(f32x4*)(ws + ws_Tt() + 512 * tt_slot(I, J / 2) + 256 * (J & 1) + 4 * lane_id()) =
+              J >= I ? down4(sA + (16 * J + 4 * g) * LD + 16 * I + c, LD) : z;
   } else {
     const T* dO = (const T*)a.dO + (t0 * a.Hv + h) * DV;
     for (int J = wv - 1; J < DV / 16; J += 3) {
@@ -259,154 +285,305 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
   }
 }
 
-// ---- the states entering the chunks, 16 value columns a workgroup
+// A walk over the chunks of one (sequence, value head) for 16 value columns, four
+// waves.  The [dk, 16] part of the state lies in registers, wave w holding its
+// rows 32w .. 32w + 31 (two blocks, one pair).  A step is serial, so the
+// waves share each of its products: a product with the state is summed over
+// the waves' own rows (no wave needs another's state), the sums, then Z (dY)
+// and Y (dX) of row block w go through LDS, three exchanges a chunk.
 template <int DK, int DV, typename T>
-__global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
-  constexpr int PD = DK + 4, NS = DV / 16, NB = DK / 64;
-  __shared__ float sK[BC * PD], sS[DK * 16], sZ[BC * 16], sY[BC * 16];
-  const int64_t sh = blockIdx.x / NS;
-  const int n0 = (int)(blockIdx.x - sh * NS) * 16, s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
-  const Seq sq(a, s);
-  const int wv = threadIdx.x >> 6, l = lane_id(), g = lane_g(), c = lane_c(), nc = sq.chunks();
-  f32x4 st[NB];
+struct Walk {
+  typedef typename FragOf<T>::type F;
+  static constexpr int NT = TermsOf<F>::N, NQ = DK / 32, NS = DV / 16;
+  static constexpr int E = 16 / sizeof(T), LD = DK + E;  // rows in LDS, 16 bytes apart
+  static constexpr int CPR = DK / E, KI = BC * CPR / 256;
+  typedef T Vec __attribute__((ext_vector_type(E)));
+  // a chunk's rows of K (Q) on their way to LDS
+  struct Rows {
+    Vec v[KI];
+  };
+  static __device__ __forceinline__ void fetch(Rows& x, const T* __restrict__ p, int64_t ld, int m) {
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
-    st[b] = a.S0 ? col_block(a.S0 + sh * DK * DV + n0, DV, 16 * (NB * wv + b), DK) : zero4();
-  for (int ck = 0; ck < nc; ++ck) {
-    const int64_t t0 = sq.t0 + (int64_t)ck * BC;
-    const int m = min(BC, sq.len - ck * BC);
-    float* ws = a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV);
-    rows_to_lds<DK, PD>(sK, (const T*)a.K + (t0 * a.Hk + hk) * DK, (int64_t)a.Hk * DK, m);
+    for (int i = 0; i < KI; ++i) {
+      const int at = threadIdx.x + 256 * i, r = at / CPR;
+      x.v[i] = *(const Vec*)(p + min(r, m - 1) * ld + at % CPR * E);
+    }
+  }
+  static __device__ __forceinline__ void put(T* s, const Rows& x, int m) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int B = NB * wv + b;
-      *(f32x4*)(sS + 256 * B + 4 * l) = st[b];
+    for (int i = 0; i < KI; ++i) {
+      const int at = threadIdx.x + 256 * i, r = at / CPR;
+      *(Vec*)(s + r * LD + at % CPR * E) = r < m ? x.v[i] : Vec{};
+    }
+  }
+  // row block w of T (or T^T): fp32 pair fragments, two at most
+  struct TRow {
+    f32x4 v[2][2];
+  };
+  static __device__ __forceinline__ void fetch_t(TRow& x, const float* __restrict__ p, int n, int l) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (i < n) {
+        x.v[i][0] = at4(p + 512 * i + 4 * l);
+        x.v[i][1] = at4(p + 512 * i + 256 + 4 * l);
+      }
+  }
+  // this wave's share of the product of the 64 rows in LDS with the state
+  static __device__ __forceinline__ void share(const T* sK, const Terms<F>& s, float* part, int wv,
+                                               Lane ln) {
+#pragma unroll
+    for (int I = 0; I < 4; ++I)
+      *(f32x4*)(part + (4 * wv + I) * 256 + 4 * ln.id) =
+          mma_in<false>(row_pair<LD>(sK, 16 * I, 32 * wv, ln), s, zero4());
+  }
+  // the sum of the shares of row block wv
+  static __device__ __forceinline__ f32x4 sum(const float* part, int wv, int l) {
+    f32x4 x[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) x[q] = at4(part + (4 * q + wv) * 256 + 4 * l);
+    if constexpr (NQ == 4) return (x[0] + x[1]) + (x[2] + x[3]);
+    return x[0] + x[1];
+  }
+  // the transposed rows of this wave's two state blocks: [block][token pair]
+  struct Cols {
+    Pair<F> v[2][2];
+  };
+  static __device__ __forceinline__ void cols(Cols& x, const T* s, int wv, Lane ln) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) x.v[h][p] = col_pair<LD>(s, 32 * p, 32 * wv + 16 * h, ln);
+  }
+  static __device__ __forceinline__ void state_in(f32x4 (&st)[2], const float* p, int n0, int wv) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      st[h] = p && wv < NQ ? col_block(p + n0, DV, 32 * wv + 16 * h, DK) : zero4();
+  }
+  static __device__ __forceinline__ void state_out(float* p, const f32x4 (&st)[2], int n0, int wv) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
-        ws[ws_S(DV) + (int64_t)(16 * B + 4 * g + v) * DV + n0 + c] = st[b][v];
-    }
-    __syncthreads();
+        p[(int64_t)(32 * wv + 16 * h + 4 * lane_g() + v) * DV + n0 + lane_c()] = st[h][v];
+  }
+};
+
+// ---- the states entering the chunks
+template <int DK, int DV, typename T>
+__global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
+  typedef Walk<DK, DV, T> W;
+  typedef typename W::F F;
+  __shared__ __attribute__((aligned(16))) T sK[BC * W::LD];
+  __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
+  __shared__ __attribute__((aligned(16))) T sZ[2 * W::NT * 512], sY[2 * W::NT * 512];
+  const int64_t sh = blockIdx.x / W::NS;
+  const int n0 = (int)(blockIdx.x - sh * W::NS) * 16, s = (int)(sh / a.Hv);
+  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
+  const Seq sq(a, s);
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
+  const Lane ln = lane_here();
+  const int l = ln.id, g = ln.g(), c = ln.c(), r0 = 16 * wv + 4 * g;
+  const bool owner = wv < W::NQ;
+  const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
+  f32x4 st[2];
+  W::state_in(st, a.S0 ? a.S0 + sh * DK * DV : nullptr, n0, wv);
+  if (nc == 0) return;
+  auto tile = [&](int ck) { return a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV); };
+  auto rows = [&](int ck) { return min(BC, sq.len - ck * BC); };
+  // what a chunk needs besides K, asked for a chunk ahead
+  struct Ops {
+    RawBlock<T> v;
+    f32x4 beta, eg, er;
+    float el;
+    typename W::TRow t;
+  };
+  auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
+    const float* ws = tile(ck);
     const float* rv = ws + ws_rows();
-    const int r0 = 16 * wv + 4 * g;
-    {
-      f32x4 x = zero4();
+    W::fetch_t(x.t, ws + ws_T() + 512 * t_slot(wv, 0), wv / 2 + 1, l);
+    x.v = raw_block((const T*)a.V + ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0, vld, 16 * wv,
+                    rows(ck));
+    x.beta = at4(rv + r0);
+    x.eg = at4(rv + BC + r0);
+    x.er = at4(rv + 2 * BC + r0);
+    x.el = rv[2 * BC - 1];
+  };
+  auto keys = [&](typename W::Rows& x, int ck) __attribute__((always_inline)) {
+    W::fetch(x, (const T*)a.K + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, kld, rows(ck));
+  };
+  const int last = nc - 1;
+  Ops op, nx;
+  typename W::Rows kr;
+  keys(kr, 0);
+  fetch(op, 0);
+  W::put(sK, kr, rows(0));
+  keys(kr, min(1, last));
+  lds_only_barrier();
+  for (int ck = 0; ck < nc; ++ck) {
+    float* ws = tile(ck);
+    fetch(nx, min(ck + 1, last));
+    __builtin_amdgcn_sched_barrier(0);
+    Terms<F> tt[2];
 #pragma unroll
-      for (int k = 0; k < DK / 16; ++k)
-        x = mma16(at4(sK + (16 * wv + c) * PD + 16 * k + 4 * g), at4(sS + 256 * k + 4 * l), x);
-      const f32x4 vv = col_block((const T*)a.V + (t0 * a.Hv + h) * DV + n0, (int64_t)a.Hv * DV,
-                                 16 * wv, m);
-      x = vv - at4(rv + BC + r0) * x;
+    for (int p = 0; p < 2; ++p)
+      if (p <= wv / 2) tt[p] = split<F>(op.t.v[p][0], op.t.v[p][1]);
+    if (owner) {
+      W::state_out(ws + ws_S(DV), st, n0, wv);
+      W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
+    }
+    lds_only_barrier();
+    typename W::Cols kc;
+    if (owner) W::cols(kc, sK, wv, ln);
+    {
+      const f32x4 x = block_of(op.v, 16 * wv, rows(ck)) - op.eg * W::sum(part, wv, l);
 #pragma unroll
       for (int v = 0; v < 4; ++v) ws[ws_X(DV) + (r0 + v) * DV + n0 + c] = x[v];
-      *(f32x4*)(sZ + 256 * wv + 4 * l) = at4(rv + r0) * x;
+      store_half<F>(sZ, wv >> 1, wv & 1, split_half<F>(op.beta * x), l);
     }
-    __syncthreads();
+    lds_only_barrier();
+    W::put(sK, kr, rows(min(ck + 1, last)));
+    keys(kr, min(ck + 2, last));
+    __builtin_amdgcn_sched_barrier(0);
     {
       f32x4 y = zero4();
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k <= wv)
-          y = mma16(at4(ws + ws_T() + (16 * wv + c) * BC + 16 * k + 4 * g),
-                    at4(sZ + 256 * k + 4 * l), y);
-      *(f32x4*)(sY + 256 * wv + 4 * l) = at4(rv + 2 * BC + r0) * y;
+      for (int p = 0; p < 2; ++p)
+        if (p <= wv / 2) y = mma_both<false>(tt[p], load_terms<F>(sZ, p, l), y);
+      store_half<F>(sY, wv >> 1, wv & 1, split_half<F>(op.er * y), l);
     }
-    __syncthreads();
-    const float el = rv[BC + BC - 1];
+    lds_only_barrier();
+    if (owner) {
+      f32x4 x[2] = {zero4(), zero4()};
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      f32x4 x = zero4();
+      for (int p = 0; p < 2; ++p) {
+        const Terms<F> y = load_terms<F>(sY, p, l);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        x = mma16(down4(sK + (16 * k + 4 * g) * PD + 16 * (NB * wv + b) + c, PD),
-                  at4(sY + 256 * k + 4 * l), x);
-      st[b] = st[b] * el + x;
+        for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(kc.v[hf][p], y, x[hf]);
+      }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * op.el + x[hf];
     }
-    __syncthreads();
+    op = nx;
   }
 }
 
 // ---- the gradients of the states leaving the chunks, last chunk first
 template <int DK, int DV, typename T>
 __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
-  constexpr int PD = DK + 4, NS = DV / 16, NB = DK / 64;
-  __shared__ float sK[BC * PD], sQ[BC * PD], sS[DK * 16], sY[BC * 16], sX[BC * 16], sO[BC * 16];
-  const int64_t sh = blockIdx.x / NS;
-  const int n0 = (int)(blockIdx.x - sh * NS) * 16, s = (int)(sh / a.Hv);
+  typedef Walk<DK, DV, T> W;
+  typedef typename W::F F;
+  __shared__ __attribute__((aligned(16))) T sK[BC * W::LD], sQ[BC * W::LD];
+  __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
+  __shared__ __attribute__((aligned(16))) T sY[2 * W::NT * 512], sX[2 * W::NT * 512],
+      sO[2 * W::NT * 512];
+  const int64_t sh = blockIdx.x / W::NS;
+  const int n0 = (int)(blockIdx.x - sh * W::NS) * 16, s = (int)(sh / a.Hv);
   const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
   const Seq sq(a, s);
-  const int wv = threadIdx.x >> 6, l = lane_id(), g = lane_g(), c = lane_c(), nc = sq.chunks();
-  f32x4 st[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-    st[b] = a.dSf ? col_block(a.dSf + sh * DK * DV + n0, DV, 16 * (NB * wv + b), DK) : zero4();
-  for (int ck = nc - 1; ck >= 0; --ck) {
-    const int64_t t0 = sq.t0 + (int64_t)ck * BC;
-    const int m = min(BC, sq.len - ck * BC);
-    float* ws = a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV);
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
+  const Lane ln = lane_here();
+  const int l = ln.id, g = ln.g(), c = ln.c(), r0 = 16 * wv + 4 * g;
+  const bool owner = wv < W::NQ;
+  const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
+  f32x4 st[2];
+  W::state_in(st, a.dSf ? a.dSf + sh * DK * DV : nullptr, n0, wv);
+  auto tile = [&](int ck) { return a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV); };
+  auto rows = [&](int ck) { return min(BC, sq.len - ck * BC); };
+  auto vat = [&](int ck) { return ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0; };
+  struct Ops {
+    RawBlock<float> r;
+    RawBlock<T> o;
+    f32x4 beta, eg, er;
+    float el;
+    typename W::TRow t;
+  };
+  auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
+    const float* ws = tile(ck);
     const float* rv = ws + ws_rows();
-    const int r0 = 16 * wv + 4 * g;
-    const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
-    const int64_t kat = (t0 * a.Hk + hk) * DK, vat = (t0 * a.Hv + h) * DV + n0;
-    rows_to_lds<DK, PD>(sK, (const T*)a.K + kat, kld, m);
-    rows_to_lds<DK, PD>(sQ, (const T*)a.Q + kat, kld, m);
-    const f32x4 eg = at4(rv + BC + r0);
-    *(f32x4*)(sO + 256 * wv + 4 * l) =
-        col_block((const T*)a.dO + vat, vld, 16 * wv, m) * eg * a.scale;
+    W::fetch_t(x.t, ws + ws_Tt() + 512 * tt_slot(wv, wv / 2), 2 - wv / 2, l);
+    x.r = raw_block((const float*)ws + ws_R() + n0, DV, 16 * wv, BC);
+    x.o = raw_block((const T*)a.dO + vat(ck), vld, 16 * wv, rows(ck));
+    x.beta = at4(rv + r0);
+    x.eg = at4(rv + BC + r0);
+    x.er = at4(rv + 2 * BC + r0);
+    x.el = rv[2 * BC - 1];
+  };
+  auto keys = [&](typename W::Rows& x, const void* p, int ck) __attribute__((always_inline)) {
+    W::fetch(x, (const T*)p + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, kld, rows(ck));
+  };
+  if (nc > 0) {
+    Ops op, nx;
+    typename W::Rows kr, qr;
+    keys(kr, a.K, nc - 1);
+    keys(qr, a.Q, nc - 1);
+    fetch(op, nc - 1);
+    W::put(sK, kr, rows(nc - 1));
+    keys(kr, a.K, max(nc - 2, 0));
+    lds_only_barrier();
+    for (int ck = nc - 1; ck >= 0; --ck) {
+      float* ws = tile(ck);
+      fetch(nx, max(ck - 1, 0));
+      W::put(sQ, qr, rows(ck));
+      keys(qr, a.Q, max(ck - 1, 0));
+      __builtin_amdgcn_sched_barrier(0);
+      Terms<F> tt[2];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int B = NB * wv + b;
-      *(f32x4*)(sS + 256 * B + 4 * l) = st[b];
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        ws[ws_dS(DK, DV) + (int64_t)(16 * B + 4 * g + v) * DV + n0 + c] = st[b][v];
-    }
-    __syncthreads();
-    {
-      f32x4 x = zero4();
-#pragma unroll
-      for (int k = 0; k < DK / 16; ++k)
-        x = mma16(at4(sK + (16 * wv + c) * PD + 16 * k + 4 * g), at4(sS + 256 * k + 4 * l), x);
-      const f32x4 r = col_block(ws + ws_R() + n0, DV, 16 * wv, BC);
-      *(f32x4*)(sY + 256 * wv + 4 * l) = r + at4(rv + 2 * BC + r0) * x;
-    }
-    __syncthreads();
-    {
-      f32x4 z = zero4();
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k >= wv)
-          z = mma16(at4(ws + ws_Tt() + (16 * wv + c) * BC + 16 * k + 4 * g),
-                    at4(sY + 256 * k + 4 * l), z);
-      const f32x4 x = at4(rv + r0) * z;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        ws[ws_R() + (r0 + v) * DV + n0 + c] = z[v];
-        if (r0 + v < m) ((T*)a.dV)[vat + (r0 + v) * vld + c] = (T)x[v];
+      for (int p = 0; p < 2; ++p)
+        if (p < 2 - wv / 2) tt[p] = split<F>(op.t.v[p][0], op.t.v[p][1]);
+      store_half<F>(sO, wv >> 1, wv & 1, split_half<F>(block_of(op.o, 16 * wv, rows(ck)) * op.eg * a.scale), l);
+      if (owner) {
+        W::state_out(ws + ws_dS(DK, DV), st, n0, wv);
+        W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
       }
-      *(f32x4*)(sX + 256 * wv + 4 * l) = -eg * x;
-    }
-    __syncthreads();
-    const float el = rv[BC + BC - 1];
+      lds_only_barrier();
+      typename W::Cols kc;
+      if (owner) W::cols(kc, sK, wv, ln);
+      store_half<F>(sY, wv >> 1, wv & 1, split_half<F>(block_of(op.r, 0, BC) + op.er * W::sum(part, wv, l)), l);
+      lds_only_barrier();
+      W::put(sK, kr, rows(max(ck - 1, 0)));
+      keys(kr, a.K, max(ck - 2, 0));
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 x[2] = {zero4(), zero4()};
+      {
+        f32x4 z = zero4();
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      f32x4 x = zero4();
+        for (int p = 0; p < 2; ++p)
+          if (p < 2 - wv / 2)
+            z = mma_both<false>(tt[p], load_terms<F>(sY, p + wv / 2, l), z);
+        const f32x4 dx = op.beta * z;
+        store_half<F>(sX, wv >> 1, wv & 1, split_half<F>(-op.eg * dx), l);
+        const int m = rows(ck);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int at = (16 * k + 4 * g) * PD + 16 * (NB * wv + b) + c;
-        x = mma16(down4(sQ + at, PD), at4(sO + 256 * k + 4 * l), x);
-        x = mma16(down4(sK + at, PD), at4(sX + 256 * k + 4 * l), x);
+        for (int v = 0; v < 4; ++v) {
+          ws[ws_R() + (r0 + v) * DV + n0 + c] = z[v];
+          if (r0 + v < m) ((T*)a.dV)[vat(ck) + (r0 + v) * vld + c] = (T)dx[v];
+        }
+        if (owner) {
+          typename W::Cols qc;
+          W::cols(qc, sQ, wv, ln);
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const Terms<F> o = load_terms<F>(sO, p, l);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(qc.v[hf][p], o, x[hf]);
+          }
+        }
       }
-      st[b] = st[b] * el + x;
+      lds_only_barrier();
+      if (owner) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const Terms<F> y = load_terms<F>(sX, p, l);
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(kc.v[hf][p], y, x[hf]);
+        }
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * op.el + x[hf];
+      }
+      op = nx;
     }
-    __syncthreads();
   }
-  if (a.dS0)
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        a.dS0[sh * DK * DV + (int64_t)(16 * (NB * wv + b) + 4 * g + v) * DV + n0 + c] = st[b][v];
+  if (a.dS0 && owner) W::state_out(a.dS0 + sh * DK * DV, st, n0, wv);
 }
 
 // ---- every chunk: dQ, dK, dbeta, dg; the value heads of a key head in turn
@@ -468,7 +645,7 @@ __global__ __launch_bounds__(256) void k_bwd_grads(const BwdArgs a) {
         f32x4 y = zero4();
 #pragma unroll
         for (int k = 0; k <= I; ++k)
-          y = mma16(at4(ws + ws_T() + (16 * I + c) * BC + 16 * k + 4 * g), z[k], y);
+          y = mma16(at4(ws + ws_T() + 512 * t_slot(I, k / 2) + 256 * (k & 1) + 4 * lane_id()), z[k], y);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sY[(16 * I + 4 * g + v) * PV + 16 * J + c] = y[v];
       }
