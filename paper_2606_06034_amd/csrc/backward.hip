@@ -43,14 +43,15 @@ namespace {
 
 constexpr int BC = 64;  // tokens a chunk
 
-// Workspace of one (chunk, value head), in floats.  T and T^T lie as the pair
-// fragments of their row blocks (tile16.hpp), 512 values each: T (I, p) with
-// 2p <= I, T^T (I, p) with 2p + 1 >= I.
+// Workspace of one (chunk, value head), in floats.  T and T^T lie as the terms
+// (split.hpp) of the pair fragments of their row blocks, 3 KB a fragment (2 KB
+// with fp32 inputs): T (I, p) with 2p <= I, T^T (I, p) with 2p + 1 >= I.
+constexpr int TS = 768;
 __host__ __device__ constexpr int t_slot(int I, int p) { return (I == 3 ? 4 : I) + p; }
 __host__ __device__ constexpr int tt_slot(int I, int p) { return (I < 2 ? 2 * I : 2 + I) + p - I / 2; }
 __host__ __device__ constexpr int64_t ws_T() { return 0; }
-__host__ __device__ constexpr int64_t ws_Tt() { return 6 * 512; }
-__host__ __device__ constexpr int64_t ws_rows() { return 12 * 512; }  // beta e^g e^{gl-g} g off
+__host__ __device__ constexpr int64_t ws_Tt() { return 6 * TS; }
+__host__ __device__ constexpr int64_t ws_rows() { return 12 * TS; }  // beta e^g e^{gl-g} g off
 __host__ __device__ constexpr int64_t ws_R() { return ws_rows() + 5 * BC; }  // P^T dO, then dZ
 __host__ __device__ constexpr int64_t ws_X(int dv) { return ws_R() + BC * dv; }
 __host__ __device__ constexpr int64_t ws_S(int dv) { return ws_X(dv) + BC * dv; }
@@ -159,12 +160,23 @@ template <typename T>
 __device__ __forceinline__ f32x4 block_of(const RawBlock<T>& x, int r0, int m) {
   f32x4 r;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) r[v] = r0 + 4 * lane_g() + v < m ? (float)x.v[v] : 0.f;
+  for (int v = 0; v < 4; ++v) r[v] = (float)x.v[v];
+  if (m < r0 + 16)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) r[v] = r0 + 4 * lane_g() + v < m ? r[v] : 0.f;
   return r;
 }
 template <typename T>
 __device__ __forceinline__ f32x4 col_block(const T* __restrict__ p, int64_t ld, int r0, int m) {
   return block_of(raw_block(p, ld, r0, m), r0, m);
+}
+
+// one block of a pair's terms as values
+__device__ __forceinline__ f32x4 half_of(const Terms<f32x4>& x, int hf) {
+  return hf ? x.t[0].hi() : x.t[0].lo();
+}
+__device__ __forceinline__ f32x4 half_of(const Terms<bf16x4>& x, int hf) {
+  return hf ? x.t[0].hi() + (x.t[1].hi() + x.t[2].hi()) : x.t[0].lo() + (x.t[1].lo() + x.t[2].lo());
 }
 
 template <typename T> struct FragOf { typedef f32x4 type; };
@@ -255,8 +267,8 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
         // (sA holds nothing that another wave reads)
         if (J <= I) *(f32x4*)(sA + (16 * I + c) * LD + 16 * J + 4 * g) = Tr.a[bidx(I, J)];
         if (J / 2 <= I / 2)
-          *(f32x4*)(ws + ws_T() + 512 * t_slot(I, J / 2) + 256 * (J & 1) + 4 * lane_id()) =
-              J <= I ? Tr.a[bidx(I, J)] : z;
+          store_half<F>((T*)(ws + ws_T() + TS * t_slot(I, J / 2)), 0, J & 1,
+                        split_half<F>(J <= I ? Tr.a[bidx(I, J)] : z), lane_id());
       }
     lds_sync<true>();
 #pragma unroll
@@ -264,8 +276,10 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
 #pragma unroll
       for (int J = 0; J < 4; ++J)
         if (J / 2 >= I / 2)
-          *(f32x4*)(ws + ws_Tt() + 512 * tt_slot(I, J / 2) + 256 * (J & 1) + 4 * lane_id()) =
-              J >= I ? down4(sA + (16 * J + 4 * g) * LD + 16 * I + c, LD) : z;
+          store_half<F>(
+              (T*)(ws + ws_Tt() + TS * tt_slot(I, J / 2)), 0, J & 1,
+              split_half<F>(J >= I ? down4(sA + (16 * J + 4 * g) * LD + 16 * I + c, LD) : z),
+              lane_id());
   } else {
     const T* dO = (const T*)a.dO + (t0 * a.Hv + h) * DV;
     for (int J = wv - 1; J < DV / 16; J += 3) {
@@ -298,35 +312,47 @@ struct Walk {
   static constexpr int E = 16 / sizeof(T), LD = DK + E;  // rows in LDS, 16 bytes apart
   static constexpr int CPR = DK / E, KI = BC * CPR / 256;
   typedef T Vec __attribute__((ext_vector_type(E)));
-  // a chunk's rows of K (Q) on their way to LDS
+  // (sequence, value head) and first value column of this workgroup.  Workgroups
+  // are dealt to the 8 XCDs in turn; all slices of a head go to one XCD, whose
+  // L2 then reads the head's chunks once.
+  static __device__ __forceinline__ int64_t head_of(int& n0) {
+    const unsigned x = blockIdx.x, r = x >> 3;
+    n0 = (int)(r % NS) * 16;
+    return (int64_t)(r / NS) * 8 + (x & 7);
+  }
+  // A chunk's rows of K (Q) on their way to LDS.  Byte offsets from the chunk's
+  // first row: at most 64 rows of all heads, 32 bits; those of the rows past
+  // the chunk's last are clamped to it by their size.
   struct Rows {
     Vec v[KI];
   };
-  static __device__ __forceinline__ void fetch(Rows& x, const T* __restrict__ p, int64_t ld, int m) {
+  static __device__ __forceinline__ void fetch(Rows& x, const T* p, const uint32_t (&off)[KI],
+                                               uint32_t last) {
+    const uint32_t col = threadIdx.x % CPR * 16;
 #pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int at = threadIdx.x + 256 * i, r = at / CPR;
-      x.v[i] = *(const Vec*)(p + min(r, m - 1) * ld + at % CPR * E);
-    }
+    for (int i = 0; i < KI; ++i)
+      x.v[i] = *(const Vec*)((const char*)p + (min(off[i], last) + col));
   }
   static __device__ __forceinline__ void put(T* s, const Rows& x, int m) {
+    T* to = s + threadIdx.x / CPR * LD + threadIdx.x % CPR * E;
+    if (m == BC) {
 #pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int at = threadIdx.x + 256 * i, r = at / CPR;
-      *(Vec*)(s + r * LD + at % CPR * E) = r < m ? x.v[i] : Vec{};
+      for (int i = 0; i < KI; ++i) *(Vec*)(to + 256 / CPR * i * LD) = x.v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < KI; ++i)
+        *(Vec*)(to + 256 / CPR * i * LD) =
+            (int)threadIdx.x / CPR + 256 / CPR * i < m ? x.v[i] : Vec{};
     }
   }
-  // row block w of T (or T^T): fp32 pair fragments, two at most
+  // row block w of T (or T^T): two pairs of terms at most
   struct TRow {
-    f32x4 v[2][2];
+    Terms<F> v[2];
   };
-  static __device__ __forceinline__ void fetch_t(TRow& x, const float* __restrict__ p, int n, int l) {
+  static __device__ __forceinline__ void fetch_t(TRow& x, const float* p, int n, int l) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (i < n) {
-        x.v[i][0] = at4(p + 512 * i + 4 * l);
-        x.v[i][1] = at4(p + 512 * i + 256 + 4 * l);
-      }
+      if (i < n) x.v[i] = load_terms<F>((const T*)(p + TS * i), 0, l);
   }
   // this wave's share of the product of the 64 rows in LDS with the state
   static __device__ __forceinline__ void share(const T* sK, const Terms<F>& s, float* part, int wv,
@@ -360,11 +386,26 @@ struct Walk {
       st[h] = p && wv < NQ ? col_block(p + n0, DV, 32 * wv + 16 * h, DK) : zero4();
   }
   static __device__ __forceinline__ void state_out(float* p, const f32x4 (&st)[2], int n0, int wv) {
+    const uint32_t at = (32 * wv + 4 * lane_g()) * DV + n0 + lane_c();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        p[(int64_t)(32 * wv + 16 * h + 4 * lane_g() + v) * DV + n0 + lane_c()] = st[h][v];
+      for (int v = 0; v < 4; ++v) p[at + (16 * h + v) * DV] = st[h][v];
+  }
+  // 4 rows from r0 of a [64, DV] array
+  static __device__ __forceinline__ void rows_out(float* p, f32x4 x, int n0, int r0) {
+    const uint32_t at = r0 * DV + n0 + lane_c();
+#pragma unroll
+    for (int v = 0; v < 4; ++v) p[at + v * DV] = x[v];
+  }
+  // this lane's rows 16 wv + 4g + v of a column of V (dO): byte offsets as above
+  static __device__ __forceinline__ RawBlock<T> fetch_col(const T* p, const uint32_t (&off)[4],
+                                                          uint32_t last) {
+    RawBlock<T> x;
+    const uint32_t col = lane_c() * sizeof(T);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x.v[v] = *(const T*)((const char*)p + (min(off[v], last) + col));
+    return x;
   }
 };
 
@@ -376,8 +417,10 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
   __shared__ __attribute__((aligned(16))) T sK[BC * W::LD];
   __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
   __shared__ __attribute__((aligned(16))) T sZ[2 * W::NT * 512], sY[2 * W::NT * 512];
-  const int64_t sh = blockIdx.x / W::NS;
-  const int n0 = (int)(blockIdx.x - sh * W::NS) * 16, s = (int)(sh / a.Hv);
+  int n0;
+  const int64_t sh = W::head_of(n0);
+  if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
+  const int s = (int)(sh / a.Hv);
   const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
   const Seq sq(a, s);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
@@ -385,6 +428,12 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
   const int l = ln.id, g = ln.g(), c = ln.c(), r0 = 16 * wv + 4 * g;
   const bool owner = wv < W::NQ;
   const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
+  uint32_t koff[W::KI], voff[4];  // byte offsets of this thread's rows of K, of V
+#pragma unroll
+  for (int i = 0; i < W::KI; ++i)
+    koff[i] = (threadIdx.x + 256 * i) / W::CPR * (uint32_t)kld * sizeof(T);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) voff[v] = (r0 + v) * (uint32_t)vld * sizeof(T);
   f32x4 st[2];
   W::state_in(st, a.S0 ? a.S0 + sh * DK * DV : nullptr, n0, wv);
   if (nc == 0) return;
@@ -400,33 +449,31 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
   auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
     const float* ws = tile(ck);
     const float* rv = ws + ws_rows();
-    W::fetch_t(x.t, ws + ws_T() + 512 * t_slot(wv, 0), wv / 2 + 1, l);
-    x.v = raw_block((const T*)a.V + ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0, vld, 16 * wv,
-                    rows(ck));
+    W::fetch_t(x.t, ws + ws_T() + TS * t_slot(wv, 0), wv / 2 + 1, l);
+    x.v = W::fetch_col((const T*)a.V + ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0, voff,
+                       (rows(ck) - 1) * (uint32_t)vld * sizeof(T));
     x.beta = at4(rv + r0);
     x.eg = at4(rv + BC + r0);
     x.er = at4(rv + 2 * BC + r0);
     x.el = rv[2 * BC - 1];
   };
   auto keys = [&](typename W::Rows& x, int ck) __attribute__((always_inline)) {
-    W::fetch(x, (const T*)a.K + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, kld, rows(ck));
+    W::fetch(x, (const T*)a.K + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, koff,
+             (rows(ck) - 1) * (uint32_t)kld * sizeof(T));
   };
   const int last = nc - 1;
-  Ops op, nx;
-  typename W::Rows kr;
-  keys(kr, 0);
-  fetch(op, 0);
-  W::put(sK, kr, rows(0));
-  keys(kr, min(1, last));
+  // two sets, asked for two chunks ahead
+  Ops ops[2];
+  typename W::Rows krs[2];
+  keys(krs[0], 0);
+  fetch(ops[0], 0);
+  W::put(sK, krs[0], rows(0));
+  keys(krs[0], min(1, last));
+  fetch(ops[1], min(1, last));
+  keys(krs[1], min(2, last));
   lds_only_barrier();
-  for (int ck = 0; ck < nc; ++ck) {
+  auto step = [&](int ck, Ops& op, typename W::Rows& kr) __attribute__((always_inline)) {
     float* ws = tile(ck);
-    fetch(nx, min(ck + 1, last));
-    __builtin_amdgcn_sched_barrier(0);
-    Terms<F> tt[2];
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-      if (p <= wv / 2) tt[p] = split<F>(op.t.v[p][0], op.t.v[p][1]);
     if (owner) {
       W::state_out(ws + ws_S(DV), st, n0, wv);
       W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
@@ -436,21 +483,23 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
     if (owner) W::cols(kc, sK, wv, ln);
     {
       const f32x4 x = block_of(op.v, 16 * wv, rows(ck)) - op.eg * W::sum(part, wv, l);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) ws[ws_X(DV) + (r0 + v) * DV + n0 + c] = x[v];
+      W::rows_out(ws + ws_X(DV), x, n0, r0);
       store_half<F>(sZ, wv >> 1, wv & 1, split_half<F>(op.beta * x), l);
     }
     lds_only_barrier();
     W::put(sK, kr, rows(min(ck + 1, last)));
-    keys(kr, min(ck + 2, last));
+    keys(kr, min(ck + 3, last));
     __builtin_amdgcn_sched_barrier(0);
     {
-      f32x4 y = zero4();
+      f32x4 y = zero4(), yl = zero4();
 #pragma unroll
       for (int p = 0; p < 2; ++p)
-        if (p <= wv / 2) y = mma_both<false>(tt[p], load_terms<F>(sZ, p, l), y);
+        if (p <= wv / 2) mma_both<false>(op.t.v[p], load_terms<F>(sZ, p, l), y, yl);
+      y += yl;
       store_half<F>(sY, wv >> 1, wv & 1, split_half<F>(op.er * y), l);
     }
+    const float el = op.el;
+    fetch(op, min(ck + 2, last));
     lds_only_barrier();
     if (owner) {
       f32x4 x[2] = {zero4(), zero4()};
@@ -461,9 +510,12 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
         for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(kc.v[hf][p], y, x[hf]);
       }
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * op.el + x[hf];
+      for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * el + x[hf];
     }
-    op = nx;
+  };
+  for (int ck = 0; ck < nc; ck += 2) {
+    step(ck, ops[0], krs[0]);
+    if (ck + 1 < nc) step(ck + 1, ops[1], krs[1]);
   }
 }
 
@@ -476,8 +528,10 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
   __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
   __shared__ __attribute__((aligned(16))) T sY[2 * W::NT * 512], sX[2 * W::NT * 512],
       sO[2 * W::NT * 512];
-  const int64_t sh = blockIdx.x / W::NS;
-  const int n0 = (int)(blockIdx.x - sh * W::NS) * 16, s = (int)(sh / a.Hv);
+  int n0;
+  const int64_t sh = W::head_of(n0);
+  if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
+  const int s = (int)(sh / a.Hv);
   const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
   const Seq sq(a, s);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
@@ -485,52 +539,59 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
   const int l = ln.id, g = ln.g(), c = ln.c(), r0 = 16 * wv + 4 * g;
   const bool owner = wv < W::NQ;
   const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
+  uint32_t koff[W::KI], voff[4];  // byte offsets of this thread's rows of K and Q, of dO
+#pragma unroll
+  for (int i = 0; i < W::KI; ++i)
+    koff[i] = (threadIdx.x + 256 * i) / W::CPR * (uint32_t)kld * sizeof(T);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) voff[v] = (r0 + v) * (uint32_t)vld * sizeof(T);
   f32x4 st[2];
   W::state_in(st, a.dSf ? a.dSf + sh * DK * DV : nullptr, n0, wv);
   auto tile = [&](int ck) { return a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV); };
   auto rows = [&](int ck) { return min(BC, sq.len - ck * BC); };
   auto vat = [&](int ck) { return ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0; };
   struct Ops {
-    RawBlock<float> r;
     RawBlock<T> o;
-    f32x4 beta, eg, er;
+    f32x4 r, beta, eg, er;
     float el;
     typename W::TRow t;
   };
   auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
     const float* ws = tile(ck);
     const float* rv = ws + ws_rows();
-    W::fetch_t(x.t, ws + ws_Tt() + 512 * tt_slot(wv, wv / 2), 2 - wv / 2, l);
-    x.r = raw_block((const float*)ws + ws_R() + n0, DV, 16 * wv, BC);
-    x.o = raw_block((const T*)a.dO + vat(ck), vld, 16 * wv, rows(ck));
+    W::fetch_t(x.t, ws + ws_Tt() + TS * tt_slot(wv, wv / 2), 2 - wv / 2, l);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x.r[v] = ws[ws_R() + (uint32_t)(r0 * DV + n0 + c) + v * DV];
+    x.o = W::fetch_col((const T*)a.dO + vat(ck), voff, (rows(ck) - 1) * (uint32_t)vld * sizeof(T));
     x.beta = at4(rv + r0);
     x.eg = at4(rv + BC + r0);
     x.er = at4(rv + 2 * BC + r0);
     x.el = rv[2 * BC - 1];
   };
   auto keys = [&](typename W::Rows& x, const void* p, int ck) __attribute__((always_inline)) {
-    W::fetch(x, (const T*)p + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, kld, rows(ck));
+    W::fetch(x, (const T*)p + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, koff,
+             (rows(ck) - 1) * (uint32_t)kld * sizeof(T));
   };
   if (nc > 0) {
-    Ops op, nx;
-    typename W::Rows kr, qr;
-    keys(kr, a.K, nc - 1);
-    keys(qr, a.Q, nc - 1);
-    fetch(op, nc - 1);
-    W::put(sK, kr, rows(nc - 1));
-    keys(kr, a.K, max(nc - 2, 0));
+    Ops ops[2];
+    typename W::Rows krs[2], qrs[2];
+    keys(krs[0], a.K, nc - 1);
+    fetch(ops[0], nc - 1);
+    keys(qrs[0], a.Q, nc - 1);
+    W::put(sK, krs[0], rows(nc - 1));
+    keys(krs[0], a.K, max(nc - 2, 0));
+    fetch(ops[1], max(nc - 2, 0));
+    keys(qrs[1], a.Q, max(nc - 2, 0));
+    keys(krs[1], a.K, max(nc - 3, 0));
     lds_only_barrier();
-    for (int ck = nc - 1; ck >= 0; --ck) {
+    auto step = [&](int ck, Ops& op, typename W::Rows& kr, typename W::Rows& qr)
+        __attribute__((always_inline)) {
       float* ws = tile(ck);
-      fetch(nx, max(ck - 1, 0));
       W::put(sQ, qr, rows(ck));
-      keys(qr, a.Q, max(ck - 1, 0));
+      keys(qr, a.Q, max(ck - 2, 0));
       __builtin_amdgcn_sched_barrier(0);
-      Terms<F> tt[2];
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-        if (p < 2 - wv / 2) tt[p] = split<F>(op.t.v[p][0], op.t.v[p][1]);
-      store_half<F>(sO, wv >> 1, wv & 1, split_half<F>(block_of(op.o, 16 * wv, rows(ck)) * op.eg * a.scale), l);
+      store_half<F>(sO, wv >> 1, wv & 1,
+                    split_half<F>(block_of(op.o, 16 * wv, rows(ck)) * op.eg * a.scale), l);
       if (owner) {
         W::state_out(ws + ws_dS(DK, DV), st, n0, wv);
         W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
@@ -538,26 +599,28 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
       lds_only_barrier();
       typename W::Cols kc;
       if (owner) W::cols(kc, sK, wv, ln);
-      store_half<F>(sY, wv >> 1, wv & 1, split_half<F>(block_of(op.r, 0, BC) + op.er * W::sum(part, wv, l)), l);
+      store_half<F>(sY, wv >> 1, wv & 1,
+                    split_half<F>(op.r + op.er * W::sum(part, wv, l)), l);
       lds_only_barrier();
       W::put(sK, kr, rows(max(ck - 1, 0)));
-      keys(kr, a.K, max(ck - 2, 0));
+      keys(kr, a.K, max(ck - 3, 0));
       __builtin_amdgcn_sched_barrier(0);
       f32x4 x[2] = {zero4(), zero4()};
       {
-        f32x4 z = zero4();
+        f32x4 z = zero4(), zl = zero4();
 #pragma unroll
         for (int p = 0; p < 2; ++p)
           if (p < 2 - wv / 2)
-            z = mma_both<false>(tt[p], load_terms<F>(sY, p + wv / 2, l), z);
+            mma_both<false>(op.t.v[p], load_terms<F>(sY, p + wv / 2, l), z, zl);
+        z += zl;
         const f32x4 dx = op.beta * z;
         store_half<F>(sX, wv >> 1, wv & 1, split_half<F>(-op.eg * dx), l);
         const int m = rows(ck);
+        W::rows_out(ws + ws_R(), z, n0, r0);
+        char* dV = (char*)((T*)a.dV + vat(ck));
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          ws[ws_R() + (r0 + v) * DV + n0 + c] = z[v];
-          if (r0 + v < m) ((T*)a.dV)[vat(ck) + (r0 + v) * vld + c] = (T)dx[v];
-        }
+        for (int v = 0; v < 4; ++v)
+          if (r0 + v < m) *(T*)(dV + (voff[v] + (uint32_t)(c * sizeof(T)))) = (T)dx[v];
         if (owner) {
           typename W::Cols qc;
           W::cols(qc, sQ, wv, ln);
@@ -569,6 +632,9 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
           }
         }
       }
+      const float el = op.el;
+      // (chunk 0 again where there is none: its R has become dZ, which no step uses)
+      fetch(op, max(ck - 2, 0));
       lds_only_barrier();
       if (owner) {
 #pragma unroll
@@ -578,9 +644,12 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
           for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(kc.v[hf][p], y, x[hf]);
         }
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * op.el + x[hf];
+        for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * el + x[hf];
       }
-      op = nx;
+    };
+    for (int ck = nc - 1; ck >= 0; ck -= 2) {
+      step(ck, ops[0], krs[0], qrs[0]);
+      if (ck > 0) step(ck - 1, ops[1], krs[1], qrs[1]);
     }
   }
   if (a.dS0 && owner) W::state_out(a.dS0 + sh * DK * DV, st, n0, wv);
@@ -589,6 +658,7 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
 // ---- every chunk: dQ, dK, dbeta, dg; the value heads of a key head in turn
 template <int DK, int DV, typename T>
 __global__ __launch_bounds__(256) void k_bwd_grads(const BwdArgs a) {
+  typedef typename FragOf<T>::type F;
   constexpr int PV = DV + 4, LD = BC + 4, NB = DK / 64;
   // sPE: Z, then dP and E
   __shared__ float sO[BC * PV], sZ[BC * PV], sY[BC * PV], sPE[2 * BC * LD], sr[5][BC];
@@ -645,7 +715,7 @@ __global__ __launch_bounds__(256) void k_bwd_grads(const BwdArgs a) {
         f32x4 y = zero4();
 #pragma unroll
         for (int k = 0; k <= I; ++k)
-          y = mma16(at4(ws + ws_T() + 512 * t_slot(I, k / 2) + 256 * (k & 1) + 4 * lane_id()), z[k], y);
+          y = mma16(half_of(load_terms<F>((const T*)(ws + ws_T() + TS * t_slot(I, k / 2)), 0, lane_id()), k & 1), z[k], y);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sY[(16 * I + 4 * g + v) * PV + 16 * J + c] = y[v];
       }
@@ -782,7 +852,7 @@ int64_t backward_tile_bytes(int dk, int dv) { return ws_tile(dk, dv) * 4; }
 
 template <int DK, int DV, typename T>
 static hipError_t run_backward(const BwdArgs& a, int64_t slots, hipStream_t st) {
-  const unsigned walks = (unsigned)((int64_t)a.nseq * a.Hv * (DV / 16));
+  const unsigned walks = (unsigned)(((int64_t)a.nseq * a.Hv + 7) / 8 * 8 * (DV / 16));
   if (slots > 0) {
     hipLaunchKernelGGL((k_bwd_prep<DK, DV, T>), dim3((unsigned)(slots * a.Hv)), dim3(256), 0, st, a);
     hipLaunchKernelGGL((k_bwd_states<DK, DV, T>), dim3(walks), dim3(256), 0, st, a);

@@ -16,9 +16,15 @@ namespace gdn {
 template <typename F> struct TermsOf { static constexpr int N = 3; };
 template <> struct TermsOf<f32x4> { static constexpr int N = 1; };
 
-// what is left of x after its bf16 part h
-__device__ __forceinline__ f32x4 rest(f32x4 x, bf16x4 h) {
-  return x - __builtin_convertvector(h, f32x4);
+// two values rounded to bf16 in one register (the low half a), and what is left
+// of them.  The compiler rounds the two apart and packs them afterwards, at
+// twice the instructions.
+__device__ __forceinline__ uint32_t take2(float& a, float& b) {
+  uint32_t r;
+  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  a -= __builtin_bit_cast(float, r << 16);
+  b -= __builtin_bit_cast(float, r & 0xffff0000u);
+  return r;
 }
 
 // four values as terms
@@ -29,10 +35,12 @@ __device__ __forceinline__ Half<F> split_half(f32x4 x) {
   if constexpr (TermsOf<F>::N == 1) {
     r.t[0] = x;
   } else {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    float a = x[0], b = x[1], c = x[2], d = x[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      r.t[i] = __builtin_convertvector(x, bf16x4);
-      x = rest(x, r.t[i]);
+      const uint32_t lo = take2(a, b), hi = take2(c, d);
+      r.t[i] = __builtin_bit_cast(bf16x4, u32x2{lo, hi});
     }
   }
   return r;
@@ -80,6 +88,22 @@ __device__ __forceinline__ f32x4 mma_both(const Terms<F>& x, const Terms<F>& y, 
 #pragma unroll
     for (int i = 0; i <= s; ++i) acc = Pair<F>::template mma<OUTQ>(x.t[i], y.t[s - i], acc);
   return acc;
+}
+// the same in two sums, one of the terms below the largest, so that half as many
+// instructions wait for each other
+template <bool OUTQ, typename F>
+__device__ __forceinline__ void mma_both(const Terms<F>& x, const Terms<F>& y, f32x4& acc,
+                                         f32x4& low) {
+  if constexpr (TermsOf<F>::N == 1) {
+    acc = Pair<F>::template mma<OUTQ>(x.t[0], y.t[0], acc);
+  } else {
+    low = Pair<F>::template mma<OUTQ>(x.t[0], y.t[2], low);
+    acc = Pair<F>::template mma<OUTQ>(x.t[1], y.t[1], acc);
+    low = Pair<F>::template mma<OUTQ>(x.t[2], y.t[0], low);
+    acc = Pair<F>::template mma<OUTQ>(x.t[1], y.t[0], acc);
+    low = Pair<F>::template mma<OUTQ>(x.t[0], y.t[1], low);
+    acc = Pair<F>::template mma<OUTQ>(x.t[0], y.t[0], acc);
+  }
 }
 
 // Terms in LDS: a slot is 64 lanes of one pair and term
