@@ -33,6 +33,7 @@
 // are differences of large sums, and their outputs are fp32.
 #include "chunk.hpp"
 #include "engine.hpp"
+#include "forward.hpp"
 #include "launch.hpp"
 #include "layer.hpp"
 #include "split.hpp"
@@ -46,7 +47,10 @@ constexpr int BC = 64;  // tokens a chunk
 // Workspace of one (chunk, value head), in floats.  T and T^T lie as the terms
 // (split.hpp) of the pair fragments of their row blocks, 3 KB a fragment (2 KB
 // with fp32 inputs): T (I, p) with 2p <= I, T^T (I, p) with 2p + 1 >= I.
+// X, R and dZ lie as column-form blocks, S and dS as row-form blocks (tile16.hpp),
+// the 4 values of a lane side by side: 1 KB a block, read and written whole.
 constexpr int TS = 768;
+__host__ __device__ constexpr int blk_at(int I, int J, int NJ) { return (I * NJ + J) * 256; }
 __host__ __device__ constexpr int t_slot(int I, int p) { return (I == 3 ? 4 : I) + p; }
 __host__ __device__ constexpr int tt_slot(int I, int p) { return (I < 2 ? 2 * I : 2 + I) + p - I / 2; }
 __host__ __device__ constexpr int64_t ws_T() { return 0; }
@@ -292,8 +296,7 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
 #pragma unroll
         for (int k = I; k < 4; ++k)
           x = mma16(down4(sP + (16 * k + 4 * g) * LD + 16 * I + c, LD), o[k], x);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) ws[ws_R() + (16 * I + 4 * g + v) * DV + 16 * J + c] = x[v];
+        *(f32x4*)(ws + ws_R() + blk_at(I, J, DV / 16) + 4 * lane_id()) = x;
       }
     }
   }
@@ -392,11 +395,19 @@ struct Walk {
 #pragma unroll
       for (int v = 0; v < 4; ++v) p[at + (16 * h + v) * DV] = st[h][v];
   }
-  // 4 rows from r0 of a [64, DV] array
-  static __device__ __forceinline__ void rows_out(float* p, f32x4 x, int n0, int r0) {
-    const uint32_t at = r0 * DV + n0 + lane_c();
+  // the same as row-form blocks, transposed through this wave's part of LDS
+  static constexpr int TB = 16 * 20;
+  static __device__ __forceinline__ void blocks_out(float* p, const f32x4 (&st)[2], int n0, int wv,
+                                                    float* t, Lane ln) {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) p[at + v * DV] = x[v];
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) t[TB * h + (4 * ln.g() + v) * 20 + ln.c()] = st[h][v];
+    lds_sync<true>();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *(f32x4*)(p + blk_at(2 * wv + h, n0 / 16, NS) + 4 * ln.id) =
+          at4(t + TB * h + ln.c() * 20 + 4 * ln.g());
   }
   // this lane's rows 16 wv + 4g + v of a column of V (dO): byte offsets as above
   static __device__ __forceinline__ RawBlock<T> fetch_col(const T* p, const uint32_t (&off)[4],
@@ -417,6 +428,7 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
   __shared__ __attribute__((aligned(16))) T sK[BC * W::LD];
   __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
   __shared__ __attribute__((aligned(16))) T sZ[2 * W::NT * 512], sY[2 * W::NT * 512];
+  __shared__ __attribute__((aligned(16))) float sT[W::NQ][2 * W::TB];
   int n0;
   const int64_t sh = W::head_of(n0);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
@@ -475,7 +487,7 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
   auto step = [&](int ck, Ops& op, typename W::Rows& kr) __attribute__((always_inline)) {
     float* ws = tile(ck);
     if (owner) {
-      W::state_out(ws + ws_S(DV), st, n0, wv);
+      W::blocks_out(ws + ws_S(DV), st, n0, wv, sT[wv], ln);
       W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
     }
     lds_only_barrier();
@@ -483,7 +495,7 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
     if (owner) W::cols(kc, sK, wv, ln);
     {
       const f32x4 x = block_of(op.v, 16 * wv, rows(ck)) - op.eg * W::sum(part, wv, l);
-      W::rows_out(ws + ws_X(DV), x, n0, r0);
+      *(f32x4*)(ws + ws_X(DV) + blk_at(wv, n0 / 16, W::NS) + 4 * l) = x;
       store_half<F>(sZ, wv >> 1, wv & 1, split_half<F>(op.beta * x), l);
     }
     lds_only_barrier();
@@ -528,6 +540,7 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
   __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
   __shared__ __attribute__((aligned(16))) T sY[2 * W::NT * 512], sX[2 * W::NT * 512],
       sO[2 * W::NT * 512];
+  __shared__ __attribute__((aligned(16))) float sT[W::NQ][2 * W::TB];
   int n0;
   const int64_t sh = W::head_of(n0);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
@@ -560,8 +573,7 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
     const float* ws = tile(ck);
     const float* rv = ws + ws_rows();
     W::fetch_t(x.t, ws + ws_Tt() + TS * tt_slot(wv, wv / 2), 2 - wv / 2, l);
-#pragma unroll
-    for (int v = 0; v < 4; ++v) x.r[v] = ws[ws_R() + (uint32_t)(r0 * DV + n0 + c) + v * DV];
+    x.r = at4(ws + ws_R() + blk_at(wv, n0 / 16, W::NS) + 4 * l);
     x.o = W::fetch_col((const T*)a.dO + vat(ck), voff, (rows(ck) - 1) * (uint32_t)vld * sizeof(T));
     x.beta = at4(rv + r0);
     x.eg = at4(rv + BC + r0);
@@ -593,7 +605,7 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
       store_half<F>(sO, wv >> 1, wv & 1,
                     split_half<F>(block_of(op.o, 16 * wv, rows(ck)) * op.eg * a.scale), l);
       if (owner) {
-        W::state_out(ws + ws_dS(DK, DV), st, n0, wv);
+        W::blocks_out(ws + ws_dS(DK, DV), st, n0, wv, sT[wv], ln);
         W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
       }
       lds_only_barrier();
@@ -616,7 +628,7 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
         const f32x4 dx = op.beta * z;
         store_half<F>(sX, wv >> 1, wv & 1, split_half<F>(-op.eg * dx), l);
         const int m = rows(ck);
-        W::rows_out(ws + ws_R(), z, n0, r0);
+        *(f32x4*)(ws + ws_R() + blk_at(wv, n0 / 16, W::NS) + 4 * l) = z;
         char* dV = (char*)((T*)a.dV + vat(ck));
 #pragma unroll
         for (int v = 0; v < 4; ++v)
@@ -656,173 +668,383 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
 }
 
 // ---- every chunk: dQ, dK, dbeta, dg; the value heads of a key head in turn
+// Eight waves.  Wave w has the 32 feature columns 32 (w % (DK / 32)) of dQ and dK
+// for NR row blocks of the chunk.  dO, dZ and Y lie in LDS as pair fragments along
+// the value columns (one form serves as left operand and, transposed, as right
+// one); S and dS come from memory as right operands, each value split into
+// terms by the waves that use it.  The blocks of dP and E wait in registers until the
+// products with the states are done, and then take the place of dO and dZ.
 template <int DK, int DV, typename T>
-__global__ __launch_bounds__(256) void k_bwd_grads(const BwdArgs a) {
+struct Grads {
   typedef typename FragOf<T>::type F;
-  constexpr int PV = DV + 4, LD = BC + 4, NB = DK / 64;
-  // sPE: Z, then dP and E
-  __shared__ float sO[BC * PV], sZ[BC * PV], sY[BC * PV], sPE[2 * BC * LD], sr[5][BC];
-  __shared__ float sdb[BC], red[2][4][BC], sdg[BC], send[4];
-  static_assert(2 * LD >= PV, "");
-  float *sP = sPE, *sE = sPE + BC * LD;
+  static constexpr int NT = TermsOf<F>::N, NP = DV / 32;  // NP: pairs along the value columns
+  static constexpr int NC = DK / 32, RG = 8 / NC, NR = 4 / RG;
+  static constexpr int LDK = DK + 16 / sizeof(T);
+  // LDS, in values of T: T, dO, dZ and Y; later dP and E along their rows and down
+  // them, and the rows of K and Q
+  static constexpr int oT = 0, oO = oT + 6 * NT * 512, oZ = oO + 4 * NP * 512;
+  static constexpr int oY = oZ + 4 * NP * NT * 512, oEnd = oY + 4 * NP * NT * 512;
+  static constexpr int oPr = 0, oPc = 6 * NT * 512, oEr = 2 * oPc, oEc = 3 * oPc, oK = 4 * oPc;
+  static constexpr int oQ = oK + BC * LDK, oEnd2 = oQ + BC * LDK;
+  static constexpr int SIZE = oEnd2 > oEnd ? oEnd2 : oEnd;
+};
+
+// sum over the 16 lanes of a row of the wave
+__device__ __forceinline__ float sum16(float x) {
+  auto add = [&](int y) { x += __builtin_bit_cast(float, y); };
+  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));   // lane ^ 1
+  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true));   // lane ^ 2
+  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x141, 0xf, 0xf, true));  // 7 - lane
+  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x140, 0xf, 0xf, true));  // 15 - lane
+  return x;
+}
+
+template <int DK, int DV, typename T>
+__global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
+  typedef Grads<DK, DV, T> G;
+  typedef typename G::F F;
+  constexpr int NT = G::NT, NP = G::NP, NR = G::NR, LDK = G::LDK;
+  constexpr int E = 16 / sizeof(T), NJ = DV / 16, RY = 8 / NJ;
+  typedef T Vec __attribute__((ext_vector_type(E)));
+  __shared__ __attribute__((aligned(16))) T sm[G::SIZE];
+  __shared__ __attribute__((aligned(16))) float sr[5][BC];
+  __shared__ __attribute__((aligned(16))) float tr[8][16 * 20];
+  __shared__ float sdb[NJ][BC], red[2][G::NC][BC], sdg[BC], send[8];
   const int64_t slot = blockIdx.x / a.Hk;
   const int hk = (int)(blockIdx.x - slot * a.Hk), gr = a.Hv / a.Hk;
   int64_t t0 = 0;
   const int m = chunk_at(a, slot, t0);
   if (m == 0) return;
-  const int wv = threadIdx.x >> 6, g = lane_g(), c = lane_c();
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = 32 * (wv % G::NC), I0 = wv / G::NC * NR;  // this wave's columns and row blocks
   const int64_t kld = (int64_t)a.Hk * DK, kat = (t0 * a.Hk + hk) * DK;
-  // this wave's NB column blocks of K and Q
-  f32x4 kf[NB][4], qf[NB][4], sumq[NB][4], sumk[NB][4];
+  const int64_t vld = (int64_t)a.Hv * DV;
+
+  for (int h = hk * gr; h < (hk + 1) * gr; ++h) {
+    // A value of its own in every turn: the LDS and memory offsets made from it
+    // are formed where they are used.  Formed before the loop, some hundred of
+    // them went to scratch, and their reloads were most of the kernel's time.
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const Lane ln{tid & 63};
+    const int l = ln.id, g = ln.g(), c = ln.c();
+    float* ws = a.ws + (slot * a.Hv + h) * ws_tile(DK, DV);
+    const float* S = ws + ws_S(DV) + blk_at(col / 16, 0, NJ) + 4 * l;
+    const float* dS = ws + ws_dS(DK, DV) + blk_at(col / 16, 0, NJ) + 4 * l;
+    // S and dS of a pair of value column blocks
+    struct States {
+      f32x4 s[2][2], d[2][2];
+    };
+    auto states = [&](States& x, int p) __attribute__((always_inline)) {
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          x.s[b][hf] = at4(S + blk_at(b, 2 * p + hf, NJ));
+          x.d[b][hf] = at4(dS + blk_at(b, 2 * p + hf, NJ));
+        }
+    };
+    // ---- T, dO and dZ into fragments, Z, and dZ . X
+    const int J = wv % NJ;
+    Terms<F> z[2];
+    {
+      f32x4 xb[4], zb[4];
+#pragma unroll
+      for (int I = 0; I < 4; ++I) {
+        xb[I] = at4(ws + ws_X(DV) + blk_at(I, J, NJ) + 4 * l);
+        zb[I] = at4(ws + ws_R() + blk_at(I, J, NJ) + 4 * l);
+      }
+      constexpr int PR = DV / 4;  // 4-value pieces a row, one of a fragment's lane each
+      const T* dO = (const T*)a.dO + (t0 * a.Hv + h) * DV;
+      F o[BC * PR / 512];
+#pragma unroll
+      for (int i = 0; i < BC * PR / 512; ++i) {
+        const int at = tid + 512 * i, r = at / PR;
+        o[i] = *(const F*)(dO + min(r, m - 1) * vld + at % PR * 4);
+      }
+      constexpr int TN = 6 * NT * 512 / E;  // 16-byte pieces of T
+      Vec tv[(TN + 511) / 512];
+#pragma unroll
+      for (int i = 0; i < (TN + 511) / 512; ++i) {
+        const int at = min(tid + 512 * i, TN - 1), sl = at / (NT * 512 / E);
+        tv[i] = *(const Vec*)((const T*)(ws + ws_T() + TS * sl) + (at - sl * (NT * 512 / E)) * E);
+      }
+      if (tid < 5 * BC) (&sr[0][0])[tid] = ws[ws_rows() + tid];
+      f32x4 bt[4];
+#pragma unroll
+      for (int I = 0; I < 4; ++I) bt[I] = at4(ws + ws_rows() + 16 * I + 4 * g);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) z[p] = split<F>(bt[2 * p] * xb[2 * p], bt[2 * p + 1] * xb[2 * p + 1]);
+      float* t = tr[wv];
+#pragma unroll
+      for (int I = 0; I < 4; ++I) {
+        if (I % RY != wv / NJ) continue;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          t[(4 * g + v) * 20 + c] = zb[I][v];
+          const float d = sum16(xb[I][v] * zb[I][v]);
+          if (c == 0) sdb[J][16 * I + 4 * g + v] = d;
+        }
+        lds_sync<true>();
+        store_half<F>(sm + G::oZ, I * NP + (J >> 1), J & 1, split_half<F>(at4(t + c * 20 + 4 * g)), l);
+        lds_sync<true>();
+      }
+#pragma unroll
+      for (int i = 0; i < BC * PR / 512; ++i) {
+        const int at = tid + 512 * i, r = at / PR, e = at % PR;
+        const int to = 16 * (e & 3) + (r & 15), hf = (e >> 2) & 1;
+        T* po = sm + G::oO + ((r >> 4) * NP + (e >> 3)) * 512;
+        *(F*)(sizeof(T) == 4 ? po + 256 * hf + 4 * to : po + 8 * to + 4 * hf) = r < m ? o[i] : F{};
+      }
+#pragma unroll
+      for (int i = 0; i < (TN + 511) / 512; ++i)
+        if (tid + 512 * i < TN) *(Vec*)(sm + G::oT + (tid + 512 * i) * E) = tv[i];
+    }
+    __syncthreads();
+    // ---- Y = T Z: value column block J of the rows I % RY
 #pragma unroll
     for (int I = 0; I < 4; ++I) {
-      const int64_t at = kat + 16 * (NB * wv + b);
-      kf[b][I] = col_block((const T*)a.K + at, kld, 16 * I, m);
-      qf[b][I] = col_block((const T*)a.Q + at, kld, 16 * I, m);
-      sumq[b][I] = sumk[b][I] = zero4();
-    }
-  for (int h = hk * gr; h < (hk + 1) * gr; ++h) {
-    const float* ws = a.ws + (slot * a.Hv + h) * ws_tile(DK, DV);
-    const float* S = ws + ws_S(DV);
-    const float* dS = ws + ws_dS(DK, DV);
-    for (int i = threadIdx.x; i < 5 * BC; i += 256) (&sr[0][0])[i] = ws[ws_rows() + i];
-    rows_to_lds<DV, PV>(sO, (const T*)a.dO + (t0 * a.Hv + h) * DV, (int64_t)a.Hv * DV, m);
-    __syncthreads();
-    {  // 4 threads a row: Z, dZ, and dZ . X
-      const int r = threadIdx.x >> 2;
-      const float b = sr[0][r];
-      float dot = 0.f;
-      for (int e = 4 * (threadIdx.x & 3); e < DV; e += 16) {
-        const f32x4 x = at4(ws + ws_X(DV) + r * DV + e), z = at4(ws + ws_R() + r * DV + e);
+      if (I % RY != wv / NJ) continue;
+      f32x4 y = zero4(), yl = zero4();
 #pragma unroll
-        for (int v = 0; v < 4; ++v) dot = __builtin_fmaf(x[v], z[v], dot);
-        *(f32x4*)(sPE + r * PV + e) = b * x;
-        *(f32x4*)(sZ + r * PV + e) = z;
+      for (int p = 0; p <= I / 2; ++p)
+        mma_both<true>(load_terms<F>(sm + G::oT, t_slot(I, p), l), z[p], y, yl);
+      store_half<F>(sm + G::oY, I * NP + (J >> 1), J & 1, split_half<F>(y + yl), l);
+    }
+    States st;
+    states(st, 0);
+    __syncthreads();
+    // ---- dP and E, a lower block each; an E block costs as much as two of dP
+    struct Blk {
+      int kind, I, J;  // kind: 0 dP, 1 E, -1 none
+    };
+    auto block = [&](int i) __attribute__((always_inline)) {
+      // waves 0, 1: two of E; the others one of E and two (6, 7: one) of dP
+      int kind, n;
+      if (wv < 2) {
+        kind = i < 2 ? 1 : -1;
+        n = 2 * wv + i;
+      } else if (i == 0) {
+        kind = 1;
+        n = wv + 2;
+      } else {
+        kind = wv < 6 || i == 1 ? 0 : -1;
+        n = wv < 6 ? 2 * (wv - 2) + i - 1 : wv + 2;
       }
-      dot += __shfl_xor(dot, 1);
-      dot += __shfl_xor(dot, 2);
-      if ((threadIdx.x & 3) == 0) sdb[r] = dot;
-    }
-    __syncthreads();
-    for (int J = wv; J < DV / 16; J += 4) {  // Y
-      f32x4 z[4];
+      const int I = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
+      return Blk{kind, I, n - I * (I + 1) / 2};
+    };
+    f32x4 pe[3];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) z[k] = down4(sPE + (16 * k + 4 * g) * PV + 16 * J + c, PV);
-#pragma unroll
-      for (int I = 0; I < 4; ++I) {
-        f32x4 y = zero4();
-#pragma unroll
-        for (int k = 0; k <= I; ++k)
-          y = mma16(half_of(load_terms<F>((const T*)(ws + ws_T() + TS * t_slot(I, k / 2)), 0, lane_id()), k & 1), z[k], y);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sY[(16 * I + 4 * g + v) * PV + 16 * J + c] = y[v];
+    for (int i = 0; i < 3; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      const Blk k = block(i);
+      f32x4 x = zero4(), xl = zero4();
+      if (k.kind == 1) {
+#pragma unroll 1
+        for (int p = 0; p < NP; ++p)
+          mma_both<false>(load_terms<F>(sm + G::oZ, k.I * NP + p, l),
+                          load_terms<F>(sm + G::oY, k.J * NP + p, l), x, xl);
+      } else if (k.kind == 0) {
+#pragma unroll 1
+        for (int p = 0; p < NP; ++p)
+          x = mma_in<false>(slot_load<F>(sm + G::oO + (k.I * NP + p) * 512, l),
+                            load_terms<F>(sm + G::oY, k.J * NP + p, l), x);
       }
-    }
-    __syncthreads();
-    for (int b = wv; b < 20; b += 4) {  // dP and E, lower blocks
-      const int bb = b >> 1, I = bb < 1 ? 0 : bb < 3 ? 1 : bb < 6 ? 2 : 3, J = bb - I * (I + 1) / 2;
-      const float* left = b & 1 ? sZ : sO;
-      f32x4 x = zero4();
-#pragma unroll
-      for (int k = 0; k < DV / 16; ++k)
-        x = mma16(at4(left + (16 * I + c) * PV + 16 * k + 4 * g),
-                  at4(sY + (16 * J + c) * PV + 16 * k + 4 * g), x);
+      x += xl;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int i = 16 * I + 4 * g + v, j = 16 * J + c;
-        const float d = i >= j ? expf((sr[3][i] - sr[3][j]) + (sr[4][i] - sr[4][j])) : 0.f;
-        if (b & 1)
-          sE[i * LD + j] = i > j ? -x[v] * d : 0.f;
+        const int r = 16 * k.I + 4 * g + v, j = 16 * k.J + c;
+        const float d = r >= j ? expf((sr[3][r] - sr[3][j]) + (sr[4][r] - sr[4][j])) : 0.f;
+        pe[i][v] = k.kind == 1 ? (r > j ? -x[v] * d : 0.f) : a.scale * x[v] * d;
+      }
+    }
+    // ---- dO S^T, dZ S^T, Y dS^T and <S, dS>
+    constexpr int CPR = DK / E, KN = BC * CPR / 512;
+    Vec kv[KN], qv[KN];
+#pragma unroll
+    for (int i = 0; i < KN; ++i) {
+      const int at = tid + 512 * i, r = at / CPR;
+      const int64_t from = kat + min(r, m - 1) * kld + at % CPR * E;
+      kv[i] = *(const Vec*)((const T*)a.K + from);
+      qv[i] = *(const Vec*)((const T*)a.Q + from);
+    }
+    f32x4 dq[2][NR], zs[2][NR], yd[2][NR];
+    float ss = 0.f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < NR; ++i) dq[b][i] = zs[b][i] = yd[b][i] = zero4();
+#pragma unroll 1
+    for (int p = 0; p < NP; ++p) {
+      Terms<F> sv[2], dv[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) ss = __builtin_fmaf(st.s[b][hf][v], st.d[b][hf][v], ss);
+        sv[b] = split<F>(st.s[b][0], st.s[b][1]);
+        dv[b] = split<F>(st.d[b][0], st.d[b][1]);
+      }
+      states(st, p + 1 < NP ? p + 1 : p);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const int at = (I0 + i) * NP + p;
+        const Pair<F> o = slot_load<F>(sm + G::oO + at * 512, l);
+        const Terms<F> z = load_terms<F>(sm + G::oZ, at, l), y = load_terms<F>(sm + G::oY, at, l);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          dq[b][i] = mma_in<false>(o, sv[b], dq[b][i]);
+          zs[b][i] = mma_both<false>(z, sv[b], zs[b][i]);
+          yd[b][i] = mma_both<false>(y, dv[b], yd[b][i]);
+        }
+      }
+    }
+    __syncthreads();
+    // ---- K and Q, and dP and E as left operands: along their rows, and down them (E
+    // with beta)
+#pragma unroll
+    for (int i = 0; i < KN; ++i) {
+      const int at = tid + 512 * i, r = at / CPR, e = at % CPR * E;
+      *(Vec*)(sm + G::oK + r * LDK + e) = r < m ? kv[i] : Vec{};
+      *(Vec*)(sm + G::oQ + r * LDK + e) = r < m ? qv[i] : Vec{};
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const Blk k = block(i);
+      if (k.kind < 0) continue;
+      T* rows = sm + (k.kind ? G::oEr : G::oPr);
+      T* cols = sm + (k.kind ? G::oEc : G::oPc);
+      const f32x4 x = pe[i];
+      float* t = tr[wv];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) t[(4 * g + v) * 20 + c] = x[v];
+      lds_sync<true>();
+      store_half<F>(rows, t_slot(k.I, k.J >> 1), k.J & 1, split_half<F>(at4(t + c * 20 + 4 * g)), l);
+      lds_sync<true>();
+      store_half<F>(cols, tt_slot(k.J, k.I >> 1), k.I & 1,
+                    split_half<F>(k.kind ? at4(&sr[0][16 * k.I + 4 * g]) * x : x), l);
+      if (k.I == k.J) {  // the block beside the diagonal that its pair takes along: zeros
+        if (k.I % 2 == 0)
+          store_half<F>(rows, t_slot(k.I, k.I >> 1), 1, split_half<F>(zero4()), l);
         else
-          sP[i * LD + j] = i >= j ? a.scale * x[v] * d : 0.f;
+          store_half<F>(cols, tt_slot(k.I, k.I >> 1), 0, split_half<F>(zero4()), l);
       }
     }
     __syncthreads();
-    f32x4 dotF[4], dotG[4];
-    float end = 0.f, ss = 0.f;
+    // ---- the rest of dQ and dK, and the sums along their rows
+    // right operands K and Q: pairs of token blocks, this wave's two column blocks
+    Pair<F> kf[2][2], qf[2][2];
 #pragma unroll
-    for (int I = 0; I < 4; ++I) dotF[I] = dotG[I] = zero4();
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int col = 16 * (NB * wv + b);
-      f32x4 dq[4], zs[4], yd[4];
+      for (int p = 0; p < 2; ++p) {
+        kf[b][p] = col_pair<LDK>(sm + G::oK, 32 * p, col + 16 * b, ln);
+        qf[b][p] = col_pair<LDK>(sm + G::oQ, 32 * p, col + 16 * b, ln);
+      }
+    // The sums over the value heads of a key head, in the place of the first one's
+    // states (which nothing reads any more); the last one writes the results.
+    float* acc = a.ws + (slot * a.Hv + hk * gr) * ws_tile(DK, DV) + ws_S(DV) + 4 * tid;
+    float end = 0.f;
 #pragma unroll
-      for (int I = 0; I < 4; ++I) dq[I] = zs[I] = yd[I] = zero4();
-#pragma unroll 2
-      for (int k = 0; k < DV / 16; ++k) {  // dO S^T, dZ S^T, Y dS^T
-        const f32x4 sv = at4(S + (int64_t)(col + c) * DV + 16 * k + 4 * g);
-        const f32x4 dv = at4(dS + (int64_t)(col + c) * DV + 16 * k + 4 * g);
+    for (int i = 0; i < NR; ++i) {
+      const int I = I0 + i, r0 = 16 * I + 4 * g;
+      const f32x4 bt = at4(&sr[0][r0]), eg = at4(&sr[1][r0]), er = at4(&sr[2][r0]);
+      f32x4 F_[2], km[2], R[2];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) ss = __builtin_fmaf(sv[v], dv[v], ss);
-#pragma unroll
-        for (int I = 0; I < 4; ++I) {
-          const int at = (16 * I + c) * PV + 16 * k + 4 * g;
-          dq[I] = mma16(at4(sO + at), sv, dq[I]);
-          zs[I] = mma16(at4(sZ + at), sv, zs[I]);
-          yd[I] = mma16(at4(sY + at), dv, yd[I]);
-        }
+      for (int b = 0; b < 2; ++b) {
+        dq[b][i] = dq[b][i] * eg * a.scale;
+        F_[b] = zero4();
+        R[b] = km[b] = er * yd[b][i];
       }
 #pragma unroll
-      for (int I = 0; I < 4; ++I) {
-        const int r0 = 16 * I + 4 * g;
-        const f32x4 bt = at4(&sr[0][r0]), eg = at4(&sr[1][r0]);
-        dq[I] = dq[I] * eg * a.scale;
-        f32x4 F = zero4(), R = at4(&sr[2][r0]) * yd[I], km;
+      for (int p = 0; p < 2; ++p) {
+        if (p <= I / 2) {
+          const Terms<F> P = load_terms<F>(sm + G::oPr, t_slot(I, p), l);
+          const Terms<F> Er = load_terms<F>(sm + G::oEr, t_slot(I, p), l);
 #pragma unroll
-        for (int k = 0; k <= I; ++k) {
-          const int at = (16 * I + c) * LD + 16 * k + 4 * g;
-          dq[I] = mma16(at4(sP + at), kf[b][k], dq[I]);
-          F = mma16(at4(sE + at), kf[b][k], F);
+          for (int b = 0; b < 2; ++b) {
+            dq[b][i] = mma_in<false>(P, kf[b][p], dq[b][i]);
+            F_[b] = mma_in<false>(Er, kf[b][p], F_[b]);
+          }
         }
-        km = R;
+        if (p >= I / 2) {
+          const Terms<F> P = load_terms<F>(sm + G::oPc, tt_slot(I, p), l);
+          const Terms<F> Ec = load_terms<F>(sm + G::oEc, tt_slot(I, p), l);
 #pragma unroll
-        for (int k = I; k < 4; ++k) {
-          const int at = (16 * k + 4 * g) * LD + 16 * I + c;
-          km = mma16(down4(sP + at, LD), qf[b][k], km);
-          km = mma16(down4(sE + at, LD), at4(&sr[0][16 * k + 4 * g]) * kf[b][k], km);
+          for (int b = 0; b < 2; ++b) {
+            km[b] = mma_in<false>(P, qf[b][p], km[b]);
+            km[b] = mma_in<false>(Ec, kf[b][p], km[b]);
+          }
         }
-        const f32x4 kp = bt * (F - eg * zs[I]);
-        dotF[I] += kf[b][I] * F;
-        dotG[I] += qf[b][I] * dq[I] + kf[b][I] * (kp - km);
-        sumq[b][I] += dq[I];
-        sumk[b][I] += kp + km;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) end = __builtin_fmaf(kf[b][I][v], R[v], end);
       }
-    }
-    end = __builtin_fmaf(sr[1][BC - 1], ss, end);
+      f32x4 dotF = zero4(), dotG = zero4();
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) end += __shfl_xor(end, o);
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 kp = bt * (F_[b] - eg * zs[b][i]);
+        // the rows' own k and q, from the pair that holds their block
+        const Pair<F> kk = I < 2 ? kf[b][0] : kf[b][1], qq = I < 2 ? qf[b][0] : qf[b][1];
+        const f32x4 k = I & 1 ? kk.hi() : kk.lo(), q = I & 1 ? qq.hi() : qq.lo();
+        dotF += k * F_[b];
+        dotG += q * dq[b][i] + k * (kp - km[b]);
 #pragma unroll
-    for (int I = 0; I < 4; ++I)
+        for (int v = 0; v < 4; ++v) end = __builtin_fmaf(k[v], R[b][v], end);
+        f32x4 sq = dq[b][i], sk = kp + km[b];
+        float* at = acc + (b * NR + i) * 2 * 2048;
+        if (h > hk * gr) {
+          sq += at4(at);
+          sk += at4(at + 2048);
+        }
+        if (h + 1 < (hk + 1) * gr) {
+          *(f32x4*)at = sq;
+          *(f32x4*)(at + 2048) = sk;
+        } else {
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (r0 + v < m) {
+              const int64_t to = kat + (r0 + v) * kld + col + 16 * b + c;
+              ((T*)a.dQ)[to] = (T)sq[v];
+              ((T*)a.dK)[to] = (T)sk[v];
+            }
+        }
+      }
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) {
-          dotF[I][v] += __shfl_xor(dotF[I][v], o);
-          dotG[I][v] += __shfl_xor(dotG[I][v], o);
-        }
+        const float f = sum16(dotF[v]), d = sum16(dotG[v]);
         if (c == 0) {
-          red[0][wv][16 * I + 4 * g + v] = dotF[I][v];
-          red[1][wv][16 * I + 4 * g + v] = dotG[I][v];
+          red[0][wv % G::NC][r0 + v] = f;
+          red[1][wv % G::NC][r0 + v] = d;
         }
       }
-    if (lane_id() == 0) send[wv] = end;
+    }
+    // (every row group has formed the same <S, dS> of its columns)
+    if (I0 == 0) end = __builtin_fmaf(sr[1][BC - 1], ss, end);
+    end = sum16(end);
+    end += __shfl_xor(end, 16);
+    end += __shfl_xor(end, 32);
+    if (l == 0) send[wv] = end;
     __syncthreads();
-    if (threadIdx.x < BC) {
-      const int r = threadIdx.x;
-      float dg = (red[1][0][r] + red[1][1][r]) + (red[1][2][r] + red[1][3][r]);
-      if (r == m - 1) dg += (send[0] + send[1]) + (send[2] + send[3]);
+    if (tid < BC) {
+      const int r = tid;
+      float db = 0.f, dg = 0.f;
+#pragma unroll
+      for (int i = 0; i < NJ; ++i) db += sdb[i][r];
+#pragma unroll
+      for (int i = 0; i < G::NC; ++i) {
+        db += red[0][i][r];
+        dg += red[1][i][r];
+      }
+      if (r == m - 1)
+        dg += ((send[0] + send[1]) + (send[2] + send[3])) +
+              ((send[4] + send[5]) + (send[6] + send[7]));
       sdg[r] = dg;
-      if (r < m)
-        a.dbeta[(t0 + r) * a.Hv + h] =
-            sdb[r] + ((red[0][0][r] + red[0][1][r]) + (red[0][2][r] + red[0][3][r]));
+      if (r < m) a.dbeta[(t0 + r) * a.Hv + h] = db;
     }
     __syncthreads();
-    if (threadIdx.x < m) {
-      const int r = threadIdx.x;
+    if (tid < m) {
+      const int r = tid;
       float dg = sdg[r];
       // the last g of a part of C tokens is in the gamma of every later row
       if (a.C < BC && r % a.C == a.C - 1)
@@ -830,19 +1052,6 @@ __global__ __launch_bounds__(256) void k_bwd_grads(const BwdArgs a) {
       a.dg[(t0 + r) * a.Hv + h] = dg;
     }
   }
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int I = 0; I < 4; ++I)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int r = 16 * I + 4 * g + v;
-        if (r < m) {
-          const int64_t at = kat + r * kld + 16 * (NB * wv + b) + c;
-          ((T*)a.dQ)[at] = (T)sumq[b][I][v];
-          ((T*)a.dK)[at] = (T)sumk[b][I][v];
-        }
-      }
 }
 
 int64_t backward_slots(int nseq, int L, bool packed) {
@@ -860,7 +1069,7 @@ static hipError_t run_backward(const BwdArgs& a, int64_t slots, hipStream_t st) 
   if (slots > 0 || a.dS0)
     hipLaunchKernelGGL((k_bwd_reverse<DK, DV, T>), dim3(walks), dim3(256), 0, st, a);
   if (slots > 0)
-    hipLaunchKernelGGL((k_bwd_grads<DK, DV, T>), dim3((unsigned)(slots * a.Hk)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_bwd_grads<DK, DV, T>), dim3((unsigned)(slots * a.Hk)), dim3(512), 0, st, a);
   return hipGetLastError();
 }
 
