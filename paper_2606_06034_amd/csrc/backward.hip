@@ -31,162 +31,9 @@
 //
 // Everything is formed in fp32, bf16 inputs too: the gradients of beta and g
 // are differences of large sums, and their outputs are fp32.
-#include "chunk.hpp"
-#include "engine.hpp"
-#include "forward.hpp"
-#include "launch.hpp"
-#include "layer.hpp"
-#include "split.hpp"
+#include "backward.hpp"
 
 namespace gdn {
-
-namespace {
-
-constexpr int BC = 64;  // tokens a chunk
-
-// Workspace of one (chunk, value head), in floats.  T and T^T lie as the terms
-// (split.hpp) of the pair fragments of their row blocks, 3 KB a fragment (2 KB
-// with fp32 inputs): T (I, p) with 2p <= I, T^T (I, p) with 2p + 1 >= I.
-// X, R and dZ lie as column-form blocks, S and dS as row-form blocks (tile16.hpp),
-// the 4 values of a lane side by side: 1 KB a block, read and written whole.
-constexpr int TS = 768;
-__host__ __device__ constexpr int blk_at(int I, int J, int NJ) { return (I * NJ + J) * 256; }
-__host__ __device__ constexpr int t_slot(int I, int p) { return (I == 3 ? 4 : I) + p; }
-__host__ __device__ constexpr int tt_slot(int I, int p) { return (I < 2 ? 2 * I : 2 + I) + p - I / 2; }
-__host__ __device__ constexpr int64_t ws_T() { return 0; }
-__host__ __device__ constexpr int64_t ws_Tt() { return 6 * TS; }
-__host__ __device__ constexpr int64_t ws_rows() { return 12 * TS; }  // beta e^g e^{gl-g} g off
-__host__ __device__ constexpr int64_t ws_R() { return ws_rows() + 5 * BC; }  // P^T dO, then dZ
-__host__ __device__ constexpr int64_t ws_X(int dv) { return ws_R() + BC * dv; }
-__host__ __device__ constexpr int64_t ws_S(int dv) { return ws_X(dv) + BC * dv; }
-__host__ __device__ constexpr int64_t ws_dS(int dk, int dv) { return ws_S(dv) + dk * dv; }
-__host__ __device__ constexpr int64_t ws_tile(int dk, int dv) { return ws_dS(dk, dv) + dk * dv; }
-
-struct BwdArgs {
-  const void *Q, *K, *V, *dO;
-  const float *beta, *g, *S0, *dSf;
-  void *dQ, *dK, *dV;
-  float *dbeta, *dg, *dS0, *ws;
-  const int* cu;
-  int nseq, L;  // L: tokens a sequence, or all tokens where cu is given
-  int nc;       // chunks a sequence (cu not given)
-  int Hk, Hv, C;
-  float scale;
-};
-
-// The chunks of sequence s lie at slots base(s), base(s) + 1, ...  Packed
-// sequences: base(s) = cu[s] / 64 + s needs no table of its own, and
-// base(s + 1) - base(s) is at least the sequence's chunks.  A sequence with
-// offsets out of range is empty.
-struct Seq {
-  int64_t t0, base;
-  int len;
-  __device__ Seq(const BwdArgs& a, int s) {
-    if (a.cu) {
-      const int b = a.cu[s], e = a.cu[s + 1];
-      const bool ok = b >= 0 && e >= b && e <= a.L;
-      t0 = ok ? b : 0;
-      len = ok ? e - b : 0;
-      base = t0 / BC + s;
-    } else {
-      t0 = (int64_t)s * a.L;
-      len = a.L;
-      base = (int64_t)s * a.nc;
-    }
-  }
-  __device__ int chunks() const { return (len + BC - 1) / BC; }
-};
-
-// first token and tokens (0: nothing to do) of the chunk at a slot
-__device__ __forceinline__ int chunk_at(const BwdArgs& a, int64_t slot, int64_t& t0) {
-  int s;
-  if (a.cu) {
-    int lo = 0, hi = a.nseq;  // the last s with base(s) <= slot
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.cu[mid] / BC + mid <= slot) lo = mid; else hi = mid;
-    }
-    s = lo;
-  } else {
-    s = (int)(slot / a.nc);
-  }
-  const Seq q(a, s);
-  const int64_t j = slot - q.base;
-  if (j < 0 || j * BC >= q.len) return 0;
-  t0 = q.t0 + j * BC;
-  return min(BC, q.len - (int)j * BC);
-}
-
-__device__ __forceinline__ f32x4 mma16(f32x4 a, f32x4 b, f32x4 acc) {
-#pragma unroll
-  for (int v = 0; v < 4; ++v)
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[v], b[v], acc, 0, 0, 0);
-  return acc;
-}
-
-// 4 values down a column (row stride ld), and 4 along a row
-__device__ __forceinline__ f32x4 down4(const float* p, int ld) {
-  return f32x4{p[0], p[ld], p[2 * ld], p[3 * ld]};
-}
-__device__ __forceinline__ f32x4 at4(const float* p) { return *(const f32x4*)p; }
-
-// rows of [tokens, H, D] (row stride ld values) into LDS as fp32, rows of PD
-// values; zeros past row m
-template <int D, int PD, typename T>
-__device__ __forceinline__ void rows_to_lds(float* s, const T* __restrict__ x, int64_t ld, int m) {
-  constexpr int E = 16 / sizeof(T), CPR = D / E;
-#pragma unroll
-  for (int i = 0; i < BC * CPR / 256; ++i) {
-    const int p = threadIdx.x + 256 * i, r = p / CPR, c = p % CPR * E;
-    f32x4 v[E / 4];
-#pragma unroll
-    for (int k = 0; k < E / 4; ++k) v[k] = zero4();
-    if (r < m)
-#pragma unroll
-      for (int k = 0; k < E / 4; ++k) v[k] = load4(x + r * ld + c + 4 * k);
-#pragma unroll
-    for (int k = 0; k < E / 4; ++k) *(f32x4*)(s + r * PD + c + 4 * k) = v[k];
-  }
-}
-
-// column-form block of rows r0 .. r0 + 15, columns from p's: as loaded (rows
-// past m repeat the last one, so that no load is behind a branch), and its
-// values (0 past m)
-template <typename T> struct RawBlock { T v[4]; };
-template <typename T>
-__device__ __forceinline__ RawBlock<T> raw_block(const T* __restrict__ p, int64_t ld, int r0, int m) {
-  RawBlock<T> x;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) x.v[v] = p[min(r0 + 4 * lane_g() + v, m - 1) * ld + lane_c()];
-  return x;
-}
-template <typename T>
-__device__ __forceinline__ f32x4 block_of(const RawBlock<T>& x, int r0, int m) {
-  f32x4 r;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) r[v] = (float)x.v[v];
-  if (m < r0 + 16)
-#pragma unroll
-    for (int v = 0; v < 4; ++v) r[v] = r0 + 4 * lane_g() + v < m ? r[v] : 0.f;
-  return r;
-}
-template <typename T>
-__device__ __forceinline__ f32x4 col_block(const T* __restrict__ p, int64_t ld, int r0, int m) {
-  return block_of(raw_block(p, ld, r0, m), r0, m);
-}
-
-// one block of a pair's terms as values
-__device__ __forceinline__ f32x4 half_of(const Terms<f32x4>& x, int hf) {
-  return hf ? x.t[0].hi() : x.t[0].lo();
-}
-__device__ __forceinline__ f32x4 half_of(const Terms<bf16x4>& x, int hf) {
-  return hf ? x.t[0].hi() + (x.t[1].hi() + x.t[2].hi()) : x.t[0].lo() + (x.t[1].lo() + x.t[2].lo());
-}
-
-template <typename T> struct FragOf { typedef f32x4 type; };
-template <> struct FragOf<__bf16> { typedef bf16x4 type; };
-
-}  // namespace
 
 // ---- every chunk: T, T^T and P^T dO
 template <int DK, int DV, typename T>
@@ -300,371 +147,6 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
       }
     }
   }
-}
-
-// A walk over the chunks of one (sequence, value head) for 16 value columns, four
-// waves.  The [dk, 16] part of the state lies in registers, wave w holding its
-// rows 32w .. 32w + 31 (two blocks, one pair).  A step is serial, so the
-// waves share each of its products: a product with the state is summed over
-// the waves' own rows (no wave needs another's state), the sums, then Z (dY)
-// and Y (dX) of row block w go through LDS, three exchanges a chunk.
-template <int DK, int DV, typename T>
-struct Walk {
-  typedef typename FragOf<T>::type F;
-  static constexpr int NT = TermsOf<F>::N, NQ = DK / 32, NS = DV / 16;
-  static constexpr int E = 16 / sizeof(T), LD = DK + E;  // rows in LDS, 16 bytes apart
-  static constexpr int CPR = DK / E, KI = BC * CPR / 256;
-  typedef T Vec __attribute__((ext_vector_type(E)));
-  // (sequence, value head) and first value column of this workgroup.  Workgroups
-  // are dealt to the 8 XCDs in turn; all slices of a head go to one XCD, whose
-  // L2 then reads the head's chunks once.
-  static __device__ __forceinline__ int64_t head_of(int& n0) {
-    const unsigned x = blockIdx.x, r = x >> 3;
-    n0 = (int)(r % NS) * 16;
-    return (int64_t)(r / NS) * 8 + (x & 7);
-  }
-  // A chunk's rows of K (Q) on their way to LDS.  Byte offsets from the chunk's
-  // first row: at most 64 rows of all heads, 32 bits; those of the rows past
-  // the chunk's last are clamped to it by their size.
-  struct Rows {
-    Vec v[KI];
-  };
-  static __device__ __forceinline__ void fetch(Rows& x, const T* p, const uint32_t (&off)[KI],
-                                               uint32_t last) {
-    const uint32_t col = threadIdx.x % CPR * 16;
-#pragma unroll
-    for (int i = 0; i < KI; ++i)
-      x.v[i] = *(const Vec*)((const char*)p + (min(off[i], last) + col));
-  }
-  static __device__ __forceinline__ void put(T* s, const Rows& x, int m) {
-    T* to = s + threadIdx.x / CPR * LD + threadIdx.x % CPR * E;
-    if (m == BC) {
-#pragma unroll
-      for (int i = 0; i < KI; ++i) *(Vec*)(to + 256 / CPR * i * LD) = x.v[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < KI; ++i)
-        *(Vec*)(to + 256 / CPR * i * LD) =
-            (int)threadIdx.x / CPR + 256 / CPR * i < m ? x.v[i] : Vec{};
-    }
-  }
-  // row block w of T (or T^T): two pairs of terms at most
-  struct TRow {
-    Terms<F> v[2];
-  };
-  static __device__ __forceinline__ void fetch_t(TRow& x, const float* p, int n, int l) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (i < n) x.v[i] = load_terms<F>((const T*)(p + TS * i), 0, l);
-  }
-  // this wave's share of the product of the 64 rows in LDS with the state
-  static __device__ __forceinline__ void share(const T* sK, const Terms<F>& s, float* part, int wv,
-                                               Lane ln) {
-#pragma unroll
-    for (int I = 0; I < 4; ++I)
-      *(f32x4*)(part + (4 * wv + I) * 256 + 4 * ln.id) =
-          mma_in<false>(row_pair<LD>(sK, 16 * I, 32 * wv, ln), s, zero4());
-  }
-  // the sum of the shares of row block wv
-  static __device__ __forceinline__ f32x4 sum(const float* part, int wv, int l) {
-    f32x4 x[NQ];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) x[q] = at4(part + (4 * q + wv) * 256 + 4 * l);
-    if constexpr (NQ == 4) return (x[0] + x[1]) + (x[2] + x[3]);
-    return x[0] + x[1];
-  }
-  // the transposed rows of this wave's two state blocks: [block][token pair]
-  struct Cols {
-    Pair<F> v[2][2];
-  };
-  static __device__ __forceinline__ void cols(Cols& x, const T* s, int wv, Lane ln) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) x.v[h][p] = col_pair<LD>(s, 32 * p, 32 * wv + 16 * h, ln);
-  }
-  static __device__ __forceinline__ void state_in(f32x4 (&st)[2], const float* p, int n0, int wv) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      st[h] = p && wv < NQ ? col_block(p + n0, DV, 32 * wv + 16 * h, DK) : zero4();
-  }
-  static __device__ __forceinline__ void state_out(float* p, const f32x4 (&st)[2], int n0, int wv) {
-    const uint32_t at = (32 * wv + 4 * lane_g()) * DV + n0 + lane_c();
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) p[at + (16 * h + v) * DV] = st[h][v];
-  }
-  // the same as row-form blocks, transposed through this wave's part of LDS
-  static constexpr int TB = 16 * 20;
-  static __device__ __forceinline__ void blocks_out(float* p, const f32x4 (&st)[2], int n0, int wv,
-                                                    float* t, Lane ln) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) t[TB * h + (4 * ln.g() + v) * 20 + ln.c()] = st[h][v];
-    lds_sync<true>();
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      *(f32x4*)(p + blk_at(2 * wv + h, n0 / 16, NS) + 4 * ln.id) =
-          at4(t + TB * h + ln.c() * 20 + 4 * ln.g());
-  }
-  // this lane's rows 16 wv + 4g + v of a column of V (dO): byte offsets as above
-  static __device__ __forceinline__ RawBlock<T> fetch_col(const T* p, const uint32_t (&off)[4],
-                                                          uint32_t last) {
-    RawBlock<T> x;
-    const uint32_t col = lane_c() * sizeof(T);
-#pragma unroll
-    for (int v = 0; v < 4; ++v) x.v[v] = *(const T*)((const char*)p + (min(off[v], last) + col));
-    return x;
-  }
-};
-
-// ---- the states entering the chunks
-template <int DK, int DV, typename T>
-__global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
-  typedef Walk<DK, DV, T> W;
-  typedef typename W::F F;
-  __shared__ __attribute__((aligned(16))) T sK[BC * W::LD];
-  __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
-  __shared__ __attribute__((aligned(16))) T sZ[2 * W::NT * 512], sY[2 * W::NT * 512];
-  __shared__ __attribute__((aligned(16))) float sT[W::NQ][2 * W::TB];
-  int n0;
-  const int64_t sh = W::head_of(n0);
-  if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
-  const int s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
-  const Seq sq(a, s);
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
-  const Lane ln = lane_here();
-  const int l = ln.id, g = ln.g(), c = ln.c(), r0 = 16 * wv + 4 * g;
-  const bool owner = wv < W::NQ;
-  const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
-  uint32_t koff[W::KI], voff[4];  // byte offsets of this thread's rows of K, of V
-#pragma unroll
-  for (int i = 0; i < W::KI; ++i)
-    koff[i] = (threadIdx.x + 256 * i) / W::CPR * (uint32_t)kld * sizeof(T);
-#pragma unroll
-  for (int v = 0; v < 4; ++v) voff[v] = (r0 + v) * (uint32_t)vld * sizeof(T);
-  f32x4 st[2];
-  W::state_in(st, a.S0 ? a.S0 + sh * DK * DV : nullptr, n0, wv);
-  if (nc == 0) return;
-  auto tile = [&](int ck) { return a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV); };
-  auto rows = [&](int ck) { return min(BC, sq.len - ck * BC); };
-  // what a chunk needs besides K, asked for a chunk ahead
-  struct Ops {
-    RawBlock<T> v;
-    f32x4 beta, eg, er;
-    float el;
-    typename W::TRow t;
-  };
-  auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
-    const float* ws = tile(ck);
-    const float* rv = ws + ws_rows();
-    W::fetch_t(x.t, ws + ws_T() + TS * t_slot(wv, 0), wv / 2 + 1, l);
-    x.v = W::fetch_col((const T*)a.V + ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0, voff,
-                       (rows(ck) - 1) * (uint32_t)vld * sizeof(T));
-    x.beta = at4(rv + r0);
-    x.eg = at4(rv + BC + r0);
-    x.er = at4(rv + 2 * BC + r0);
-    x.el = rv[2 * BC - 1];
-  };
-  auto keys = [&](typename W::Rows& x, int ck) __attribute__((always_inline)) {
-    W::fetch(x, (const T*)a.K + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, koff,
-             (rows(ck) - 1) * (uint32_t)kld * sizeof(T));
-  };
-  const int last = nc - 1;
-  // two sets, asked for two chunks ahead
-  Ops ops[2];
-  typename W::Rows krs[2];
-  keys(krs[0], 0);
-  fetch(ops[0], 0);
-  W::put(sK, krs[0], rows(0));
-  keys(krs[0], min(1, last));
-  fetch(ops[1], min(1, last));
-  keys(krs[1], min(2, last));
-  lds_only_barrier();
-  auto step = [&](int ck, Ops& op, typename W::Rows& kr) __attribute__((always_inline)) {
-    float* ws = tile(ck);
-    if (owner) {
-      W::blocks_out(ws + ws_S(DV), st, n0, wv, sT[wv], ln);
-      W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
-    }
-    lds_only_barrier();
-    typename W::Cols kc;
-    if (owner) W::cols(kc, sK, wv, ln);
-    {
-      const f32x4 x = block_of(op.v, 16 * wv, rows(ck)) - op.eg * W::sum(part, wv, l);
-      *(f32x4*)(ws + ws_X(DV) + blk_at(wv, n0 / 16, W::NS) + 4 * l) = x;
-      store_half<F>(sZ, wv >> 1, wv & 1, split_half<F>(op.beta * x), l);
-    }
-    lds_only_barrier();
-    W::put(sK, kr, rows(min(ck + 1, last)));
-    keys(kr, min(ck + 3, last));
-    __builtin_amdgcn_sched_barrier(0);
-    {
-      f32x4 y = zero4(), yl = zero4();
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-        if (p <= wv / 2) mma_both<false>(op.t.v[p], load_terms<F>(sZ, p, l), y, yl);
-      y += yl;
-      store_half<F>(sY, wv >> 1, wv & 1, split_half<F>(op.er * y), l);
-    }
-    const float el = op.el;
-    fetch(op, min(ck + 2, last));
-    lds_only_barrier();
-    if (owner) {
-      f32x4 x[2] = {zero4(), zero4()};
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const Terms<F> y = load_terms<F>(sY, p, l);
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(kc.v[hf][p], y, x[hf]);
-      }
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * el + x[hf];
-    }
-  };
-  for (int ck = 0; ck < nc; ck += 2) {
-    step(ck, ops[0], krs[0]);
-    if (ck + 1 < nc) step(ck + 1, ops[1], krs[1]);
-  }
-}
-
-// ---- the gradients of the states leaving the chunks, last chunk first
-template <int DK, int DV, typename T>
-__global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
-  typedef Walk<DK, DV, T> W;
-  typedef typename W::F F;
-  __shared__ __attribute__((aligned(16))) T sK[BC * W::LD], sQ[BC * W::LD];
-  __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
-  __shared__ __attribute__((aligned(16))) T sY[2 * W::NT * 512], sX[2 * W::NT * 512],
-      sO[2 * W::NT * 512];
-  __shared__ __attribute__((aligned(16))) float sT[W::NQ][2 * W::TB];
-  int n0;
-  const int64_t sh = W::head_of(n0);
-  if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
-  const int s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
-  const Seq sq(a, s);
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
-  const Lane ln = lane_here();
-  const int l = ln.id, g = ln.g(), c = ln.c(), r0 = 16 * wv + 4 * g;
-  const bool owner = wv < W::NQ;
-  const int64_t kld = (int64_t)a.Hk * DK, vld = (int64_t)a.Hv * DV;
-  uint32_t koff[W::KI], voff[4];  // byte offsets of this thread's rows of K and Q, of dO
-#pragma unroll
-  for (int i = 0; i < W::KI; ++i)
-    koff[i] = (threadIdx.x + 256 * i) / W::CPR * (uint32_t)kld * sizeof(T);
-#pragma unroll
-  for (int v = 0; v < 4; ++v) voff[v] = (r0 + v) * (uint32_t)vld * sizeof(T);
-  f32x4 st[2];
-  W::state_in(st, a.dSf ? a.dSf + sh * DK * DV : nullptr, n0, wv);
-  auto tile = [&](int ck) { return a.ws + ((sq.base + ck) * a.Hv + h) * ws_tile(DK, DV); };
-  auto rows = [&](int ck) { return min(BC, sq.len - ck * BC); };
-  auto vat = [&](int ck) { return ((sq.t0 + (int64_t)ck * BC) * a.Hv + h) * DV + n0; };
-  struct Ops {
-    RawBlock<T> o;
-    f32x4 r, beta, eg, er;
-    float el;
-    typename W::TRow t;
-  };
-  auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
-    const float* ws = tile(ck);
-    const float* rv = ws + ws_rows();
-    W::fetch_t(x.t, ws + ws_Tt() + TS * tt_slot(wv, wv / 2), 2 - wv / 2, l);
-    x.r = at4(ws + ws_R() + blk_at(wv, n0 / 16, W::NS) + 4 * l);
-    x.o = W::fetch_col((const T*)a.dO + vat(ck), voff, (rows(ck) - 1) * (uint32_t)vld * sizeof(T));
-    x.beta = at4(rv + r0);
-    x.eg = at4(rv + BC + r0);
-    x.er = at4(rv + 2 * BC + r0);
-    x.el = rv[2 * BC - 1];
-  };
-  auto keys = [&](typename W::Rows& x, const void* p, int ck) __attribute__((always_inline)) {
-    W::fetch(x, (const T*)p + ((sq.t0 + (int64_t)ck * BC) * a.Hk + hk) * DK, koff,
-             (rows(ck) - 1) * (uint32_t)kld * sizeof(T));
-  };
-  if (nc > 0) {
-    Ops ops[2];
-    typename W::Rows krs[2], qrs[2];
-    keys(krs[0], a.K, nc - 1);
-    fetch(ops[0], nc - 1);
-    keys(qrs[0], a.Q, nc - 1);
-    W::put(sK, krs[0], rows(nc - 1));
-    keys(krs[0], a.K, max(nc - 2, 0));
-    fetch(ops[1], max(nc - 2, 0));
-    keys(qrs[1], a.Q, max(nc - 2, 0));
-    keys(krs[1], a.K, max(nc - 3, 0));
-    lds_only_barrier();
-    auto step = [&](int ck, Ops& op, typename W::Rows& kr, typename W::Rows& qr)
-        __attribute__((always_inline)) {
-      float* ws = tile(ck);
-      W::put(sQ, qr, rows(ck));
-      keys(qr, a.Q, max(ck - 2, 0));
-      __builtin_amdgcn_sched_barrier(0);
-      store_half<F>(sO, wv >> 1, wv & 1,
-                    split_half<F>(block_of(op.o, 16 * wv, rows(ck)) * op.eg * a.scale), l);
-      if (owner) {
-        W::blocks_out(ws + ws_dS(DK, DV), st, n0, wv, sT[wv], ln);
-        W::share(sK, split<F>(st[0], st[1]), part, wv, ln);
-      }
-      lds_only_barrier();
-      typename W::Cols kc;
-      if (owner) W::cols(kc, sK, wv, ln);
-      store_half<F>(sY, wv >> 1, wv & 1,
-                    split_half<F>(op.r + op.er * W::sum(part, wv, l)), l);
-      lds_only_barrier();
-      W::put(sK, kr, rows(max(ck - 1, 0)));
-      keys(kr, a.K, max(ck - 3, 0));
-      __builtin_amdgcn_sched_barrier(0);
-      f32x4 x[2] = {zero4(), zero4()};
-      {
-        f32x4 z = zero4(), zl = zero4();
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-          if (p < 2 - wv / 2)
-            mma_both<false>(op.t.v[p], load_terms<F>(sY, p + wv / 2, l), z, zl);
-        z += zl;
-        const f32x4 dx = op.beta * z;
-        store_half<F>(sX, wv >> 1, wv & 1, split_half<F>(-op.eg * dx), l);
-        const int m = rows(ck);
-        *(f32x4*)(ws + ws_R() + blk_at(wv, n0 / 16, W::NS) + 4 * l) = z;
-        char* dV = (char*)((T*)a.dV + vat(ck));
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (r0 + v < m) *(T*)(dV + (voff[v] + (uint32_t)(c * sizeof(T)))) = (T)dx[v];
-        if (owner) {
-          typename W::Cols qc;
-          W::cols(qc, sQ, wv, ln);
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const Terms<F> o = load_terms<F>(sO, p, l);
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(qc.v[hf][p], o, x[hf]);
-          }
-        }
-      }
-      const float el = op.el;
-      // (chunk 0 again where there is none: its R has become dZ, which no step uses)
-      fetch(op, max(ck - 2, 0));
-      lds_only_barrier();
-      if (owner) {
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const Terms<F> y = load_terms<F>(sX, p, l);
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) x[hf] = mma_in<false>(kc.v[hf][p], y, x[hf]);
-        }
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) st[hf] = st[hf] * el + x[hf];
-      }
-    };
-    for (int ck = nc - 1; ck >= 0; ck -= 2) {
-      step(ck, ops[0], krs[0], qrs[0]);
-      if (ck > 0) step(ck - 1, ops[1], krs[1], qrs[1]);
-    }
-  }
-  if (a.dS0 && owner) W::state_out(a.dS0 + sh * DK * DV, st, n0, wv);
 }
 
 // ---- every chunk: dQ, dK, dbeta, dg; the value heads of a key head in turn
@@ -1061,13 +543,12 @@ int64_t backward_tile_bytes(int dk, int dv) { return ws_tile(dk, dv) * 4; }
 
 template <int DK, int DV, typename T>
 static hipError_t run_backward(const BwdArgs& a, int64_t slots, hipStream_t st) {
-  const unsigned walks = (unsigned)(((int64_t)a.nseq * a.Hv + 7) / 8 * 8 * (DV / 16));
-  if (slots > 0) {
+  if (slots > 0)
     hipLaunchKernelGGL((k_bwd_prep<DK, DV, T>), dim3((unsigned)(slots * a.Hv)), dim3(256), 0, st, a);
-    hipLaunchKernelGGL((k_bwd_states<DK, DV, T>), dim3(walks), dim3(256), 0, st, a);
+  if (slots > 0 || a.dS0) {
+    const hipError_t e = launch_walks(a, DK, DV, sizeof(T) == 4 ? 0 : 1, st);
+    if (e != hipSuccess) return e;
   }
-  if (slots > 0 || a.dS0)
-    hipLaunchKernelGGL((k_bwd_reverse<DK, DV, T>), dim3(walks), dim3(256), 0, st, a);
   if (slots > 0)
     hipLaunchKernelGGL((k_bwd_grads<DK, DV, T>), dim3((unsigned)(slots * a.Hk)), dim3(512), 0, st, a);
   return hipGetLastError();

@@ -80,6 +80,15 @@ __device__ __forceinline__ f32x4 mma_in(const Terms<F>& x, const Pair<F>& y, f32
     acc = Pair<F>::template mma<OUTQ>(x.t[i], y, acc);
   return acc;
 }
+// the same for N left operands and one right one, term after term, so that
+// neighbouring instructions do not wait for each other
+template <bool OUTQ, int N, typename F>
+__device__ __forceinline__ void mma_in(const Pair<F> (&x)[N], const Terms<F>& y, f32x4 (&acc)[N]) {
+#pragma unroll
+  for (int i = TermsOf<F>::N - 1; i >= 0; --i)
+#pragma unroll
+    for (int n = 0; n < N; ++n) acc[n] = Pair<F>::template mma<OUTQ>(x[n], y.t[i], acc[n]);
+}
 // acc += x y of two fp32 values
 template <bool OUTQ, typename F>
 __device__ __forceinline__ f32x4 mma_both(const Terms<F>& x, const Terms<F>& y, f32x4 acc) {
@@ -176,6 +185,14 @@ __device__ __forceinline__ void lds_only_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
+// The same for a wave that only copies to LDS by DMA and has waited for the copies
+// that the barrier is to publish: a fence would wait for all of them.
+__device__ __forceinline__ void copier_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 }  // namespace gdn
