@@ -17,11 +17,14 @@ template <typename F> struct TermsOf { static constexpr int N = 3; };
 template <> struct TermsOf<f32x4> { static constexpr int N = 1; };
 
 // two values rounded to bf16 in one register (the low half a), and what is left
-// of them.  The compiler rounds the two apart and packs them afterwards, at
-// twice the instructions.
+// of them.  (Taken apart by bits: from the converted values as such the compiler
+// rounds the two apart and packs them afterwards, at twice the instructions.  Not
+// by an instruction in assembly either: the wait states that a vector instruction
+// needs after a matrix instruction on its registers are not kept for it.)
 __device__ __forceinline__ uint32_t take2(float& a, float& b) {
-  uint32_t r;
-  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t r = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
   a -= __builtin_bit_cast(float, r << 16);
   b -= __builtin_bit_cast(float, r & 0xffff0000u);
   return r;

@@ -14,25 +14,21 @@ namespace gdn {
 namespace {
 
 // ---- bf16 inputs
-// The state's [dk, 16] part lies in the registers of WPS waves, a half of the
-// rows each when WPS = 2.  A wave forms everything of a chunk's step by itself, in
-// fragments that chain from one product to the next without leaving registers;
-// only the two halves of K S are exchanged (and added) through LDS.  Splitting the
-// step's rows over four waves instead, with three exchanges a chunk, took twice as
-// long.  Two more waves copy the next chunks' K (Q), T, V (dO) and gates into LDS by
-// DMA, so that neither the copies nor their waits lie in the chain.
+// One wave a slice holds the state's [dk, 16] part and forms everything of a chunk's
+// step by itself, in fragments that chain from one product to the next in
+// registers, without an exchange.  Two more waves of the workgroup copy the next
+// chunks' K (Q), T, V (dO) and gates into LDS by DMA, so that neither the copies nor
+// their waits lie in the chain.
 //   NSL: slices a workgroup; REV: the walk from the last chunk; R: chunks in the LDS
-//   ring (of Q, which a step reads last, always two)
-template <int DK, int DV, int NSL, int WPS, bool REV, int R>
+//   ring (of Q two)
+template <int DK, int DV, int NSL, bool REV, int R>
 struct Flow {
   typedef __bf16 T;
   typedef bf16x4 F;
   static constexpr int NS = DV / 16, NG = NS / NSL;  // slices, workgroups a head
-  static constexpr int NQ = DK / 32 / WPS, NB = 2 * NQ;  // pairs and blocks of state rows a wave
-  static constexpr int CW = NSL * WPS, LW = 2, B = 64 * (CW + LW);
-  // With three chunks in the ring Q(i) is asked for in step i - 1 and K (i) a step
-  // before, and both are awaited in the step after: Q by a barrier before its use.
-  static constexpr bool MID = WPS == 2 || (REV && R > 2);
+  static constexpr int NQ = DK / 32, NB = 2 * NQ;  // pairs and blocks of state rows
+  static constexpr int CW = NSL, LW = 2, B = 64 * (CW + LW);
+  static_assert(!REV || R == 2, "");
   // LDS of a chunk, in values of T
   static constexpr int oK = 0, oT = oK + BC * DK, oV = oT + 18 * 512, oR = oV + BC * 16 * NSL;
   static constexpr int BUF = oR + 512;
@@ -54,21 +50,6 @@ struct Flow {
     const int r = r0 + 4 * ln.g() + (ln.c() >> 2), k = c0 + 4 * (ln.c() & 3);
     return join(read_transposed(s + at(r, k)), read_transposed(s + at(r + 16, k)));
   }
-  // one wave a SIMD: every operand of a step in registers
-  static constexpr bool DEEP = CW + LW <= 4 && WPS == 2;
-  struct Keys {
-    Pair<F> v[DEEP ? NQ : 1][4];
-  };
-  struct Slots {
-    Terms<F> v[DEEP ? 6 : 4];
-  };
-  // the transposed rows of state pair q: [2 token pair + block]
-  static __device__ __forceinline__ void fill(Keys& x, const T* s, int q, int half, Lane ln) {
-    if constexpr (!DEEP)
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        x.v[0][k] = col_pair(s, 32 * (k >> 1), 16 * (half * NB + 2 * q + (k & 1)), ln);
-  }
   // column-form block of rows r0 .. and 16 columns c0 .. of the slices' rows of V (dO)
   static __device__ __forceinline__ f32x4 val_block(const T* s, int r0, int c0, Lane ln) {
     const int r = r0 + 4 * ln.g() + (ln.c() >> 2);
@@ -83,14 +64,13 @@ struct Flow {
 
 }  // namespace
 
-template <int DK, int DV, int NSL, int WPS, bool REV, int R>
-__global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_walk(const BwdArgs a) {
-  typedef Flow<DK, DV, NSL, WPS, REV, R> W;
+template <int DK, int DV, int NSL, bool REV, int R>
+__global__ __launch_bounds__((Flow<DK, DV, NSL, REV, R>::B)) void k_bwd_walk(const BwdArgs a) {
+  typedef Flow<DK, DV, NSL, REV, R> W;
   typedef __bf16 T;
   typedef bf16x4 F;
   constexpr int NQ = W::NQ, NB = W::NB, TB = 16 * 20;
   __shared__ __attribute__((aligned(16))) T sm[R][W::BUF], sq2[2][REV ? BC * DK : 8];
-  __shared__ __attribute__((aligned(16))) float part[NSL][WPS == 2 ? 2 * 1024 : 4];
   __shared__ __attribute__((aligned(16))) float tr[W::CW][2 * TB];
   // Workgroups are dealt to the 8 XCDs in turn; all those of a head go to one, whose
   // L2 then reads the head's chunks once.
@@ -110,8 +90,7 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
 
   if (wv >= W::CW) {
     // ---- loader.  Step i's operands are read between the barrier that ends step
-    // i - 1 and the one that ends step i (Q's after the barrier in the middle of step
-    // i).  Rows past a chunk's last token repeat it: their beta is 0, which takes them
+    // i - 1 and the one that ends step i.  Rows past a chunk's last token repeat it: their beta is 0, which takes them
     // out of Z and dX, and dO's are masked where they are used.  Steps past the
     // last load its operands again, into buffers that no step reads.
     const int lw = wv - W::CW;
@@ -163,7 +142,6 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
           else
             __builtin_amdgcn_s_waitcnt(0x0F70 | (n1 & 15) | ((n1 >> 4) << 14));
         }
-        if (W::MID) copier_barrier();
         if (R == 2) wait_vmem();
         copier_barrier();
       }
@@ -172,13 +150,13 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
     return;
   }
 
-  // ---- the waves of slice wv / WPS; this one has the state rows 16 NB half ..
-  const int sl = wv / WPS, half = wv % WPS, J = n0 / 16 + sl;
+  // ---- the wave of slice wv
+  const int sl = wv, J = n0 / 16 + sl;
   const float* init = REV ? a.dSf : a.S0;
   f32x4 st[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
-    st[b] = init ? col_block(init + sh * DK * DV + 16 * J, DV, 16 * (half * NB + b), DK) : zero4();
+    st[b] = init ? col_block(init + sh * DK * DV + 16 * J, DV, 16 * b, DK) : zero4();
   f32x4 r[4];  // R, asked for a chunk ahead
   auto fetch_r = [&](int ck) __attribute__((always_inline)) {
     const float* p = tile(ck) + ws_R() + 4 * l;
@@ -193,42 +171,17 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
     const T *sK = buf + W::oK, *sQ = sq2[i & 1], *sT = buf + W::oT, *sV = buf + W::oV;
     const float* rv = (const float*)(buf + W::oR) + 4 * g;  // beta, e^gamma, e^{gl - gamma}
     float* ws = tile(ck);
-    // All that the step reads of LDS, at once where a wave has a SIMD's registers to
-    // itself (41 waits of a hundred cycles each otherwise), else where it is used.
-    typename W::Keys kr, kc, qc;
-    typename W::Slots ts;
-    if constexpr (W::DEEP) {
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int I = 0; I < 4; ++I)
-          kr.v[q][I] = W::row_pair(sK, 16 * I, 32 * (half * NQ + q), ln);
-#pragma unroll
-      for (int k = 0; k < 6; ++k) ts.v[k] = load_terms<F>(sT, k, l);
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          kc.v[q][k] = W::col_pair(sK, 32 * (k >> 1), 16 * (half * NB + 2 * q + (k & 1)), ln);
-      __builtin_amdgcn_sched_barrier(0);
-    }
     // K S (K dS)
     f32x4 x[4];
 #pragma unroll
     for (int I = 0; I < 4; ++I) x[I] = zero4();
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      const Terms<F> sp = split<F>(st[2 * q], st[2 * q + 1]);
-      if constexpr (!W::DEEP)
+      Pair<F> kr[4];
 #pragma unroll
-        for (int I = 0; I < 4; ++I)
-          kr.v[0][I] = W::row_pair(sK, 16 * I, 32 * (half * NQ + q), ln);
-      mma_in<false, 4>(kr.v[W::DEEP ? q : 0], sp, x);
+      for (int I = 0; I < 4; ++I) kr[I] = W::row_pair(sK, 16 * I, 32 * q, ln);
+      mma_in<false, 4>(kr, split<F>(st[2 * q], st[2 * q + 1]), x);
     }
-    if constexpr (WPS == 2)
-#pragma unroll
-      for (int I = 0; I < 4; ++I)
-        *(f32x4*)(part[sl] + 1024 * half + 256 * I + 4 * l) = x[I];
     // the state, for the per-chunk launch: row-form blocks by way of LDS
     float* out = ws + (REV ? ws_dS(DK, DV) : ws_S(DV)) + 4 * l;
 #pragma unroll
@@ -241,27 +194,8 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
       lds_sync<true>();
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
-        *(f32x4*)(out + blk_at(half * NB + 2 * q + hf, J, W::NS)) = at4(t + TB * hf + c * 20 + 4 * g);
+        *(f32x4*)(out + blk_at(2 * q + hf, J, W::NS)) = at4(t + TB * hf + c * 20 + 4 * g);
       lds_sync<true>();
-    }
-    if constexpr (WPS == 2) {
-      // (R has come before the other wave may write dZ in its place)
-      if constexpr (REV)
-#pragma unroll
-        for (int I = 0; I < 4; ++I) pin(r[I]);
-      lds_only_barrier();
-#pragma unroll
-      for (int I = 0; I < 4; ++I) x[I] += at4(part[sl] + 1024 * (1 - half) + 256 * I + 4 * l);
-    } else if constexpr (W::MID) {
-      lds_only_barrier();
-    }
-    if constexpr (REV && W::DEEP) {
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          qc.v[q][k] = W::col_pair(sQ, 32 * (k >> 1), 16 * (half * NB + 2 * q + (k & 1)), ln);
-      __builtin_amdgcn_sched_barrier(0);
     }
     // Z (dY), then Y (dZ)
     Terms<F> y[2];
@@ -273,8 +207,7 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
           z[I] = r[I] + at4(rv + 2 * BC + 16 * I) * x[I];
         } else {
           const f32x4 xx = W::val_block(sV, 16 * I, 16 * sl, ln) - at4(rv + BC + 16 * I) * x[I];
-          if (WPS == 1 || I / 2 == half)
-            *(f32x4*)(ws + ws_X(DV) + blk_at(I, J, W::NS) + 4 * l) = xx;
+          *(f32x4*)(ws + ws_X(DV) + blk_at(I, J, W::NS) + 4 * l) = xx;
           z[I] = at4(rv + 16 * I) * xx;
         }
       }
@@ -287,17 +220,16 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
       for (int I = 0; I < 4; ++I) u[I] = ul[I] = zero4();
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
+        Terms<F> ts[4];
 #pragma unroll
         for (int k = 0; k < 6; ++k) {
           constexpr int tx[6] = {0, 1, 2, 1, 0, 0}, ty[6] = {2, 1, 0, 0, 1, 0};
 #pragma unroll
           for (int I = 0; I < 4; ++I) {
             if (REV ? p < I / 2 : p > I / 2) continue;
-            const int sl6 = REV ? tt_slot(I, p) : t_slot(I, p);
-            if constexpr (!W::DEEP)
-              if (k == 0) ts.v[I] = load_terms<F>(sT, sl6, l);
+            if (k == 0) ts[I] = load_terms<F>(sT, REV ? tt_slot(I, p) : t_slot(I, p), l);
             f32x4& acc = k & 1 ? u[I] : ul[I];
-            acc = Pair<F>::template mma<false>(ts.v[W::DEEP ? sl6 : I].t[tx[k]], zt[p].t[ty[k]], acc);
+            acc = Pair<F>::template mma<false>(ts[I].t[tx[k]], zt[p].t[ty[k]], acc);
           }
         }
       }
@@ -305,16 +237,13 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
       for (int I = 0; I < 4; ++I) {
         u[I] += ul[I];
         if constexpr (REV) {
-          if (WPS == 1 || I / 2 == half)
-            *(f32x4*)(ws + ws_R() + blk_at(I, J, W::NS) + 4 * l) = u[I];
+          *(f32x4*)(ws + ws_R() + blk_at(I, J, W::NS) + 4 * l) = u[I];
           u[I] = at4(rv + 16 * I) * u[I];  // dX
-          if (WPS == 1 || I / 2 == half) {
-            const int m = rows(ck), r0 = 16 * I + 4 * g;
-            T* dV = (T*)a.dV + ((sq.t0 + (int64_t)ck * BC + r0) * a.Hv + h) * DV + 16 * J + c;
+          const int m = rows(ck), r0 = 16 * I + 4 * g;
+          T* dV = (T*)a.dV + ((sq.t0 + (int64_t)ck * BC + r0) * a.Hv + h) * DV + 16 * J + c;
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-              if (r0 + v < m) dV[v * vld] = (T)u[I][v];
-          }
+          for (int v = 0; v < 4; ++v)
+            if (r0 + v < m) dV[v * vld] = (T)u[I][v];
           z[I] = -at4(rv + BC + 16 * I) * u[I];
         } else {
           z[I] = at4(rv + 2 * BC + 16 * I) * u[I];
@@ -339,16 +268,20 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         f32x4 u[2] = {zero4(), zero4()}, w[2] = {zero4(), zero4()};
-        W::fill(kc, sK, q, half, ln);
-        W::fill(qc, sQ, q, half, ln);
+        Pair<F> qc[4], kc[4];  // [2 token pair + block]
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          qc[k] = W::col_pair(sQ, 32 * (k >> 1), 32 * q + 16 * (k & 1), ln);
+          kc[k] = W::col_pair(sK, 32 * (k >> 1), 32 * q + 16 * (k & 1), ln);
+        }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
           for (int t = 2; t >= 0; --t)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              u[hf] = Pair<F>::template mma<false>(qc.v[W::DEEP ? q : 0][2 * p + hf], ot[p].t[t], u[hf]);
-              w[hf] = Pair<F>::template mma<false>(kc.v[W::DEEP ? q : 0][2 * p + hf], y[p].t[t], w[hf]);
+              u[hf] = Pair<F>::template mma<false>(qc[2 * p + hf], ot[p].t[t], u[hf]);
+              w[hf] = Pair<F>::template mma<false>(kc[2 * p + hf], y[p].t[t], w[hf]);
             }
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) st[2 * q + hf] = st[2 * q + hf] * el + (u[hf] + w[hf]);
@@ -359,14 +292,17 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
       for (int b = 0; b < NB; ++b) u[b] = zero4();
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
-        W::fill(kc, sK, q, half, ln);
+        Pair<F> kc[4];  // [2 token pair + block]
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          kc[k] = W::col_pair(sK, 32 * (k >> 1), 32 * q + 16 * (k & 1), ln);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
           for (int t = 2; t >= 0; --t)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf)
-              u[2 * q + hf] = Pair<F>::template mma<false>(kc.v[W::DEEP ? q : 0][2 * p + hf], y[p].t[t],
+              u[2 * q + hf] = Pair<F>::template mma<false>(kc[2 * p + hf], y[p].t[t],
                                                            u[2 * q + hf]);
       }
 #pragma unroll
@@ -379,7 +315,7 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
-        a.dS0[sh * DK * DV + (int64_t)(16 * (half * NB + b) + 4 * g + v) * DV + 16 * J + c] =
+        a.dS0[sh * DK * DV + (int64_t)(16 * b + 4 * g + v) * DV + 16 * J + c] =
             st[b][v];
 }
 
@@ -392,8 +328,8 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, WPS, REV, R>::B)) void k_bwd_wal
 // the rest in step i - 1.  Four loaders: a copy takes one 60 ns to issue, and the
 // barriers wait for it.
 template <int DK, int DV, bool REV>
-struct Team : Flow<DK, DV, 1, 1, REV, 2> {
-  typedef Flow<DK, DV, 1, 1, REV, 2> W;
+struct Team : Flow<DK, DV, 1, REV, 2> {
+  typedef Flow<DK, DV, 1, REV, 2> W;
   static constexpr int LW = 4, B = 64 * (4 + LW), NQ = DK / 32;
   // copies a loader: of K or Q, and of T, V and the gates
   static constexpr int KN = W::KC / LW, QN = REV ? KN : 0, TN = (18 + LW - 1) / LW + 2;
@@ -1011,16 +947,24 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
 template <int DK, int DV, bool REV>
 static void walk_bf16(const BwdArgs& a, hipStream_t st) {
   const int64_t heads = (int64_t)a.nseq * a.Hv, slices = heads * (DV / 16);
-#define GDN_WALK(NSL, WPS, R)                                                                    \
-  hipLaunchKernelGGL((k_bwd_walk<DK, DV, NSL, WPS, REV, R>),                                     \
-                     dim3((unsigned)((heads + 7) / 8 * 8 * (DV / 16 / NSL))),                    \
-                     dim3(Flow<DK, DV, NSL, WPS, REV, R>::B), 0, st, a)
-  if (slices <= 512)
+  // A CU takes one team (a slice) or one workgroup of four lone waves (four slices).
+  // A team's step takes 1.9 us (REV 2.4), a workgroup's 3.9 (6.0), so teams walk up to
+  // two rounds of slices: us for 32 chunks, DK = DV = 128, 512 slices 127 (REV 160),
+  // 768 slices 197 (245), where the lone waves take 127 (195).  Packed sequences
+  // differ in length, and their number says little of how many walk side by side
+  // for long: with 22 sequences of 1 to 4096 tokens, 2816 slices, teams take 183
+  // (227), lone waves 191 (320).  Taken as a sixth of their number.
+  const int64_t chains = a.cu ? slices / 6 : slices;
+  if (chains <= 512) {
     hipLaunchKernelGGL((k_bwd_team<DK, DV, REV>),
-                       dim3((unsigned)((heads + 7) / 8 * 8 * (DV / 16))), dim3(Team<DK, DV, REV>::B), 0, st, a);
-  else
-    GDN_WALK(4, 1, REV ? 2 : 3);
-#undef GDN_WALK
+                       dim3((unsigned)((heads + 7) / 8 * 8 * (DV / 16))),
+                       dim3(Team<DK, DV, REV>::B), 0, st, a);
+  } else {
+    constexpr int R = REV ? 2 : 3;
+    hipLaunchKernelGGL((k_bwd_walk<DK, DV, 4, REV, R>),
+                       dim3((unsigned)((heads + 7) / 8 * 8 * (DV / 64))),
+                       dim3(Flow<DK, DV, 4, REV, R>::B), 0, st, a);
+  }
 }
 
 template <int DK, int DV>

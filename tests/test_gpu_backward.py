@@ -110,6 +110,28 @@ def test_packed(dt, C):
     compare(run(x, lens, C, 64 ** -0.5, True), oracle(x, lens, C, 64 ** -0.5), dt)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,Hk,Hv,dk,dv,packed", [
+    (3, 130, 11, 22, 128, 128, False), (5, 97, 9, 27, 64, 64, False),
+    (2, 200, 17, 34, 64, 128, False), (140, 80, 3, 6, 128, 64, True)])
+def test_many_slices(dt, B, L, Hk, Hv, dk, dv, packed):
+    """Past 512 slices of 16 value columns (packed sequences: past six times
+    that many) the walks run another way: sampled sequences and heads."""
+    lens = [1 + s * (L - 1) // (B - 1) for s in range(B)] if packed else [L] * B
+    assert B * Hv * dv // 16 > (3072 if packed else 512)
+    x = make(lens, Hk, Hv, dk, dv, 64, dt, dv)
+    got = run(x, lens, 64, 0.3, packed)
+    r = Hv // Hk
+    for s, hk in [(0, 0), (B - 1, Hk - 1), (B // 2, Hk // 2)]:
+        t = sum(lens[:s])
+        w, hv = slice(t, t + lens[s]), slice(hk * r, (hk + 1) * r)
+        sub = {k: (v[s:s + 1, hv] if k in ("S0", "dS") else
+                   v[w, hk:hk + 1] if k in ("Q", "K") else v[w, hv]) for k, v in x.items()}
+        flat = [a.reshape((-1,) + tuple(a.shape[2:])) for a in got[:5]]
+        part = [a[w, hk:hk + 1] if i < 2 else a[w, hv] for i, a in enumerate(flat)]
+        compare(part + [got[5][s:s + 1, hv]], oracle(sub, [lens[s]], 64, 0.3), dt)
+
+
 def test_packed_is_each_sequence_alone_bit_for_bit():
     lens = [70, 3, 129]
     x = make(lens, 1, 2, 64, 64, 64, "bf16", 1)
