@@ -171,16 +171,6 @@ struct Grads {
   static constexpr int SIZE = oEnd2 > oEnd ? oEnd2 : oEnd;
 };
 
-// sum over the 16 lanes of a row of the wave
-__device__ __forceinline__ float sum16(float x) {
-  auto add = [&](int y) { x += __builtin_bit_cast(float, y); };
-  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));   // lane ^ 1
-  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true));   // lane ^ 2
-  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x141, 0xf, 0xf, true));  // 7 - lane
-  add(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x140, 0xf, 0xf, true));  // 15 - lane
-  return x;
-}
-
 template <int DK, int DV, typename T>
 __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
   typedef Grads<DK, DV, T> G;

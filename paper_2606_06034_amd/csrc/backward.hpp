@@ -5,6 +5,7 @@
 #include "chunk.hpp"
 #include "engine.hpp"
 #include "forward.hpp"
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "layer.hpp"
 #include "split.hpp"

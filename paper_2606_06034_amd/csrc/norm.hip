@@ -11,9 +11,9 @@
 // registers, not over memory; a workgroup walks rows with its weights, and
 // in the backward pass its sums for dw and db, in registers.  The sums of the
 // workgroups go through a workspace and are added up by a second launch in a
-// fixed order (no atomics: the same call gives the same bits).  Rows past
-// 1024 x 2 pieces are read from memory twice (three times with a mean) by one
-// workgroup each.
+// fixed order (no atomics: the same call gives the same bits).  Rows too long for
+// the registers are read from memory in every pass, by one workgroup each.
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "layer.hpp"
 #include "tile16.hpp"
@@ -37,6 +37,19 @@ template <> struct Piece<__bf16> {
   bf16x8u v;
 };
 
+// a piece as it lies in memory (0 past the row's end), and its values
+template <typename T>
+__device__ __forceinline__ auto load_raw(const T* __restrict__ row, int e, int D) {
+  constexpr int E = Piece<T>::E;
+  decltype(Piece<T>::v) p;
+  if (e + E <= D) {
+    p = *(const decltype(Piece<T>::v)*)(row + e);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) p[i] = e + i < D ? row[e + i] : (T)0.f;
+  }
+  return p;
+}
 // elements e .. e + E - 1 of a row of D (0 past its end)
 template <typename T, int E = Piece<T>::E>
 __device__ __forceinline__ void load_piece(float (&x)[E], const T* __restrict__ row, int e, int D) {
@@ -95,11 +108,8 @@ __device__ __forceinline__ float sigmoid(float z) {
 // calls take in turn, so that one barrier a call is enough.
 template <int TPR>
 __device__ __forceinline__ void row_sums(float& a, float& b, float* red, int& buf) {
-#pragma unroll
-  for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) {
-    a += __shfl_xor(a, o);
-    b += __shfl_xor(b, o);
-  }
+  a = sum_lanes<(TPR < 64 ? TPR : 64)>(a);
+  b = sum_lanes<(TPR < 64 ? TPR : 64)>(b);
   if constexpr (TPR > 64) {
     constexpr int W = TPR / 64;
     float* r = red + buf * 32;
@@ -272,10 +282,17 @@ struct GradPiece {
   }
 };
 
+// A row's pieces as they lie in memory, asked for a row ahead.
+template <typename T, int NV, bool GATE>
+struct RawRow {
+  decltype(Piece<T>::v) x[NV], dy[NV], z[GATE ? NV : 1];
+  float mean, rstd;
+};
+
 // Workgroups of B threads, B / TPR rows at a time; each leaves its sums of dw
 // and db in row blockIdx.x of the workspace: ws [parts][D], then the same for
-// db.  want: bit 0 dw, bit 1 db.
-template <typename T, int TPR, int NV, int B>
+// db.  want: bit 0 dw, bit 1 db.  GATE: z is given; BIAS: b or db is.
+template <typename T, int TPR, int NV, int B, bool GATE, bool BIAS>
 __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
   constexpr int E = Piece<T>::E, RPB = B / TPR;
   extern __shared__ float part[];  // 64 values of row_sums, then the sums [2][D]
@@ -283,49 +300,81 @@ __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
   float* sum = part + 64;
   int buf = 0;
   const int t = threadIdx.x % TPR, r = threadIdx.x / TPR, D = a.D;
-  float w[NV][E], bias[NV][E], dw[NV][E], db[NV][E];
+  float w[NV][E], bias[GATE && BIAS ? NV : 1][E], dw[NV][E], db[BIAS ? NV : 1][E];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     load_param<E>(w[k], a.w, a.wbf, 1.f, (t + k * TPR) * E, D);
-    load_param<E>(bias[k], a.z ? a.b : nullptr, a.wbf, 0.f, (t + k * TPR) * E, D);
+    if constexpr (GATE && BIAS) load_param<E>(bias[k], a.b, a.wbf, 0.f, (t + k * TPR) * E, D);
 #pragma unroll
-    for (int i = 0; i < E; ++i) dw[k][i] = db[k][i] = 0.f;
+    for (int i = 0; i < E; ++i) {
+      dw[k][i] = 0.f;
+      if constexpr (BIAS) db[k][i] = 0.f;
+    }
   }
   const float inv = 1.f / (float)D;
-  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
-    const bool live = row0 + r < a.rows;
-    const int64_t row = live ? row0 + r : a.rows - 1;
-    const float mean = a.rms ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
-    GradPiece<T> p[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) p[k].form(a, row, (t + k * TPR) * E, w[k], bias[k], mean, rstd);
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float dh = p[k].dn[i] * w[k][i];
-        s1 += dh;
-        // (past the row's end dn is 0 and xh finite only by luck: x is 0 there)
-        s2 = __builtin_fmaf(dh, p[k].h[i], s2);
-      }
-    row_sums<TPR>(s1, s2, red, buf);
-    if (!live) continue;
-    s1 = a.rms ? 0.f : s1 * inv;
-    s2 *= inv;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  typedef RawRow<T, NV, GATE> Row;
+  auto fetch = [&](Row& x, int64_t row) __attribute__((always_inline)) {
+    row = row < a.rows ? row : a.rows - 1;
+    const int64_t at = row * D;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int e = (t + k * TPR) * E;
-      float dx[E];
+      x.x[k] = load_raw<T>((const T*)a.x + at, e, D);
+      x.dy[k] = load_raw<T>((const T*)a.dy + at, e, D);
+      if constexpr (GATE) x.z[k] = load_raw<T>((const T*)a.z + at, e, D);
+    }
+    x.mean = a.rms ? 0.f : a.mean_in[row];
+    x.rstd = a.rstd_in[row];
+  };
+  Row cur, nx;
+  fetch(cur, (int64_t)blockIdx.x * RPB + r);
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += step) {
+    fetch(nx, row0 + step + r);
+    const bool live = row0 + r < a.rows;
+    const int64_t at = (live ? row0 + r : a.rows - 1) * D;
+    // dn (dy without a gate) and dz, then the row's two sums
+    float dn[NV][E], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float dz[E];
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        dx[i] = rstd * (p[k].dn[i] * w[k][i] - s1 - p[k].h[i] * s2);
-        dw[k][i] = __builtin_fmaf(p[k].dn[i], p[k].h[i], dw[k][i]);
-        db[k][i] += p[k].dn[i];
+        const float h = ((float)cur.x[k][i] - cur.mean) * cur.rstd;
+        float d = (float)cur.dy[k][i];
+        if constexpr (GATE) {
+          const float z = (float)cur.z[k][i], s = sigmoid(z);
+          float n = h * w[k][i];
+          if constexpr (BIAS) n += bias[k][i];
+          dz[i] = d * n * (s * __builtin_fmaf(z, 1.f - s, 1.f));
+          d *= z * s;
+        }
+        dn[k][i] = d;
+        const float dh = d * w[k][i];
+        s1 += dh;
+        s2 = __builtin_fmaf(dh, h, s2);  // (past the row's end d is 0)
       }
-      store_piece<T>((T*)a.out + row * D, dx, e, D);
-      if (a.z) store_piece<T>((T*)a.dz + row * D, p[k].dz, e, D);
+      if constexpr (GATE)
+        if (live) store_piece<T>((T*)a.dz + at, dz, (t + k * TPR) * E, D);
     }
+    row_sums<TPR>(s1, s2, red, buf);
+    if (live) {
+      s1 = a.rms ? 0.f : s1 * inv;
+      s2 *= inv;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float dx[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float h = ((float)cur.x[k][i] - cur.mean) * cur.rstd;
+          dx[i] = cur.rstd * (dn[k][i] * w[k][i] - s1 - h * s2);
+          dw[k][i] = __builtin_fmaf(dn[k][i], h, dw[k][i]);
+          if constexpr (BIAS) db[k][i] += dn[k][i];
+        }
+        store_piece<T>((T*)a.out + at, dx, (t + k * TPR) * E, D);
+      }
+    }
+    cur = nx;
   }
   if (!want) return;
   // the sums of the rows that ran side by side: within a wave by exchange,
@@ -337,7 +386,7 @@ __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
 #pragma unroll
       for (int o = TPR; o < 64; o <<= 1) {
         dw[k][i] += __shfl_xor(dw[k][i], o);
-        db[k][i] += __shfl_xor(db[k][i], o);
+        if constexpr (BIAS) db[k][i] += __shfl_xor(db[k][i], o);
       }
   constexpr int GROUPS = TPR < 64 ? B / 64 : RPB;
   const int64_t at = (int64_t)blockIdx.x * D, half = (int64_t)gridDim.x * D;
@@ -348,7 +397,8 @@ __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
       for (int i = 0; i < E; ++i) {
         const int e = (t + k * TPR) * E + i;
         if (e < D && (want & 1)) a.ws[at + e] = dw[k][i];
-        if (e < D && (want & 2)) a.ws[half + at + e] = db[k][i];
+        if constexpr (BIAS)
+          if (e < D && (want & 2)) a.ws[half + at + e] = db[k][i];
       }
     return;
   }
@@ -362,14 +412,14 @@ __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
           const int e = (t + k * TPR) * E + i;
           if (e < D) {
             sum[e] = gi ? sum[e] + dw[k][i] : dw[k][i];
-            sum[D + e] = gi ? sum[D + e] + db[k][i] : db[k][i];
+            if constexpr (BIAS) sum[D + e] = gi ? sum[D + e] + db[k][i] : db[k][i];
           }
         }
     __syncthreads();
   }
   for (int e = threadIdx.x; e < D; e += B) {
     if (want & 1) a.ws[at + e] = sum[e];
-    if (want & 2) a.ws[half + at + e] = sum[D + e];
+    if (BIAS && (want & 2)) a.ws[half + at + e] = sum[D + e];
   }
 }
 
@@ -431,6 +481,7 @@ __global__ __launch_bounds__(256) void k_norm_parts(const float* __restrict__ ws
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
   float x = 0.f;
   if (d < D)
+#pragma unroll 8
     for (int p = r; p < parts; p += 16) x += from[(int64_t)p * D + d];
   s[r][c] = x;
   __syncthreads();
@@ -470,14 +521,26 @@ template <typename T>
 static hipError_t norm_backward(const NormArgs& a, int want, hipStream_t st) {
   const int n = (a.D + Piece<T>::E - 1) / Piece<T>::E;
   const int parts = norm_backward_parts(a.rows, a.D);
-#define GDN_X(TPR, NV)                                                                           \
-  if (n <= TPR * NV) {                                                                           \
-    hipLaunchKernelGGL((k_norm_grad<T, TPR, NV, 1024>), dim3((unsigned)parts), dim3(1024),       \
-                       (64 + (TPR < 1024 ? 2 * a.D : 0)) * sizeof(float), st, a, want);          \
-    return hipGetLastError();                                                                    \
+  const bool bias = a.b || (want & 2);
+#define GDN_G(TPR, NV, GATE, BIAS)                                                          \
+  hipLaunchKernelGGL((k_norm_grad<T, TPR, NV, 1024, GATE, BIAS>), dim3((unsigned)parts),    \
+                     dim3(1024), (64 + (TPR < 1024 ? 2 * a.D : 0)) * sizeof(float), st, a, want)
+#define GDN_X(TPR, NV)                                        \
+  if (n <= TPR * NV) {                                        \
+    if (a.z && bias) GDN_G(TPR, NV, true, true);              \
+    else if (a.z) GDN_G(TPR, NV, true, false);                \
+    else if (bias) GDN_G(TPR, NV, false, true);               \
+    else GDN_G(TPR, NV, false, false);                        \
+    return hipGetLastError();                                 \
   }
-  GDN_NORM_SHAPES(GDN_X)
+  // one piece a thread: two with their sums pass the 128 registers that a workgroup
+  // of 1024 threads has for each (with fp32's four values a piece they do not)
+  GDN_X(16, 1) GDN_X(32, 1) GDN_X(64, 1) GDN_X(128, 1) GDN_X(256, 1) GDN_X(512, 1) GDN_X(1024, 1)
+  if constexpr (sizeof(T) == 4) {
+    GDN_X(1024, 2)
+  }
 #undef GDN_X
+#undef GDN_G
   hipLaunchKernelGGL((k_norm_grad_long<T>), dim3((unsigned)parts), dim3(1024), 0, st, a, want);
   return hipGetLastError();
 }
