@@ -41,8 +41,8 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
   typedef typename FragOf<T>::type F;
   constexpr int LD = BC + 4;
   __shared__ float sA[BC * LD], sP[BC * LD], sr[5][BC];
-  const int64_t slot = blockIdx.x / a.Hv;
-  const int h = (int)(blockIdx.x - slot * a.Hv), hk = h / (a.Hv / a.Hk);
+  const uint32_t slot = blockIdx.x / (uint32_t)a.Hv;
+  const int h = (int)(blockIdx.x - slot * (uint32_t)a.Hv), hk = h / a.gr;
   int64_t t0 = 0;
   const int m = chunk_at(a, slot, t0);
   if (m == 0) return;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const int i = 16 * wv + 4 * g + v, j = 16 * J + c;
-        const float d = i >= j ? expf((sr[3][i] - sr[3][j]) + (sr[4][i] - sr[4][j])) : 0.f;
+        const float d = i >= j ? __expf((sr[3][i] - sr[3][j]) + (sr[4][i] - sr[4][j])) : 0.f;
         sA[i * LD + j] = i > j ? -sr[0][i] * kk[v] * d : 0.f;
         sP[i * LD + j] = i >= j ? a.scale * qk[v] * d : 0.f;
       }
@@ -176,14 +176,15 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
   typedef Grads<DK, DV, T> G;
   typedef typename G::F F;
   constexpr int NT = G::NT, NP = G::NP, NR = G::NR, LDK = G::LDK;
-  constexpr int E = 16 / sizeof(T), NJ = DV / 16, RY = 8 / NJ;
+  constexpr int E = 16 / sizeof(T), NJ = DV / 16, RY = 8 / NJ, TB = 16 * 20;
   typedef T Vec __attribute__((ext_vector_type(E)));
   __shared__ __attribute__((aligned(16))) T sm[G::SIZE];
   __shared__ __attribute__((aligned(16))) float sr[5][BC];
-  __shared__ __attribute__((aligned(16))) float tr[8][16 * 20];
-  __shared__ float sdb[NJ][BC], red[2][G::NC][BC], sdg[BC], send[8];
-  const int64_t slot = blockIdx.x / a.Hk;
-  const int hk = (int)(blockIdx.x - slot * a.Hk), gr = a.Hv / a.Hk;
+  __shared__ __attribute__((aligned(16))) float tr[8][2 * TB];
+  __shared__ __attribute__((aligned(16))) float sdb[NJ][BC];
+  __shared__ float red[2][G::NC][BC], sdg[BC], send[8];
+  const uint32_t slot = blockIdx.x / (uint32_t)a.Hk;
+  const int hk = (int)(blockIdx.x - slot * (uint32_t)a.Hk), gr = a.gr;
   int64_t t0 = 0;
   const int m = chunk_at(a, slot, t0);
   if (m == 0) return;
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
     asm volatile("" : "+v"(tid));
     const Lane ln{tid & 63};
     const int l = ln.id, g = ln.g(), c = ln.c();
-    float* ws = a.ws + (slot * a.Hv + h) * ws_tile(DK, DV);
+    float* ws = a.ws + ((int64_t)slot * a.Hv + h) * ws_tile(DK, DV);
     const float* S = ws + ws_S(DV) + blk_at(col / 16, 0, NJ) + 4 * l;
     const float* dS = ws + ws_dS(DK, DV) + blk_at(col / 16, 0, NJ) + 4 * l;
     // S and dS of a pair of value column blocks
@@ -248,18 +249,30 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int p = 0; p < 2; ++p) z[p] = split<F>(bt[2 * p] * xb[2 * p], bt[2 * p + 1] * xb[2 * p + 1]);
+      // dZ in row form by way of LDS, two blocks a turn
       float* t = tr[wv];
 #pragma unroll
-      for (int I = 0; I < 4; ++I) {
-        if (I % RY != wv / NJ) continue;
+      for (int n = 0; n < 4 / RY; n += 2) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          t[(4 * g + v) * 20 + c] = zb[I][v];
-          const float d = sum16(xb[I][v] * zb[I][v]);
-          if (c == 0) sdb[J][16 * I + 4 * g + v] = d;
+        for (int k = 0; k < 2; ++k) {
+          const int I = (n + k) * RY + wv / NJ;
+          const f32x4 zv = wv / NJ ? zb[(n + k) * RY + RY - 1] : zb[(n + k) * RY];
+          const f32x4 xv = wv / NJ ? xb[(n + k) * RY + RY - 1] : xb[(n + k) * RY];
+          f32x4 dot;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            t[TB * k + (4 * g + v) * 20 + c] = zv[v];
+            dot[v] = sum16(xv[v] * zv[v]);
+          }
+          if (c == 0) *(f32x4*)(sdb[J] + 16 * I + 4 * g) = dot;
         }
         lds_sync<true>();
-        store_half<F>(sm + G::oZ, I * NP + (J >> 1), J & 1, split_half<F>(at4(t + c * 20 + 4 * g)), l);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int I = (n + k) * RY + wv / NJ;
+          store_half<F>(sm + G::oZ, I * NP + (J >> 1), J & 1,
+                        split_half<F>(at4(t + TB * k + c * 20 + 4 * g)), l);
+        }
         lds_sync<true>();
       }
 #pragma unroll
@@ -274,22 +287,43 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
         if (tid + 512 * i < TN) *(Vec*)(sm + G::oT + (tid + 512 * i) * E) = tv[i];
     }
     __syncthreads();
-    // ---- Y = T Z: value column block J of the rows I % RY
+    // ---- Y = T Z: value column block J of the rows I % RY; the terms of each kind side
+    // by side, so that neighbouring instructions do not wait for each other
+    constexpr int tx[6] = {0, 1, 2, 1, 0, 0}, ty[6] = {2, 1, 0, 0, 1, 0};
+    {
+      constexpr int RN = 4 / RY;
+      f32x4 y[RN], yl[RN];
 #pragma unroll
-    for (int I = 0; I < 4; ++I) {
-      if (I % RY != wv / NJ) continue;
-      f32x4 y = zero4(), yl = zero4();
+      for (int n = 0; n < RN; ++n) y[n] = yl[n] = zero4();
 #pragma unroll
-      for (int p = 0; p <= I / 2; ++p)
-        mma_both<true>(load_terms<F>(sm + G::oT, t_slot(I, p), l), z[p], y, yl);
-      store_half<F>(sm + G::oY, I * NP + (J >> 1), J & 1, split_half<F>(y + yl), l);
+      for (int p = 0; p < 2; ++p) {
+        Terms<F> ts[RN];
+#pragma unroll
+        for (int n = 0; n < RN; ++n) {
+          const int I = n * RY + wv / NJ;  // (2 p <= I where p <= n RY / 2)
+          if (p <= n * RY / 2) ts[n] = load_terms<F>(sm + G::oT, t_slot(I, p), l);
+        }
+#pragma unroll
+        for (int k = NT == 1 ? 5 : 0; k < 6; ++k)
+#pragma unroll
+          for (int n = 0; n < RN; ++n)
+            if (p <= n * RY / 2) {
+              f32x4& acc = k & 1 ? y[n] : yl[n];
+              acc = Pair<F>::template mma<true>(ts[n].t[NT == 1 ? 0 : tx[k]], z[p].t[NT == 1 ? 0 : ty[k]],
+                                                acc);
+            }
+      }
+#pragma unroll
+      for (int n = 0; n < RN; ++n)
+        store_half<F>(sm + G::oY, (n * RY + wv / NJ) * NP + (J >> 1), J & 1,
+                      split_half<F>(y[n] + yl[n]), l);
     }
     States st;
     states(st, 0);
     __syncthreads();
     // ---- dP and E, a lower block each; an E block costs as much as two of dP
     struct Blk {
-      int kind, I, J;  // kind: 0 dP, 1 E, -1 none
+      int kind, I, J;  // kind: 0 dP, 1 E, -1 none (then any block)
     };
     auto block = [&](int i) __attribute__((always_inline)) {
       // waves 0, 1: two of E; the others one of E and two (6, 7: one) of dP
@@ -304,34 +338,46 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
         kind = wv < 6 || i == 1 ? 0 : -1;
         n = wv < 6 ? 2 * (wv - 2) + i - 1 : wv + 2;
       }
+      n = min(n, 9);
       const int I = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
       return Blk{kind, I, n - I * (I + 1) / 2};
     };
-    f32x4 pe[3];
+    f32x4 pe[3], pl[3];
+    Blk bk[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-      const Blk k = block(i);
-      f32x4 x = zero4(), xl = zero4();
-      if (k.kind == 1) {
+      bk[i] = block(i);
+      pe[i] = pl[i] = zero4();
+    }
 #pragma unroll 1
-        for (int p = 0; p < NP; ++p)
-          mma_both<false>(load_terms<F>(sm + G::oZ, k.I * NP + p, l),
-                          load_terms<F>(sm + G::oY, k.J * NP + p, l), x, xl);
-      } else if (k.kind == 0) {
-#pragma unroll 1
-        for (int p = 0; p < NP; ++p)
-          x = mma_in<false>(slot_load<F>(sm + G::oO + (k.I * NP + p) * 512, l),
-                            load_terms<F>(sm + G::oY, k.J * NP + p, l), x);
-      }
-      x += xl;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int r = 16 * k.I + 4 * g + v, j = 16 * k.J + c;
-        const float d = r >= j ? expf((sr[3][r] - sr[3][j]) + (sr[4][r] - sr[4][j])) : 0.f;
-        pe[i][v] = k.kind == 1 ? (r > j ? -x[v] * d : 0.f) : a.scale * x[v] * d;
+    for (int p = 0; p < NP; ++p) {
+      // the first is an E; the second another (waves 0, 1) or a dP, the third a dP
+      Terms<F> e0 = load_terms<F>(sm + G::oZ, bk[0].I * NP + p, l);
+      Terms<F> y0 = load_terms<F>(sm + G::oY, bk[0].J * NP + p, l);
+      if (wv < 2) {
+        const Terms<F> e1 = load_terms<F>(sm + G::oZ, bk[1].I * NP + p, l);
+        const Terms<F> y1 = load_terms<F>(sm + G::oY, bk[1].J * NP + p, l);
+        mma_both<false>(e0, y0, pe[0], pl[0]);
+        mma_both<false>(e1, y1, pe[1], pl[1]);
+      } else {
+        const Pair<F> o1 = slot_load<F>(sm + G::oO + (bk[1].I * NP + p) * 512, l);
+        const Terms<F> y1 = load_terms<F>(sm + G::oY, bk[1].J * NP + p, l);
+        mma_both<false>(e0, y0, pe[0], pl[0]);
+        pe[1] = mma_in<false>(o1, y1, pe[1]);
+        if (bk[2].kind == 0)
+          pe[2] = mma_in<false>(slot_load<F>(sm + G::oO + (bk[2].I * NP + p) * 512, l),
+                                load_terms<F>(sm + G::oY, bk[2].J * NP + p, l), pe[2]);
       }
     }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int r = 16 * bk[i].I + 4 * g + v, j = 16 * bk[i].J + c;
+        const float x = pe[i][v] + pl[i][v];
+        const float d = r >= j ? __expf((sr[3][r] - sr[3][j]) + (sr[4][r] - sr[4][j])) : 0.f;
+        pe[i][v] = bk[i].kind == 1 ? (r > j ? -x * d : 0.f) : a.scale * x * d;
+      }
     // ---- dO S^T, dZ S^T, Y dS^T and <S, dS>
     constexpr int CPR = DK / E, KN = BC * CPR / 512;
     Vec kv[KN], qv[KN];
@@ -367,11 +413,15 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
         const Pair<F> o = slot_load<F>(sm + G::oO + at * 512, l);
         const Terms<F> z = load_terms<F>(sm + G::oZ, at, l), y = load_terms<F>(sm + G::oY, at, l);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          dq[b][i] = mma_in<false>(o, sv[b], dq[b][i]);
-          zs[b][i] = mma_both<false>(z, sv[b], zs[b][i]);
-          yd[b][i] = mma_both<false>(y, dv[b], yd[b][i]);
-        }
+        for (int k = NT == 1 ? 5 : 0; k < 6; ++k)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int kx = NT == 1 ? 0 : tx[k], ky = NT == 1 ? 0 : ty[k];
+            zs[b][i] = Pair<F>::template mma<true>(z.t[kx], sv[b].t[ky], zs[b][i]);
+            yd[b][i] = Pair<F>::template mma<true>(y.t[kx], dv[b].t[ky], yd[b][i]);
+            if (k >= 6 - NT)
+              dq[b][i] = Pair<F>::template mma<true>(o, sv[b].t[5 - k], dq[b][i]);
+          }
       }
     }
     __syncthreads();
@@ -385,7 +435,7 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      const Blk k = block(i);
+      const Blk k = bk[i];
       if (k.kind < 0) continue;
       T* rows = sm + (k.kind ? G::oEr : G::oPr);
       T* cols = sm + (k.kind ? G::oEc : G::oPc);
@@ -418,18 +468,23 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
       }
     // The sums over the value heads of a key head, in the place of the first one's
     // states (which nothing reads any more); the last one writes the results.
-    float* acc = a.ws + (slot * a.Hv + hk * gr) * ws_tile(DK, DV) + ws_S(DV) + 4 * tid;
+    float* acc = a.ws + ((int64_t)slot * a.Hv + hk * gr) * ws_tile(DK, DV) + ws_S(DV) + 4 * tid;
     float end = 0.f;
+    T* const dQp = (T*)a.dQ + kat;
+    T* const dKp = (T*)a.dK + kat;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const int I = I0 + i, r0 = 16 * I + 4 * g;
-      const f32x4 bt = at4(&sr[0][r0]), eg = at4(&sr[1][r0]), er = at4(&sr[2][r0]);
-      f32x4 F_[2], km[2], R[2];
+      // row form: this lane has row r, 4 columns
+      const int I = I0 + i, r = 16 * I + c;
+      const float bt = sr[0][r], eg = sr[1][r], er = sr[2][r];
+      f32x4 F_[2], km[2], ke[2], R[2], kv[2], qv[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        dq[b][i] = dq[b][i] * eg * a.scale;
-        F_[b] = zero4();
+        kv[b] = load4(sm + G::oK + r * LDK + col + 16 * b + 4 * g);
+        qv[b] = load4(sm + G::oQ + r * LDK + col + 16 * b + 4 * g);
+        dq[b][i] *= eg * a.scale;
         R[b] = km[b] = er * yd[b][i];
+        F_[b] = ke[b] = zero4();
       }
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -437,32 +492,36 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
           const Terms<F> P = load_terms<F>(sm + G::oPr, t_slot(I, p), l);
           const Terms<F> Er = load_terms<F>(sm + G::oEr, t_slot(I, p), l);
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            dq[b][i] = mma_in<false>(P, kf[b][p], dq[b][i]);
-            F_[b] = mma_in<false>(Er, kf[b][p], F_[b]);
-          }
+          for (int k = NT - 1; k >= 0; --k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              dq[b][i] = Pair<F>::template mma<true>(P.t[k], kf[b][p], dq[b][i]);
+              F_[b] = Pair<F>::template mma<true>(Er.t[k], kf[b][p], F_[b]);
+            }
         }
         if (p >= I / 2) {
           const Terms<F> P = load_terms<F>(sm + G::oPc, tt_slot(I, p), l);
           const Terms<F> Ec = load_terms<F>(sm + G::oEc, tt_slot(I, p), l);
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            km[b] = mma_in<false>(P, qf[b][p], km[b]);
-            km[b] = mma_in<false>(Ec, kf[b][p], km[b]);
-          }
+          for (int k = NT - 1; k >= 0; --k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              km[b] = Pair<F>::template mma<true>(P.t[k], qf[b][p], km[b]);
+              ke[b] = Pair<F>::template mma<true>(Ec.t[k], kf[b][p], ke[b]);
+            }
         }
       }
-      f32x4 dotF = zero4(), dotG = zero4();
+      float dotF = 0.f, dotG = 0.f;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const f32x4 kp = bt * (F_[b] - eg * zs[b][i]);
-        // the rows' own k and q, from the pair that holds their block
-        const Pair<F> kk = I < 2 ? kf[b][0] : kf[b][1], qq = I < 2 ? qf[b][0] : qf[b][1];
-        const f32x4 k = I & 1 ? kk.hi() : kk.lo(), q = I & 1 ? qq.hi() : qq.lo();
-        dotF += k * F_[b];
-        dotG += q * dq[b][i] + k * (kp - km[b]);
+        km[b] += ke[b];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) end = __builtin_fmaf(k[v], R[b][v], end);
+        for (int v = 0; v < 4; ++v) {
+          dotF = __builtin_fmaf(kv[b][v], F_[b][v], dotF);
+          dotG += qv[b][v] * dq[b][i][v] + kv[b][v] * (kp[v] - km[b][v]);
+          end = __builtin_fmaf(kv[b][v], R[b][v], end);
+        }
         f32x4 sq = dq[b][i], sk = kp + km[b];
         float* at = acc + (b * NR + i) * 2 * 2048;
         if (h > hk * gr) {
@@ -472,23 +531,19 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
         if (h + 1 < (hk + 1) * gr) {
           *(f32x4*)at = sq;
           *(f32x4*)(at + 2048) = sk;
-        } else {
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            if (r0 + v < m) {
-              const int64_t to = kat + (r0 + v) * kld + col + 16 * b + c;
-              ((T*)a.dQ)[to] = (T)sq[v];
-              ((T*)a.dK)[to] = (T)sk[v];
-            }
+        } else if (r < m) {
+          const uint32_t to = (uint32_t)r * (uint32_t)kld + (uint32_t)(col + 16 * b + 4 * g);
+          store4(dQp + to, sq);
+          store4(dKp + to, sk);
         }
       }
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float f = sum16(dotF[v]), d = sum16(dotG[v]);
-        if (c == 0) {
-          red[0][wv % G::NC][r0 + v] = f;
-          red[1][wv % G::NC][r0 + v] = d;
-        }
+      dotF += __shfl_xor(dotF, 16);
+      dotG += __shfl_xor(dotG, 16);
+      dotF += __shfl_xor(dotF, 32);
+      dotG += __shfl_xor(dotG, 32);
+      if (g == 0) {
+        red[0][wv % G::NC][r] = dotF;
+        red[1][wv % G::NC][r] = dotG;
       }
     }
     // (every row group has formed the same <S, dS> of its columns)
@@ -550,7 +605,7 @@ hipError_t launch_backward(const void* Q, const void* K, const void* V, const fl
                            float* ws, const int* cu, int nseq, int L, int Hk, int Hv, int dk,
                            int dv, int C, float scale, int dtype, hipStream_t st) {
   BwdArgs a{Q,  K,     V,  dO,  beta, g,  S0,   dSf, dQ,              dK, dV, dbeta,
-            dg, dS0,   ws, cu,  nseq, L,  (L + BC - 1) / BC, Hk, Hv, C, scale};
+            dg, dS0,   ws, cu,  nseq, L,  (L + BC - 1) / BC, Hk, Hv, C, scale, Hk ? Hv / Hk : 1};
   const int64_t slots = L > 0 ? backward_slots(nseq, L, cu != nullptr) : 0;
   GDN_DK_SWITCH(dk, GDN_DV_SWITCH(dv, {
     return dtype == 0 ? run_backward<DK, DV, float>(a, slots, st)

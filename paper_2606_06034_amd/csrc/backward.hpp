@@ -42,6 +42,7 @@ struct BwdArgs {
   int nc;       // chunks a sequence (cu not given)
   int Hk, Hv, C;
   float scale;
+  int gr;  // value heads a key head
 };
 
 // The chunks of sequence s lie at slots base(s), base(s) + 1, ...  Packed
@@ -68,17 +69,18 @@ struct Seq {
 };
 
 // first token and tokens (0: nothing to do) of the chunk at a slot
-__device__ __forceinline__ int chunk_at(const BwdArgs& a, int64_t slot, int64_t& t0) {
+// (slots and heads of a launch fit 32 bits; a 64-bit division takes a thousand cycles)
+__device__ __forceinline__ int chunk_at(const BwdArgs& a, uint32_t slot, int64_t& t0) {
   int s;
   if (a.cu) {
     int lo = 0, hi = a.nseq;  // the last s with base(s) <= slot
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.cu[mid] / BC + mid <= slot) lo = mid; else hi = mid;
+      if (a.cu[mid] / BC + mid <= (int)slot) lo = mid; else hi = mid;
     }
     s = lo;
   } else {
-    s = (int)(slot / a.nc);
+    s = (int)(slot / (uint32_t)a.nc);
   }
   const Seq q(a, s);
   const int64_t j = slot - q.base;

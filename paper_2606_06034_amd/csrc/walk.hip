@@ -77,8 +77,8 @@ __global__ __launch_bounds__((Flow<DK, DV, NSL, REV, R>::B)) void k_bwd_walk(con
   const unsigned xr = blockIdx.x >> 3;
   const int64_t sh = (int64_t)(xr / W::NG) * 8 + (blockIdx.x & 7);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
-  const int n0 = (int)(xr % W::NG) * 16 * NSL, s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
+  const int n0 = (int)(xr % W::NG) * 16 * NSL, s = (int)((uint32_t)sh / (uint32_t)a.Hv);
+  const int h = (int)((uint32_t)sh - (uint32_t)s * (uint32_t)a.Hv), hk = h / a.gr;
   const Seq sq(a, s);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
   const Lane ln = lane_here();
@@ -353,8 +353,8 @@ __global__ __launch_bounds__((Team<DK, DV, REV>::B)) void k_bwd_team(const BwdAr
   const unsigned xr = blockIdx.x >> 3;  // all slices of a head on one XCD
   const int64_t sh = (int64_t)(xr / NS) * 8 + (blockIdx.x & 7);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
-  const int J = (int)(xr % NS), s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
+  const int J = (int)(xr % NS), s = (int)((uint32_t)sh / (uint32_t)a.Hv);
+  const int h = (int)((uint32_t)sh - (uint32_t)s * (uint32_t)a.Hv), hk = h / a.gr;
   const Seq sq(a, s);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
   const Lane ln = lane_here();
@@ -709,8 +709,8 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
   int n0;
   const int64_t sh = W::head_of(n0);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
-  const int s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
+  const int s = (int)((uint32_t)sh / (uint32_t)a.Hv);
+  const int h = (int)((uint32_t)sh - (uint32_t)s * (uint32_t)a.Hv), hk = h / a.gr;
   const Seq sq(a, s);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
   const Lane ln = lane_here();
@@ -821,8 +821,8 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
   int n0;
   const int64_t sh = W::head_of(n0);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
-  const int s = (int)(sh / a.Hv);
-  const int h = (int)(sh - (int64_t)s * a.Hv), hk = h / (a.Hv / a.Hk);
+  const int s = (int)((uint32_t)sh / (uint32_t)a.Hv);
+  const int h = (int)((uint32_t)sh - (uint32_t)s * (uint32_t)a.Hv), hk = h / a.gr;
   const Seq sq(a, s);
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nc = sq.chunks();
   const Lane ln = lane_here();
