@@ -21,9 +21,9 @@
 // of are these dot products, so K K^T and Q K^T are not formed again; F is
 // divided by nothing, so beta = 0 is an ordinary value.)
 //
-// Four launches: k_bwd_prep (every chunk: T, P^T dO), k_bwd_states (the states
-// entering the chunks, first to last), k_bwd_reverse (the gradients of the
-// states leaving them, last to first), k_bwd_grads (every chunk: the
+// Three launches: k_bwd_prep (every chunk: T, P^T dO), the walks along the chunks of
+// walk.hip (the states entering the chunks, first to last, and the gradients of the
+// states leaving them, last to first, side by side), k_bwd_grads (every chunk: the
 // gradients).  The chunks here are always of 64 tokens, whatever chunk size
 // the caller's g restarts at (16, 32 or 64): the result of the exact layer
 // does not depend on it, and gamma is g plus the last g of the 64-chunk's

@@ -28,10 +28,16 @@ struct Flow {
   static constexpr int NS = DV / 16, NG = NS / NSL;  // slices, workgroups a head
   static constexpr int NQ = DK / 32, NB = 2 * NQ;  // pairs and blocks of state rows
   static constexpr int CW = NSL, LW = 2, B = 64 * (CW + LW);
+  static constexpr int KD = DK, VD = DV, RING = R, TB = 16 * 20;
+  static constexpr bool BACK = REV;
   static_assert(!REV || R == 2, "");
   // LDS of a chunk, in values of T
   static constexpr int oK = 0, oT = oK + BC * DK, oV = oT + 18 * 512, oR = oV + BC * 16 * NSL;
   static constexpr int BUF = oR + 512;
+  struct Lds {
+    T sm[R][BUF], sq2[2][REV ? BC * DK : 8];
+    float tr[CW][2 * TB];
+  };
   // rows of K and Q in 16-byte pieces, piece p of row r at p ^ (r & SW): the 16 rows that
   // a wave reads one piece of lie in different banks
   static constexpr int CPR = DK / 8, SW = CPR - 1, RPI = 64 / CPR;
@@ -64,14 +70,16 @@ struct Flow {
 
 }  // namespace
 
-template <int DK, int DV, int NSL, bool REV, int R>
-__global__ __launch_bounds__((Flow<DK, DV, NSL, REV, R>::B)) void k_bwd_walk(const BwdArgs a) {
-  typedef Flow<DK, DV, NSL, REV, R> W;
+template <typename W>
+__device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& lds) {
+  constexpr int DK = W::KD, DV = W::VD, NSL = W::CW, R = W::RING;
+  constexpr bool REV = W::BACK;
   typedef __bf16 T;
   typedef bf16x4 F;
-  constexpr int NQ = W::NQ, NB = W::NB, TB = 16 * 20;
-  __shared__ __attribute__((aligned(16))) T sm[R][W::BUF], sq2[2][REV ? BC * DK : 8];
-  __shared__ __attribute__((aligned(16))) float tr[W::CW][2 * TB];
+  constexpr int NQ = W::NQ, NB = W::NB, TB = W::TB;
+  auto& sm = lds.sm;
+  auto& sq2 = lds.sq2;
+  auto& tr = lds.tr;
   // Workgroups are dealt to the 8 XCDs in turn; all those of a head go to one, whose
   // L2 then reads the head's chunks once.
   const unsigned xr = blockIdx.x >> 3;
@@ -335,21 +343,29 @@ struct Team : Flow<DK, DV, 1, REV, 2> {
   static constexpr int KN = W::KC / LW, QN = REV ? KN : 0, TN = (18 + LW - 1) / LW + 2;
   static constexpr int oT = 0, oV = 18 * 512, oR = oV + BC * 16, oQ = oR + 512;
   static constexpr int BUF = oQ + (REV ? BC * DK : 0);
+  struct Lds {
+    typename W::T sk[2][BC * DK], sm[2][BUF];
+    float part[NQ * 4 * 256], tr[NQ][2 * W::TB];
+    typename W::T sZ[6 * 512], sY[6 * 512], sO[REV ? 6 * 512 : 8];
+  };
   template <int N>
   static __device__ __forceinline__ void wait() {  // for all but the last N copies
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
   }
 };
 
-template <int DK, int DV, bool REV>
-__global__ __launch_bounds__((Team<DK, DV, REV>::B)) void k_bwd_team(const BwdArgs a) {
-  typedef Team<DK, DV, REV> W;
+template <typename W>
+__device__ __forceinline__ void team(const BwdArgs& a, typename W::Lds& lds) {
+  constexpr int DK = W::KD, DV = W::VD;
+  constexpr bool REV = W::BACK;
   typedef __bf16 T;
   typedef bf16x4 F;
-  constexpr int NQ = W::NQ, NS = DV / 16, TB = 16 * 20;
-  __shared__ __attribute__((aligned(16))) T sk[2][BC * DK], sm[2][W::BUF];
-  __shared__ __attribute__((aligned(16))) float part[NQ * 4 * 256], tr[NQ][2 * TB];
-  __shared__ __attribute__((aligned(16))) T sZ[6 * 512], sY[6 * 512], sO[REV ? 6 * 512 : 8];
+  constexpr int NQ = W::NQ, NS = DV / 16, TB = W::TB;
+  auto& sk = lds.sk;
+  auto& sm = lds.sm;
+  auto& tr = lds.tr;
+  float* part = lds.part;
+  T *sZ = lds.sZ, *sY = lds.sY, *sO = lds.sO;
   const unsigned xr = blockIdx.x >> 3;  // all slices of a head on one XCD
   const int64_t sh = (int64_t)(xr / NS) * 8 + (blockIdx.x & 7);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
@@ -585,13 +601,18 @@ __global__ __launch_bounds__((Team<DK, DV, REV>::B)) void k_bwd_team(const BwdAr
 // state's rows 32w .. 32w + 31 (two blocks, one pair); a product with the state is
 // summed over the waves' own rows (no wave needs another's state), the sums, then
 // Z (dY) and Y (dX) of row block w go through LDS, three exchanges a chunk.
-template <int DK, int DV, typename T>
+template <int DK, int DV>
 struct Walk {
-  typedef typename FragOf<T>::type F;
-  static constexpr int NT = TermsOf<F>::N, NQ = DK / 32, NS = DV / 16;
-  static constexpr int E = 16 / sizeof(T), LD = DK + E;  // rows in LDS, 16 bytes apart
-  static constexpr int CPR = DK / E, KI = BC * CPR / 256;
-  typedef T Vec __attribute__((ext_vector_type(E)));
+  typedef float T;
+  typedef f32x4 F;
+  static constexpr int NQ = DK / 32, NS = DV / 16;
+  static constexpr int E = 4, LD = DK + E;  // rows in LDS, 16 bytes apart
+  static constexpr int CPR = DK / E, KI = BC * CPR / 256, TB = 16 * 20;
+  typedef f32x4 Vec;
+  struct Lds {
+    float sK[BC * LD], sQ[BC * LD], part[NQ * 4 * 256], sZ[2 * 512], sY[2 * 512], sO[2 * 512];
+    float sT[NQ][2 * TB];
+  };
   // (sequence, value head) and first value column of this workgroup.  Workgroups
   // are dealt to the 8 XCDs in turn; all slices of a head go to one XCD, whose
   // L2 then reads the head's chunks once.
@@ -673,7 +694,6 @@ struct Walk {
       for (int v = 0; v < 4; ++v) p[at + (16 * h + v) * DV] = st[h][v];
   }
   // the same as row-form blocks, transposed through this wave's part of LDS
-  static constexpr int TB = 16 * 20;
   static __device__ __forceinline__ void blocks_out(float* p, const f32x4 (&st)[2], int n0, int wv,
                                                     float* t, Lane ln) {
 #pragma unroll
@@ -698,14 +718,13 @@ struct Walk {
 };
 
 // ---- the states entering the chunks
-template <int DK, int DV, typename T>
-__global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
-  typedef Walk<DK, DV, T> W;
-  typedef typename W::F F;
-  __shared__ __attribute__((aligned(16))) T sK[BC * W::LD];
-  __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
-  __shared__ __attribute__((aligned(16))) T sZ[2 * W::NT * 512], sY[2 * W::NT * 512];
-  __shared__ __attribute__((aligned(16))) float sT[W::NQ][2 * W::TB];
+template <int DK, int DV>
+__device__ __forceinline__ void states_f32(const BwdArgs& a, typename Walk<DK, DV>::Lds& lds) {
+  typedef Walk<DK, DV> W;
+  typedef float T;
+  typedef f32x4 F;
+  float *sK = lds.sK, *part = lds.part, *sZ = lds.sZ, *sY = lds.sY;
+  auto& sT = lds.sT;
   int n0;
   const int64_t sh = W::head_of(n0);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
@@ -809,15 +828,13 @@ __global__ __launch_bounds__(256) void k_bwd_states(const BwdArgs a) {
 }
 
 // ---- the gradients of the states leaving the chunks, last chunk first
-template <int DK, int DV, typename T>
-__global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
-  typedef Walk<DK, DV, T> W;
-  typedef typename W::F F;
-  __shared__ __attribute__((aligned(16))) T sK[BC * W::LD], sQ[BC * W::LD];
-  __shared__ __attribute__((aligned(16))) float part[W::NQ * 4 * 256];
-  __shared__ __attribute__((aligned(16))) T sY[2 * W::NT * 512], sX[2 * W::NT * 512],
-      sO[2 * W::NT * 512];
-  __shared__ __attribute__((aligned(16))) float sT[W::NQ][2 * W::TB];
+template <int DK, int DV>
+__device__ __forceinline__ void reverse_f32(const BwdArgs& a, typename Walk<DK, DV>::Lds& lds) {
+  typedef Walk<DK, DV> W;
+  typedef float T;
+  typedef f32x4 F;
+  float *sK = lds.sK, *sQ = lds.sQ, *part = lds.part, *sX = lds.sZ, *sY = lds.sY, *sO = lds.sO;
+  auto& sT = lds.sT;
   int n0;
   const int64_t sh = W::head_of(n0);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
@@ -944,40 +961,69 @@ __global__ __launch_bounds__(256) void k_bwd_reverse(const BwdArgs a) {
   if (a.dS0 && owner) W::state_out(a.dS0 + sh * DK * DV, st, n0, wv);
 }
 
-template <int DK, int DV, bool REV>
-static void walk_bf16(const BwdArgs& a, hipStream_t st) {
-  const int64_t heads = (int64_t)a.nseq * a.Hv, slices = heads * (DV / 16);
-  // A CU takes one team (a slice) or one workgroup of four lone waves (four slices).
-  // A team's step takes 1.9 us (REV 2.4), a workgroup's 3.9 (6.0), so teams walk up to
-  // two rounds of slices: us for 32 chunks, DK = DV = 128, 512 slices 127 (REV 160),
-  // 768 slices 197 (245), where the lone waves take 127 (195).  Packed sequences
-  // differ in length, and their number says little of how many walk side by side
-  // for long: with 22 sequences of 1 to 4096 tokens, 2816 slices, teams take 183
-  // (227), lone waves 191 (320).  Taken as a sixth of their number.
-  const int64_t chains = a.cu ? slices / 6 : slices;
-  if (chains <= 512) {
-    hipLaunchKernelGGL((k_bwd_team<DK, DV, REV>),
-                       dim3((unsigned)((heads + 7) / 8 * 8 * (DV / 16))),
-                       dim3(Team<DK, DV, REV>::B), 0, st, a);
-  } else {
-    constexpr int R = REV ? 2 : 3;
-    hipLaunchKernelGGL((k_bwd_walk<DK, DV, 4, REV, R>),
-                       dim3((unsigned)((heads + 7) / 8 * 8 * (DV / 64))),
-                       dim3(Flow<DK, DV, 4, REV, R>::B), 0, st, a);
-  }
+// ---- both walks in one launch: neither reads what the other writes, and one of them
+// leaves half the chip idle where slices are few.  The slower one goes first.  (One
+// after the other, 128 chunks of 16 heads of 128 by 128 in bf16 took 213 + 265 us
+// where they take 303 now, 16 chunks in fp32 43 + 62 where they take 64.  Past 256
+// slices of fp32 it costs some 8%: 2 x 512 slices of 32 chunks 447 for 415 us, since a
+// CU takes two workgroups of the walk over the states alone.)
+template <int DK, int DV>
+__global__ __launch_bounds__(512) void k_bwd_teams(const BwdArgs a) {
+  typedef Team<DK, DV, true> R;
+  typedef Team<DK, DV, false> S;
+  static_assert(R::B == 512 && S::B == 512, "");
+  __shared__ union __attribute__((aligned(16))) {
+    typename R::Lds r;
+    typename S::Lds s;
+  } lds;
+  if (blockIdx.y == 0)
+    team<R>(a, lds.r);
+  else
+    team<S>(a, lds.s);
+}
+
+template <int DK, int DV>
+__global__ __launch_bounds__(384) void k_bwd_lone(const BwdArgs a) {
+  typedef Flow<DK, DV, 4, true, 2> R;
+  typedef Flow<DK, DV, 4, false, 3> S;
+  static_assert(R::B == 384 && S::B == 384, "");
+  __shared__ union __attribute__((aligned(16))) {
+    typename R::Lds r;
+    typename S::Lds s;
+  } lds;
+  if (blockIdx.y == 0)
+    lone_waves<R>(a, lds.r);
+  else
+    lone_waves<S>(a, lds.s);
+}
+
+template <int DK, int DV>
+__global__ __launch_bounds__(256) void k_bwd_walks_f32(const BwdArgs a) {
+  __shared__ __attribute__((aligned(16))) typename Walk<DK, DV>::Lds lds;
+  if (blockIdx.y == 0)
+    reverse_f32<DK, DV>(a, lds);
+  else
+    states_f32<DK, DV>(a, lds);
 }
 
 template <int DK, int DV>
 static hipError_t run_walks(const BwdArgs& a, int dtype, hipStream_t st) {
-  if (dtype == 1) {
-    if (a.L > 0) walk_bf16<DK, DV, false>(a, st);
-    walk_bf16<DK, DV, true>(a, st);
-  } else {
-    const unsigned n = (unsigned)(((int64_t)a.nseq * a.Hv + 7) / 8 * 8 * (DV / 16));
-    if (a.L > 0)
-      hipLaunchKernelGGL((k_bwd_states<DK, DV, float>), dim3(n), dim3(256), 0, st, a);
-    hipLaunchKernelGGL((k_bwd_reverse<DK, DV, float>), dim3(n), dim3(256), 0, st, a);
-  }
+  const int64_t heads = (int64_t)a.nseq * a.Hv, slices = heads * (DV / 16);
+  const unsigned n = (unsigned)((heads + 7) / 8 * 8), both = a.L > 0 ? 2 : 1;
+  // A CU takes one team (a slice) or one workgroup of four lone waves (four slices).
+  // A team's step takes 2.3 us at most, a workgroup's 4 to 6, so teams walk while both
+  // directions' are two rounds: us for 32 chunks, DK = DV = 128, teams and lone waves:
+  // 128 slices 70 and 139, 256 133 and 148, 320 190 and 165, 512 281 and 187.  Packed
+  // sequences differ in length, and few of them walk side by side for long; 8192 tokens
+  // in 4 of them (512 slices) take 292 and 299, in 9 (1152) 298 and 179 to 299 and 320,
+  // in 22 (2816) 376 and 345; with half the heads in 11 (704) 155 and 255.
+  const int64_t chains = a.cu ? slices / 4 : slices;
+  if (dtype == 0)
+    hipLaunchKernelGGL((k_bwd_walks_f32<DK, DV>), dim3(n * (DV / 16), both), dim3(256), 0, st, a);
+  else if (chains <= 256)
+    hipLaunchKernelGGL((k_bwd_teams<DK, DV>), dim3(n * (DV / 16), both), dim3(512), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_bwd_lone<DK, DV>), dim3(n * (DV / 64), both), dim3(384), 0, st, a);
   return hipGetLastError();
 }
 
