@@ -35,19 +35,53 @@
 
 namespace gdn {
 
-// ---- every chunk: T, T^T and P^T dO
+// ---- every chunk: T and P^T dO
+// Wave w forms row block w of A and P, each block of A in row form and of P in column
+// form, which is the row form of P^T; then wave 0 inverts I + A while the others
+// form P^T dO, P as terms.  What a thread needs of K, Q and dO is asked for at the start.
 template <int DK, int DV, typename T>
 __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
   typedef typename FragOf<T>::type F;
-  constexpr int LD = BC + 4;
-  __shared__ float sA[BC * LD], sP[BC * LD], sr[5][BC];
+  constexpr int E = 16 / sizeof(T), LDV = DV + E, NQ = DK / 32, CPR = DV / E, ON = BC * CPR / 256;
+  typedef T Vec __attribute__((ext_vector_type(E)));
+  __shared__ __attribute__((aligned(16))) float sA[10 * 256];
+  __shared__ __attribute__((aligned(16))) T sP[6 * TermsOf<F>::N * 512], sO[BC * LDV];
+  __shared__ __attribute__((aligned(16))) float sr[5][BC];
   const uint32_t slot = blockIdx.x / (uint32_t)a.Hv;
   const int h = (int)(blockIdx.x - slot * (uint32_t)a.Hv), hk = h / a.gr;
   int64_t t0 = 0;
   const int m = chunk_at(a, slot, t0);
   if (m == 0) return;
   float* ws = a.ws + (int64_t)blockIdx.x * ws_tile(DK, DV);
-  const int wv = threadIdx.x >> 6, g = lane_g(), c = lane_c();
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Lane ln = lane_here();
+  const int l = ln.id, g = ln.g(), c = ln.c();
+  Pair<F> q[NQ], k[NQ], kj[3][NQ];
+  {
+    const uint32_t ld = (uint32_t)a.Hk * DK;
+    const T* Kp = (const T*)a.K + (t0 * a.Hk + hk) * DK;
+    const T* Qp = (const T*)a.Q + (t0 * a.Hk + hk) * DK;
+    auto rows = [&](Pair<F>(&x)[NQ], const T* p, int I) __attribute__((always_inline)) {
+      const uint32_t at = min(16 * I + c, m - 1) * ld + 8 * g;
+#pragma unroll
+      for (int s = 0; s < NQ; ++s) x[s] = load_row8<F>(p + (at + 32 * s));
+    };
+    rows(k, Kp, wv);
+    rows(q, Qp, wv);
+#pragma unroll
+    for (int J = 0; J < 3; ++J)
+      if (J < wv) rows(kj[J], Kp, J);
+  }
+  Vec o[ON];
+  {
+    const T* dO = (const T*)a.dO + (t0 * a.Hv + h) * DV;
+    const uint32_t ld = (uint32_t)a.Hv * DV;
+#pragma unroll
+    for (int i = 0; i < ON; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      o[i] = *(const Vec*)(dO + (min(at / CPR, m - 1) * ld + at % CPR * E));
+    }
+  }
   if (threadIdx.x < BC) {
     const int r = threadIdx.x, rr = r < m ? r : m - 1;
     const float* gp = a.g + t0 * a.Hv + h;
@@ -67,84 +101,74 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
 #pragma unroll
     for (int k = 0; k < 5; ++k) ws[ws_rows() + k * BC + r] = sr[k][r];
   }
-  __syncthreads();
-  // row block wv of A and P
-  {
-    Pair<F> q[DK / 32], k[DK / 32], kj[DK / 32];
-    const int64_t ld = (int64_t)a.Hk * DK;
-    const T* Kp = (const T*)a.K + (t0 * a.Hk + hk) * DK;
-    const T* Qp = (const T*)a.Q + (t0 * a.Hk + hk) * DK;
-    auto rows = [&](Pair<F>(&x)[DK / 32], const T* p, int I) __attribute__((always_inline)) {
-      const int r = 16 * I + c, rr = r < m ? r : m - 1;
 #pragma unroll
-      for (int s = 0; s < DK / 32; ++s) {
-        x[s] = load_row8<F>(p + rr * ld + 32 * s + 8 * g);
-        if (r >= m) x[s] = Pair<F>::zero();
-      }
-    };
-    rows(q, Qp, wv);
-    rows(k, Kp, wv);
-    for (int J = 0; J <= wv; ++J) {
-      rows(kj, Kp, J);
+  for (int i = 0; i < ON; ++i) {
+    const int at = threadIdx.x + 256 * i;
+    *(Vec*)(sO + at / CPR * LDV + at % CPR * E) = at / CPR < m ? o[i] : Vec{};
+  }
+  __syncthreads();
+  {
+    auto block = [&](const Pair<F>(&x)[NQ], int J) __attribute__((always_inline)) {
       f32x4 kk = zero4(), qk = zero4();
 #pragma unroll
-      for (int s = 0; s < DK / 32; ++s) {
-        kk = Pair<F>::template mma<false>(k[s], kj[s], kk);
-        qk = Pair<F>::template mma<false>(q[s], kj[s], qk);
+      for (int s = 0; s < NQ; ++s) {
+        kk = Pair<F>::template mma<true>(k[s], x[s], kk);
+        qk = Pair<F>::template mma<false>(q[s], x[s], qk);
       }
+      // (rows past the chunk's last repeat it; beta is 0 there, P is masked)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int i = 16 * wv + 4 * g + v, j = 16 * J + c;
-        const float d = i >= j ? __expf((sr[3][i] - sr[3][j]) + (sr[4][i] - sr[4][j])) : 0.f;
-        sA[i * LD + j] = i > j ? -sr[0][i] * kk[v] * d : 0.f;
-        sP[i * LD + j] = i >= j ? a.scale * qk[v] * d : 0.f;
+        const int e = 4 * g + v;
+        const int ia = 16 * wv + c, ja = 16 * J + e, ip = 16 * wv + e, jp = 16 * J + c;
+        const float da = __expf((sr[3][ia] - sr[3][ja]) + (sr[4][ia] - sr[4][ja]));
+        const float dp = __expf((sr[3][ip] - sr[3][jp]) + (sr[4][ip] - sr[4][jp]));
+        kk[v] = ia > ja ? -sr[0][ia] * kk[v] * da : 0.f;
+        qk[v] = ip >= jp && ip < m ? a.scale * qk[v] * dp : 0.f;
       }
-    }
+      *(f32x4*)(sA + bidx(wv, J) * 256 + 4 * l) = kk;
+      store_half<F>(sP, tt_slot(J, wv >> 1), wv & 1, split_half<F>(qk), l);
+    };
+#pragma unroll
+    for (int J = 0; J < 3; ++J)
+      if (J < wv) block(kj[J], J);
+    block(k, wv);
+    if (wv & 1)  // the block before the diagonal that its pair takes along
+      store_half<F>(sP, tt_slot(wv, wv >> 1), 0, split_half<F>(zero4()), l);
   }
   __syncthreads();
   if (wv == 0) {
     Acc<4> Lr, Tr;
 #pragma unroll
-    for (int I = 0; I < 4; ++I)
-#pragma unroll
-      for (int J = 0; J <= I; ++J)
-        Lr.a[bidx(I, J)] = at4(sA + (16 * I + c) * LD + 16 * J + 4 * g);
+    for (int i = 0; i < 10; ++i) Lr.a[i] = at4(sA + 256 * i + 4 * l);
     blockwise_inverse<4, f32x4>(Lr, Tr);
-    const f32x4 z = zero4();
 #pragma unroll
     for (int I = 0; I < 4; ++I)
 #pragma unroll
-      for (int J = 0; J < 4; ++J) {
-        // (sA holds nothing that another wave reads)
-        if (J <= I) *(f32x4*)(sA + (16 * I + c) * LD + 16 * J + 4 * g) = Tr.a[bidx(I, J)];
-        if (J / 2 <= I / 2)
-          store_half<F>((T*)(ws + ws_T() + TS * t_slot(I, J / 2)), 0, J & 1,
-                        split_half<F>(J <= I ? Tr.a[bidx(I, J)] : z), lane_id());
-      }
-    lds_sync<true>();
-#pragma unroll
-    for (int I = 0; I < 4; ++I)
-#pragma unroll
-      for (int J = 0; J < 4; ++J)
-        if (J / 2 >= I / 2)
-          store_half<F>(
-              (T*)(ws + ws_Tt() + TS * tt_slot(I, J / 2)), 0, J & 1,
-              split_half<F>(J >= I ? down4(sA + (16 * J + 4 * g) * LD + 16 * I + c, LD) : z),
-              lane_id());
+      for (int p = 0; p <= I / 2; ++p)
+        store_terms<F>((T*)(ws + ws_T() + TS * t_slot(I, p)),
+                       split<F>(Tr.a[bidx(I, 2 * p)],
+                                2 * p < I ? Tr.a[bidx(I, 2 * p + (2 * p < I))] : zero4()),
+                       l);
   } else {
-    const T* dO = (const T*)a.dO + (t0 * a.Hv + h) * DV;
+    Terms<F> P[6];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) P[i] = load_terms<F>(sP, i, l);
+#pragma unroll 1
     for (int J = wv - 1; J < DV / 16; J += 3) {
-      f32x4 o[4];
+      f32x4 x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = col_block(dO + 16 * J, (int64_t)a.Hv * DV, 16 * k, m);
+      for (int I = 0; I < 4; ++I) x[I] = zero4();
 #pragma unroll
-      for (int I = 0; I < 4; ++I) {
-        f32x4 x = zero4();
+      for (int p = 0; p < 2; ++p) {
+        const Pair<F> y = col_pair<LDV>(sO, 32 * p, 16 * J, ln);
 #pragma unroll
-        for (int k = I; k < 4; ++k)
-          x = mma16(down4(sP + (16 * k + 4 * g) * LD + 16 * I + c, LD), o[k], x);
-        *(f32x4*)(ws + ws_R() + blk_at(I, J, DV / 16) + 4 * lane_id()) = x;
+        for (int t = TermsOf<F>::N - 1; t >= 0; --t)
+#pragma unroll
+          for (int I = 0; I < 4; ++I)
+            if (p >= I / 2) x[I] = Pair<F>::template mma<false>(P[tt_slot(I, p)].t[t], y, x[I]);
       }
+#pragma unroll
+      for (int I = 0; I < 4; ++I) *(f32x4*)(ws + ws_R() + blk_at(I, J, DV / 16) + 4 * l) = x[I];
     }
   }
 }

@@ -14,9 +14,10 @@ namespace gdn {
 
 constexpr int BC = 64;  // tokens a chunk
 
-// Workspace of one (chunk, value head), in floats.  T and T^T lie as the terms
-// (split.hpp) of the pair fragments of their row blocks, 3 KB a fragment (2 KB
-// with fp32 inputs): T (I, p) with 2p <= I, T^T (I, p) with 2p + 1 >= I.
+// Workspace of one (chunk, value head), in floats.  T lies as the terms (split.hpp)
+// of the pair fragments of its row blocks, 3 KB a fragment (2 KB with fp32 inputs):
+// (I, p) with 2p <= I; T^T is read from the same fragments, its pairs (I, p) have
+// 2p + 1 >= I.
 // X, R and dZ lie as column-form blocks, S and dS as row-form blocks (tile16.hpp),
 // the 4 values of a lane side by side: 1 KB a block, read and written whole.
 constexpr int TS = 768;
@@ -24,8 +25,7 @@ __host__ __device__ constexpr int blk_at(int I, int J, int NJ) { return (I * NJ 
 __host__ __device__ constexpr int t_slot(int I, int p) { return (I == 3 ? 4 : I) + p; }
 __host__ __device__ constexpr int tt_slot(int I, int p) { return (I < 2 ? 2 * I : 2 + I) + p - I / 2; }
 __host__ __device__ constexpr int64_t ws_T() { return 0; }
-__host__ __device__ constexpr int64_t ws_Tt() { return 6 * TS; }
-__host__ __device__ constexpr int64_t ws_rows() { return 12 * TS; }  // beta e^g e^{gl-g} g off
+__host__ __device__ constexpr int64_t ws_rows() { return 6 * TS; }  // beta e^g e^{gl-g} g off
 __host__ __device__ constexpr int64_t ws_R() { return ws_rows() + 5 * BC; }  // P^T dO, then dZ
 __host__ __device__ constexpr int64_t ws_X(int dv) { return ws_R() + BC * dv; }
 __host__ __device__ constexpr int64_t ws_S(int dv) { return ws_X(dv) + BC * dv; }

@@ -56,6 +56,17 @@ struct Flow {
     const int r = r0 + 4 * ln.g() + (ln.c() >> 2), k = c0 + 4 * (ln.c() & 3);
     return join(read_transposed(s + at(r, k)), read_transposed(s + at(r + 16, k)));
   }
+  // the pair (I, p) of T^T: the blocks (2p, I) and (2p + 1, I) of T's fragments,
+  // transposed.  Lane l of a slot holds T's row l % 16, columns 4 (l / 16) ...
+  static __device__ __forceinline__ Terms<F> t_rows(const T* s, int I, int p, Lane ln) {
+    const T* at = s + 8 * (16 * (ln.c() & 3) + 4 * ln.g() + (ln.c() >> 2)) + 4 * (I & 1);
+    Terms<F> r;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      r.t[i] = join(read_transposed(slot_at(at, t_slot(2 * p, I >> 1), i, 3)),
+                    read_transposed(slot_at(at, t_slot(2 * p + 1, I >> 1), i, 3)));
+    return r;
+  }
   // column-form block of rows r0 .. and 16 columns c0 .. of the slices' rows of V (dO)
   static __device__ __forceinline__ f32x4 val_block(const T* s, int r0, int c0, Lane ln) {
     const int r = r0 + 4 * ln.g() + (ln.c() >> 2);
@@ -118,7 +129,7 @@ __device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& ld
       T* to = sm[i % R];
       const float* ws = tile(ck);
       load_rows(a.K, ck, to + W::oK);
-      const float* t = ws + (REV ? ws_Tt() : ws_T()) + 4 * l;
+      const float* t = ws + ws_T() + 4 * l;
 #pragma unroll
       for (int k = 0; k < 9; ++k)
         W::copy(to + W::oT + (2 * k + lw) * 512, t + (2 * k + lw) * 256);
@@ -235,7 +246,7 @@ __device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& ld
 #pragma unroll
           for (int I = 0; I < 4; ++I) {
             if (REV ? p < I / 2 : p > I / 2) continue;
-            if (k == 0) ts[I] = load_terms<F>(sT, REV ? tt_slot(I, p) : t_slot(I, p), l);
+            if (k == 0) ts[I] = REV ? W::t_rows(sT, I, p, ln) : load_terms<F>(sT, t_slot(I, p), l);
             f32x4& acc = k & 1 ? u[I] : ul[I];
             acc = Pair<F>::template mma<false>(ts[I].t[tx[k]], zt[p].t[ty[k]], acc);
           }
@@ -401,7 +412,7 @@ __device__ __forceinline__ void team(const BwdArgs& a, typename W::Lds& lds) {
       const int ck = chunk(min(i, nc - 1)), m = rows(ck);
       T* to = sm[i & 1];
       const float* ws = tile(ck);
-      const float* t = ws + (REV ? ws_Tt() : ws_T()) + 4 * l;
+      const float* t = ws + ws_T() + 4 * l;
 #pragma unroll
       for (int k = 0; k < W::TN - 2; ++k) {
         const int n = min(W::LW * k + lw, 17);
@@ -509,7 +520,7 @@ __device__ __forceinline__ void team(const BwdArgs& a, typename W::Lds& lds) {
 #pragma unroll
     for (int p = 0; p < 2; ++p)
       if (REV ? p >= wv / 2 : p <= wv / 2)
-        tt[p] = load_terms<F>(sT, REV ? tt_slot(wv, p) : t_slot(wv, p), l);
+        tt[p] = REV ? W::t_rows(sT, wv, p, ln) : load_terms<F>(sT, t_slot(wv, p), l);
     lds_only_barrier();  // 2
     f32x4 u = zero4(), ul = zero4(), w[2] = {zero4(), zero4()};
     {
@@ -646,7 +657,7 @@ struct Walk {
             (int)threadIdx.x / CPR + 256 / CPR * i < m ? x.v[i] : Vec{};
     }
   }
-  // row block w of T (or T^T): two pairs of terms at most
+  // row block w of T: two pairs at most
   struct TRow {
     Terms<F> v[2];
   };
@@ -654,6 +665,17 @@ struct Walk {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (i < n) x.v[i] = load_terms<F>((const T*)(p + TS * i), 0, l);
+  }
+  // the same of T^T, from T's fragments: the blocks (J, w), J from the pair of w on
+  static __device__ __forceinline__ void fetch_tt(TRow& x, const float* p, int w, Lane ln) {
+    const float* at = p + 256 * (w & 1) + 4 * (16 * (ln.c() >> 2) + 4 * ln.g()) + (ln.c() & 3);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (i < 2 - w / 2) {
+        const int J = 2 * (i + w / 2);
+        x.v[i].t[0] = join(down4(at + TS * t_slot(J, w >> 1), 4),
+                           down4(at + TS * t_slot(J + 1, w >> 1), 4));
+      }
   }
   // this wave's share of the product of the 64 rows in LDS with the state
   static __device__ __forceinline__ void share(const T* sK, const Terms<F>& s, float* part, int wv,
@@ -866,7 +888,7 @@ __device__ __forceinline__ void reverse_f32(const BwdArgs& a, typename Walk<DK, 
   auto fetch = [&](Ops& x, int ck) __attribute__((always_inline)) {
     const float* ws = tile(ck);
     const float* rv = ws + ws_rows();
-    W::fetch_t(x.t, ws + ws_Tt() + TS * tt_slot(wv, wv / 2), 2 - wv / 2, l);
+    W::fetch_tt(x.t, ws + ws_T(), wv, ln);
     x.r = at4(ws + ws_R() + blk_at(wv, n0 / 16, W::NS) + 4 * l);
     x.o = W::fetch_col((const T*)a.dO + vat(ck), voff, (rows(ck) - 1) * (uint32_t)vld * sizeof(T));
     x.beta = at4(rv + r0);
