@@ -37,12 +37,39 @@ namespace gdn {
 
 // ---- every chunk: T and P^T dO
 // Wave w forms row block w of A and P, each block of A in row form and of P in column
-// form, which is the row form of P^T; then wave 0 inverts I + A while the others
-// form P^T dO, P as terms.  What a thread needs of K, Q and dO is asked for at the start.
+// form, which is the row form of P^T, and inverts its own diagonal block; then it has
+// block column w of T, and its part of the columns of P^T dO, P as terms.  What a
+// thread needs of K, Q and dO is asked for at the start.
+
+// X = (I - L)^-1 of a strictly lower 16 x 16 block, lr its row form, in both forms: with
+// O_k the entries of L that join two blocks of size 2^k into one of size 2^(k+1),
+// X_1 = I + O_0 and X_{k+1} = X_k + X_k O_k X_k, exact since O_k X_k O_k = 0.
+__device__ __forceinline__ void inverse16(const f32x4& lr, f32x4& xr, f32x4& xc, Lane ln) {
+  const int g = ln.g(), c = ln.c();
+  const f32x4 lc = mma16(lr, eye4(ln), zero4());
+  xr = xc = eye4(ln);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    if (in_level(c, 4 * g + v, 0)) xr[v] += lr[v];
+    if (in_level(4 * g + v, c, 0)) xc[v] += lc[v];
+  }
+#pragma unroll
+  for (int k = 1; k < 4; ++k) {
+    f32x4 oc;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) oc[v] = in_level(4 * g + v, c, k) ? lc[v] : 0.f;
+    const f32x4 t = mma16(oc, xr, zero4());  // X_k O_k, row form
+    const f32x4 n = mma16(t, xc, xc);
+    xr = mma16(xc, t, xr);
+    xc = n;
+  }
+}
+
 template <int DK, int DV, typename T>
 __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
   typedef typename FragOf<T>::type F;
   constexpr int E = 16 / sizeof(T), LDV = DV + E, NQ = DK / 32, CPR = DV / E, ON = BC * CPR / 256;
+  constexpr int NJ = DV / 16, TW = TS * 4 / sizeof(T);  // TW: values of T a slot of T
   typedef T Vec __attribute__((ext_vector_type(E)));
   __shared__ __attribute__((aligned(16))) float sA[10 * 256];
   __shared__ __attribute__((aligned(16))) T sP[6 * TermsOf<F>::N * 512], sO[BC * LDV];
@@ -107,6 +134,7 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
     *(Vec*)(sO + at / CPR * LDV + at % CPR * E) = at / CPR < m ? o[i] : Vec{};
   }
   __syncthreads();
+  f32x4 xc;  // the inverse of this wave's diagonal block, column form
   {
     auto block = [&](const Pair<F>(&x)[NQ], int J) __attribute__((always_inline)) {
       f32x4 kk = zero4(), qk = zero4();
@@ -125,36 +153,47 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
         kk[v] = ia > ja ? -sr[0][ia] * kk[v] * da : 0.f;
         qk[v] = ip >= jp && ip < m ? a.scale * qk[v] * dp : 0.f;
       }
-      *(f32x4*)(sA + bidx(wv, J) * 256 + 4 * l) = kk;
       store_half<F>(sP, tt_slot(J, wv >> 1), wv & 1, split_half<F>(qk), l);
+      return kk;
     };
 #pragma unroll
     for (int J = 0; J < 3; ++J)
-      if (J < wv) block(kj[J], J);
-    block(k, wv);
-    if (wv & 1)  // the block before the diagonal that its pair takes along
+      if (J < wv) *(f32x4*)(sA + bidx(wv, J) * 256 + 4 * l) = block(kj[J], J);
+    f32x4 xr;
+    inverse16(block(k, wv), xr, xc, ln);
+    *(f32x4*)(sA + bidx(wv, wv) * 256 + 4 * l) = xr;
+    T* const Tw = (T*)(ws + ws_T());
+    store_half<F>(Tw + TW * t_slot(wv, wv >> 1), 0, wv & 1, split_half<F>(xr), l);
+    if (wv & 1) {  // the blocks beside the diagonal that their pairs take along: zeros
+      store_half<F>(Tw + TW * t_slot(wv - 1, wv >> 1), 0, 1, split_half<F>(zero4()), l);
       store_half<F>(sP, tt_slot(wv, wv >> 1), 0, split_half<F>(zero4()), l);
+    }
   }
   __syncthreads();
-  if (wv == 0) {
-    Acc<4> Lr, Tr;
+  {
+    // X_IJ = X_II sum_{K = J}^{I - 1} L_IK X_KJ, J = w, rows in order
+    f32x4 X[4] = {xc, zero4(), zero4(), zero4()};  // X_{w + d, w}, column form
 #pragma unroll
-    for (int i = 0; i < 10; ++i) Lr.a[i] = at4(sA + 256 * i + 4 * l);
-    blockwise_inverse<4, f32x4>(Lr, Tr);
+    for (int d = 1; d < 4; ++d) {
+      const int I = wv + d;
+      if (I > 3) continue;
+      f32x4 x = zero4();
 #pragma unroll
-    for (int I = 0; I < 4; ++I)
-#pragma unroll
-      for (int p = 0; p <= I / 2; ++p)
-        store_terms<F>((T*)(ws + ws_T() + TS * t_slot(I, p)),
-                       split<F>(Tr.a[bidx(I, 2 * p)],
-                                2 * p < I ? Tr.a[bidx(I, 2 * p + (2 * p < I))] : zero4()),
-                       l);
-  } else {
+      for (int e = 0; e < d; ++e) x = mma16(at4(sA + bidx(I, wv + e) * 256 + 4 * l), X[e], x);
+      const f32x4 xi = at4(sA + bidx(I, I) * 256 + 4 * l);
+      X[d] = mma16(xi, x, zero4());
+      store_half<F>((T*)(ws + ws_T()) + TW * t_slot(I, wv >> 1), 0, wv & 1,
+                    split_half<F>(mma16(x, xi, zero4())), l);
+    }
+  }
+  {
     Terms<F> P[6];
 #pragma unroll
     for (int i = 0; i < 6; ++i) P[i] = load_terms<F>(sP, i, l);
+    // wave 3 has had no products of T, wave 0 the most
+    const int J1 = (wv + 1) * (NJ / 4) - (wv < 3);
 #pragma unroll 1
-    for (int J = wv - 1; J < DV / 16; J += 3) {
+    for (int J = wv * (NJ / 4) - (wv > 0); J < J1; ++J) {
       f32x4 x[4];
 #pragma unroll
       for (int I = 0; I < 4; ++I) x[I] = zero4();
@@ -168,7 +207,7 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
             if (p >= I / 2) x[I] = Pair<F>::template mma<false>(P[tt_slot(I, p)].t[t], y, x[I]);
       }
 #pragma unroll
-      for (int I = 0; I < 4; ++I) *(f32x4*)(ws + ws_R() + blk_at(I, J, DV / 16) + 4 * l) = x[I];
+      for (int I = 0; I < 4; ++I) *(f32x4*)(ws + ws_R() + blk_at(I, J, NJ) + 4 * l) = x[I];
     }
   }
 }

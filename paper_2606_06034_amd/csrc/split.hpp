@@ -147,20 +147,6 @@ __device__ __forceinline__ Terms<F> load_terms(const T* s, int pair, int l) {
   }
   return r;
 }
-// one pair and its terms in slots of their own, in memory
-template <typename F, typename T>
-__device__ __forceinline__ void store_terms(T* s, const Terms<F>& x, int l) {
-#pragma unroll
-  for (int i = 0; i < TermsOf<F>::N; ++i) {
-    if constexpr (TermsOf<F>::N == 1) {
-      *(f32x4*)(s + 4 * l) = x.t[i].a;
-      *(f32x4*)(s + 256 + 4 * l) = x.t[i].b;
-    } else {
-      *(bf16x8*)(s + 512 * i + 8 * l) = x.t[i].v;
-    }
-  }
-}
-
 // Rows of an input in LDS, LD values apart: a pair along a row (slot s of lane
 // (g, c): column c0 + 16 (s / 4) + 4g + s % 4 of row r0 + c) and one down the
 // rows (row r0 + 16 (s / 4) + 4g + s % 4 of column c0 + c).  In bf16 the second
