@@ -75,14 +75,6 @@ __device__ __forceinline__ f32x4 mma_in(const Pair<F>& x, const Terms<F>& y, f32
     acc = Pair<F>::template mma<OUTQ>(x, y.t[i], acc);
   return acc;
 }
-// acc += x y, the input y exact
-template <bool OUTQ, typename F>
-__device__ __forceinline__ f32x4 mma_in(const Terms<F>& x, const Pair<F>& y, f32x4 acc) {
-#pragma unroll
-  for (int i = TermsOf<F>::N - 1; i >= 0; --i)
-    acc = Pair<F>::template mma<OUTQ>(x.t[i], y, acc);
-  return acc;
-}
 // the same for N left operands and one right one, term after term, so that
 // neighbouring instructions do not wait for each other
 template <bool OUTQ, int N, typename F>
@@ -92,17 +84,8 @@ __device__ __forceinline__ void mma_in(const Pair<F> (&x)[N], const Terms<F>& y,
 #pragma unroll
     for (int n = 0; n < N; ++n) acc[n] = Pair<F>::template mma<OUTQ>(x[n], y.t[i], acc[n]);
 }
-// acc += x y of two fp32 values
-template <bool OUTQ, typename F>
-__device__ __forceinline__ f32x4 mma_both(const Terms<F>& x, const Terms<F>& y, f32x4 acc) {
-#pragma unroll
-  for (int s = TermsOf<F>::N - 1; s >= 0; --s)
-#pragma unroll
-    for (int i = 0; i <= s; ++i) acc = Pair<F>::template mma<OUTQ>(x.t[i], y.t[s - i], acc);
-  return acc;
-}
-// the same in two sums, one of the terms below the largest, so that half as many
-// instructions wait for each other
+// acc += x y of two fp32 values, in two sums, one of the terms below the largest, so
+// that half as many instructions wait for each other
 template <bool OUTQ, typename F>
 __device__ __forceinline__ void mma_both(const Terms<F>& x, const Terms<F>& y, f32x4& acc,
                                          f32x4& low) {
@@ -152,11 +135,6 @@ __device__ __forceinline__ Terms<F> load_terms(const T* s, int pair, int l) {
 // rows (row r0 + 16 (s / 4) + 4g + s % 4 of column c0 + c).  In bf16 the second
 // is two of the transposing LDS reads: 16 lanes read a 4 x 16 block, lane i the
 // four values at row i / 4, columns 4 (i % 4), and lane c receives column c.
-template <int LD>
-__device__ __forceinline__ Pair<bf16x4> row_pair(const __bf16* s, int r0, int c0, Lane ln) {
-  const __bf16* p = s + (r0 + ln.c()) * LD + c0 + 4 * ln.g();
-  return join(*(const bf16x4*)p, *(const bf16x4*)(p + 16));
-}
 template <int LD>
 __device__ __forceinline__ Pair<f32x4> row_pair(const float* s, int r0, int c0, Lane ln) {
   const float* p = s + (r0 + ln.c()) * LD + c0 + 4 * ln.g();
