@@ -73,7 +73,8 @@ int gdn_chunk_backward_workspace(int nseq, int L, int Hv, int dk, int dv, int pa
   if (!bytes) return GDN_ERR_NULL;
   if (nseq < 0 || L < 0 || Hv < 0 || !valid_d(dk) || !valid_d(dv)) return GDN_ERR_SHAPE;
   const int64_t slots = L > 0 && nseq > 0 ? gdn::backward_slots(nseq, L, packed != 0) : 0;
-  if (Hv > 0 && (!grid_ok(slots, 256) || !grid_ok(slots * Hv, 256))) return GDN_ERR_SHAPE;
+  // (the per-chunk launches' workgroups have 512 work items at most)
+  if (Hv > 0 && (!grid_ok(slots, 512) || !grid_ok(slots * Hv, 512))) return GDN_ERR_SHAPE;
   *bytes = slots * Hv * gdn::backward_tile_bytes(dk, dv);
   return GDN_OK;
 }
@@ -88,7 +89,7 @@ int backward(const void* Q, const void* K, const void* V, const float* beta, con
   if (!(C == 16 || C == 32 || C == 64)) return C == 128 ? GDN_ERR_UNSUPPORTED : GDN_ERR_SHAPE;
   int64_t need = 0;
   if (int r = gdn_chunk_backward_workspace(nseq, L, Hv, dk, dv, packed, &need)) return r;
-  if (!grid_ok((int64_t)nseq * Hv * (dv / 16), 256)) return GDN_ERR_SHAPE;
+  if (!grid_ok(((int64_t)nseq * Hv + 7) / 8 * 8 * (dv / 16), 512)) return GDN_ERR_SHAPE;
   if (!fdtype(dtype)) return GDN_ERR_DTYPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
   if (packed && !cu) return GDN_ERR_NULL;

@@ -609,10 +609,8 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
           store4(dKp + to, sk);
         }
       }
-      dotF += __shfl_xor(dotF, 16);
-      dotG += __shfl_xor(dotG, 16);
-      dotF += __shfl_xor(dotF, 32);
-      dotG += __shfl_xor(dotG, 32);
+      dotF = sum_apart32(sum_apart16(dotF));
+      dotG = sum_apart32(sum_apart16(dotG));
       if (g == 0) {
         red[0][wv % G::NC][r] = dotF;
         red[1][wv % G::NC][r] = dotG;
@@ -620,9 +618,7 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
     }
     // (every row group has formed the same <S, dS> of its columns)
     if (I0 == 0) end = __builtin_fmaf(sr[1][BC - 1], ss, end);
-    end = sum16(end);
-    end += __shfl_xor(end, 16);
-    end += __shfl_xor(end, 32);
+    end = sum_lanes<64>(end);
     if (l == 0) send[wv] = end;
     __syncthreads();
     if (tid < BC) {

@@ -15,6 +15,7 @@
 //
 // Bound: the state is read and written once a call, 8 bytes for 7 flops a
 // token, so a call is HBM traffic up to tens of tokens.
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "layer.hpp"
 #include "tile16.hpp"
@@ -52,10 +53,7 @@ __device__ __forceinline__ void store_4(__bf16* p, f32x4 x) {
 
 // sum over the 8 row groups (lanes 8, 16, 32 apart); every lane gets it
 __device__ __forceinline__ float sum_groups(float x) {
-  x += __shfl_xor(x, 8);
-  x += __shfl_xor(x, 16);
-  x += __shfl_xor(x, 32);
-  return x;
+  return sum_apart32(sum_apart16(sum_apart8(x)));
 }
 
 }  // namespace
@@ -66,13 +64,14 @@ __global__ __launch_bounds__(256) void k_recurrent(
     const TIO* __restrict__ Q, const TIO* __restrict__ K, const TIO* __restrict__ V,
     const float* __restrict__ beta, const float* __restrict__ g, const float* S0, TIO* __restrict__ O,
     float* Sfin, const int* __restrict__ slots, int n_states, const int* __restrict__ cu,
-    int64_t waves, int T, int Hk, int Hv, float scale) {
+    uint32_t waves, int T, int Hk, int Hv, float scale) {
   constexpr int NR = DK / 8, NC = DV / 32;
-  const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
+  const uint32_t w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (w >= waves) return;
   const int l = lane_id(), r0 = (l >> 3) * NR;
-  const int64_t sh = w / NC;
-  const int s = (int)(sh / Hv), h = (int)(sh - (int64_t)s * Hv), hk = h / (Hv / Hk);
+  const uint32_t sh = w / NC;
+  const int s = (int)(sh / (uint32_t)Hv), h = (int)(sh - (uint32_t)s * (uint32_t)Hv);
+  const int hk = h / (Hv / Hk);
   const int col = (int)(w - sh * NC) * 32 + 4 * (l & 7);
   int64_t t0 = (int64_t)s * T, n = T;
   if (cu) {
@@ -150,16 +149,16 @@ hipError_t launch_recurrent(const void* Q, const void* K, const void* V, const f
                             const int* slots, int n_states, const int* cu, int nseq, int T, int Hk,
                             int Hv, int dk, int dv, float scale, int dtype, hipStream_t st) {
   const int64_t waves = (int64_t)nseq * Hv * (dv / 32);
-  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);  // (checked to fit the grid)
   GDN_DK_SWITCH(dk, GDN_DV_SWITCH(dv, {
     if (dtype == 0)
       hipLaunchKernelGGL((k_recurrent<DK, DV, float>), grid, block, 0, st, (const float*)Q,
                          (const float*)K, (const float*)V, beta, g, S0, (float*)O, Sfin, slots,
-                         n_states, cu, waves, T, Hk, Hv, scale);
+                         n_states, cu, (uint32_t)waves, T, Hk, Hv, scale);
     else
       hipLaunchKernelGGL((k_recurrent<DK, DV, __bf16>), grid, block, 0, st, (const __bf16*)Q,
                          (const __bf16*)K, (const __bf16*)V, beta, g, S0, (__bf16*)O, Sfin, slots,
-                         n_states, cu, waves, T, Hk, Hv, scale);
+                         n_states, cu, (uint32_t)waves, T, Hk, Hv, scale);
     return hipGetLastError();
   }))
   return hipErrorNotSupported;

@@ -125,7 +125,7 @@ def test_packed_backward_refusals(change, code):
 
 
 def test_backward_workspace():
-    tile = 4 * (12 * 768 + 5 * 64 + 2 * 64 * 128 + 2 * 128 * 128)
+    tile = 4 * (6 * 768 + 5 * 64 + 2 * 64 * 128 + 2 * 128 * 128)
     assert G.gdn_chunk_backward_workspace(2, 100, 3, 128, 128) == 2 * 2 * 3 * tile
     assert G.gdn_chunk_backward_workspace(5, 100, 3, 128, 128, packed=True) == (1 + 5) * 3 * tile
     assert G.gdn_chunk_backward_workspace(2, 0, 3, 128, 128) == 0
