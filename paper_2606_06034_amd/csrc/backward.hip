@@ -42,7 +42,7 @@ namespace gdn {
 // thread needs of K, Q and dO is asked for at the start.
 // (With T left to wave 0 and P^T dO in fp32 instructions the others waited for it: 79 us
 // for 8192 tokens of 16 heads, 128 by 128 in bf16; now 50.  At 4 x 8192 tokens of 32
-// value heads 330 us, 98 KB a chunk and head at 4.9 TB/s: HBM bounds it.)
+// value heads 324 us for 1.76 GB, 5.4 TB/s: HBM bounds it.)
 
 // X = (I - L)^-1 of a strictly lower 16 x 16 block, lr its row form, in both forms: with
 // O_k the entries of L that join two blocks of size 2^k into one of size 2^(k+1),

@@ -13,8 +13,11 @@
 // load of the wave covers whole 128-byte lines of 8 rows, and the sums over
 // the rows end in three exchanges between lanes.
 //
-// Bound: the state is read and written once a call, 8 bytes for 7 flops a
-// token, so a call is HBM traffic up to tens of tokens.
+// Bound: the state is read and written once a call, 8 bytes for 7 flops a token.
+// One token is HBM traffic: 256 sequences of 32 heads of 128 by 128, 1.08 GB, take
+// 199 us, 5.4 TB/s.  A further token is 350 vector instructions of a wave: 48
+// sequences of 1 to 8 tokens, 21 heads of 128 by 64 (two waves a SIMD), 68 MB, take
+// 19 us, of which the tokens are 9.
 #include "lanes.hpp"
 #include "launch.hpp"
 #include "layer.hpp"

@@ -6,7 +6,8 @@
 // Bound: a chunk's step is a chain of three dependent products, K S, T Z and K^T Y
 // (K dS, T^T dY and K^T dX), a hundred kilobytes of operands apart from the next,
 // in the one wave or two that own the slice's state; past as many slices as SIMDs,
-// HBM (the states themselves: 64 KB a chunk).
+// HBM (the states themselves: 64 KB a chunk): 4 x 8192 tokens of 32 heads of 128 by
+// 128 in bf16 take 1.29 ms and move 6 GB, 4.7 TB/s.
 #include "backward.hpp"
 
 namespace gdn {
