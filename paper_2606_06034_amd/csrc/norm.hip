@@ -286,7 +286,7 @@ struct GradPiece {
   }
 };
 
-// A row's pieces as they lie in memory, asked for a row ahead.
+// A row's pieces as they lie in memory, asked for two rows ahead.
 template <typename T, int NV, bool GATE>
 struct RawRow {
   decltype(Piece<T>::v) x[NV], dy[NV], z[GATE ? NV : 1];
@@ -331,10 +331,7 @@ __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
     x.mean = a.rms ? 0.f : a.mean_in[row];
     x.rstd = a.rstd_in[row];
   };
-  Row cur, nx;
-  fetch(cur, (int64_t)blockIdx.x * RPB + r);
-  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += step) {
-    fetch(nx, row0 + step + r);
+  auto rows = [&](const Row& cur, int64_t row0) __attribute__((always_inline)) {
     const bool live = row0 + r < a.rows;
     const int64_t at = (live ? row0 + r : a.rows - 1) * D;
     // dn (dy without a gate) and dz, then the row's two sums
@@ -378,7 +375,19 @@ __global__ __launch_bounds__(B) void k_norm_grad(const NormArgs a, int want) {
         store_piece<T>((T*)a.out + at, dx, (t + k * TPR) * E, D);
       }
     }
-    cur = nx;
+  };
+  // two sets in turn, each asked for again when it has been used: copied from one to the
+  // other they were waited for before the next ones were asked for
+  Row r0, r1;
+  int64_t row0 = (int64_t)blockIdx.x * RPB;
+  fetch(r0, row0 + r);
+  fetch(r1, row0 + step + r);
+  for (; row0 < a.rows; row0 += 2 * step) {
+    rows(r0, row0);
+    fetch(r0, row0 + 2 * step + r);
+    if (row0 + step >= a.rows) break;
+    rows(r1, row0 + step);
+    fetch(r1, row0 + 3 * step + r);
   }
   if (!want) return;
   // the sums of the rows that ran side by side: within a wave by exchange,
