@@ -215,6 +215,15 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
   }
 }
 
+// dg of row r from gamma's gradient: the last g of a part of C tokens is in the gamma of
+// every later row
+__device__ __forceinline__ float part_sum(const float* dgamma, int r, int m, int C) {
+  float dg = dgamma[r];
+  if (C < BC && r % C == C - 1)
+    for (int i = r + 1; i < m; ++i) dg += dgamma[i];
+  return dg;
+}
+
 // ---- every chunk: dQ, dK, dbeta, dg; the value heads of a key head in turn
 // Eight waves.  Wave w has the 32 feature columns 32 (w % (DK / 32)) of dQ and dK
 // for NR row blocks of the chunk.  dO, dZ and Y lie in LDS as pair fragments along
@@ -222,12 +231,10 @@ __global__ __launch_bounds__(256) void k_bwd_prep(const BwdArgs a) {
 // one); S and dS come from memory as right operands, each value split into
 // terms by the waves that use it.  The blocks of dP and E wait in registers until the
 // products with the states are done, and then take the place of dO and dZ.
-// Bound: the instructions of two waves a SIMD (a workgroup fills a CU's LDS), some 3000
-// vector and 800 matrix ones a chunk and wave, 45000 cycles; they are in the same phase, so
-// one's vector work hides little of the other's matrix work.  8192 tokens of 16 heads of
-// 128 by 128 in bf16 take 200 us, 290 KB a chunk and head at 3 TB/s.  (Asking for the
-// next chunk's operands a chunk ahead, and the two waves at different priorities, changed
-// nothing.)
+// Bound: the instructions of two waves a SIMD (a workgroup fills a CU's LDS), which are in
+// the same phase, so that one's vector work hides little of the other's matrix work:
+// 45000 cycles a chunk, 20 us.  (Asking for the next chunk's operands a chunk ahead, and
+// the two waves at different priorities, changed nothing.)
 template <int DK, int DV, typename T>
 struct Grads {
   typedef typename FragOf<T>::type F;
@@ -638,14 +645,401 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
       if (r < m) a.dbeta[(t0 + r) * a.Hv + h] = db;
     }
     __syncthreads();
-    if (tid < m) {
-      const int r = tid;
-      float dg = sdg[r];
-      // the last g of a part of C tokens is in the gamma of every later row
-      if (a.C < BC && r % a.C == a.C - 1)
-        for (int i = r + 1; i < m; ++i) dg += sdg[i];
-      a.dg[(t0 + r) * a.Hv + h] = dg;
+    if (tid < m) a.dg[(t0 + tid) * a.Hv + h] = part_sum(sdg, tid, m, a.C);
+  }
+}
+
+// The same with four waves and half the LDS, for more chunks than CUs: two workgroups
+// share a CU, each in its own phase, so that one's matrix work runs beside the other's
+// vector work and loads.  The value columns are taken 64 at a time; P and E take the
+// place of what they were formed from one after the other.  The states' terms are those
+// of S, then those of dS: both at once, or the next pair's states asked for ahead, went
+// to scratch (168 us became 185 and more).
+// Bound: vector instructions (36% of the cycles), matrix instructions (27%), LDS (27%) of
+// two waves a SIMD, and their waits for memory.  8192 tokens of 16 heads of 128 by 128 in
+// bf16 take 168 us, 290 KB a chunk and head at 3.5 TB/s; 4 x 8192 of 32 value heads 1.45 ms.
+template <int DK, int DV>
+struct Halves {
+  static constexpr int NC = DK / 32, RG = 4 / NC, NR = 4 / RG, LDK = DK + 8;
+  // LDS, in bf16 values: T, and dO, dZ and Y of 64 value columns; later P or E along its
+  // rows and down them, the rows of K and Q, and a block a wave to transpose by
+  static constexpr int oT = 0, oO = 18 * 512, oZ = oO + 8 * 512, oY = oZ + 24 * 512;
+  static constexpr int oEnd = oY + 24 * 512;
+  static constexpr int oR = 0, oC = 18 * 512, oK = 36 * 512, oQ = oK + BC * LDK;
+  static constexpr int oTr = oQ + BC * LDK, oEnd2 = oTr + 4 * 512;
+  static constexpr int SIZE = oEnd2 > oEnd ? oEnd2 : oEnd;
+};
+
+template <int DK, int DV>
+__global__ __launch_bounds__(256, 2) void k_bwd_grads_half(const BwdArgs a) {
+  typedef Halves<DK, DV> G;
+  typedef __bf16 T;
+  typedef bf16x4 F;
+  typedef bf16x8 Vec;
+  constexpr int NR = G::NR, LDK = G::LDK, NJ = DV / 16;
+  __shared__ __attribute__((aligned(16))) T sm[G::SIZE];
+  __shared__ __attribute__((aligned(16))) float sr[5][BC];
+  __shared__ float sdb[NJ][BC], red[2][G::NC][BC], sdg[BC], send[4];
+  const uint32_t slot = blockIdx.x / (uint32_t)a.Hk;
+  const int hk = (int)(blockIdx.x - slot * (uint32_t)a.Hk), gr = a.gr;
+  int64_t t0 = 0;
+  const int m = chunk_at(a, slot, t0);
+  if (m == 0) return;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = 32 * (wv % G::NC), I0 = G::RG == 1 ? 0 : wv / G::NC * NR;
+  const int64_t kat = (t0 * a.Hk + hk) * DK;
+  const uint32_t kld = (uint32_t)a.Hk * DK, vld = (uint32_t)a.Hv * DV;
+
+  for (int h = hk * gr; h < (hk + 1) * gr; ++h) {
+    int tid = threadIdx.x;  // (a value of its own in every turn, as above)
+    asm volatile("" : "+v"(tid));
+    const Lane ln{tid & 63};
+    const int l = ln.id, g = ln.g(), c = ln.c();
+    float* ws = a.ws + ((int64_t)slot * a.Hv + h) * ws_tile(DK, DV);
+    // a 16 x 16 block from column form to row form: row 4g + v lies at 4v + g
+    auto turn_in = [&](float* t, const f32x4& x) __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) t[(4 * v + g) * 16 + c] = x[v];
+    };
+    auto turn_out = [&](const float* t) __attribute__((always_inline)) {
+      return at4(t + (4 * (c & 3) + (c >> 2)) * 16 + 4 * g);
+    };
+    // the blocks of dP (kind 0) and E (1) of this wave: an E costs as much as two of dP
+    struct Blk {
+      int kind, I, J;
+    };
+    Blk bk[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      const int e = wv < 2 ? 3 : 2;  // this wave's blocks of E come first
+      const int n = wv < 2 ? (i < 3 ? 3 * wv + i : 2 * wv + i - 3)
+                           : (i < 2 ? 2 + 2 * wv + i : 3 * wv + i - 4);
+      const int I = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
+      bk[i] = Blk{i < e, I, n - I * (I + 1) / 2};
     }
+    f32x4 pe[5], dq[2][NR], zs[2][NR], yd[2][NR];
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) pe[i] = zero4();
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < NR; ++i) dq[b][i] = zs[b][i] = yd[b][i] = zero4();
+
+#pragma unroll 1
+    for (int vh = 0; vh < DV / 64; ++vh) {
+      const int J = 4 * vh + wv;
+      if (vh) __syncthreads();  // the last columns' operands have been used
+      Terms<F> z[2];
+      {
+        f32x4 xb[4], zb[4], bt[4];
+#pragma unroll
+        for (int I = 0; I < 4; ++I) {
+          xb[I] = at4(ws + ws_X(DV) + blk_at(I, J, NJ) + 4 * l);
+          zb[I] = at4(ws + ws_R() + blk_at(I, J, NJ) + 4 * l);
+          bt[I] = at4(ws + ws_rows() + 16 * I + 4 * g);
+        }
+        const T* dO = (const T*)a.dO + (t0 * a.Hv + h) * DV + 64 * vh;
+        F o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = tid + 256 * i;
+          o[i] = *(const F*)(dO + ((uint32_t)min(at >> 4, m - 1) * vld + (uint32_t)(4 * (at & 15))));
+        }
+        if (vh == 0) {
+#pragma unroll
+          for (int i = 0; i < 5; ++i) {
+            const int at = tid + 256 * i, sl = at / 192;  // 192 pieces of 16 bytes a slot
+            if (at < 6 * 192)
+              *(Vec*)(sm + G::oT + at * 8) =
+                  *(const Vec*)((const T*)(ws + ws_T() + TS * sl) + (at - 192 * sl) * 8);
+          }
+          for (int i = tid; i < 5 * BC; i += 256) (&sr[0][0])[i] = ws[ws_rows() + i];
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          z[p] = split<F>(bt[2 * p] * xb[2 * p], bt[2 * p + 1] * xb[2 * p + 1]);
+        float* t = (float*)(sm + G::oY) + 1024 * wv;  // (Y is not there yet)
+#pragma unroll
+        for (int I = 0; I < 4; ++I) {
+          turn_in(t + 256 * I, zb[I]);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float d = sum16(xb[I][v] * zb[I][v]);
+            if (c == 0) sdb[J][16 * I + 4 * g + v] = d;
+          }
+        }
+        lds_sync<true>();
+#pragma unroll
+        for (int I = 0; I < 4; ++I)
+          store_half<F>(sm + G::oZ, 2 * I + (wv >> 1), wv & 1,
+                        split_half<F>(turn_out(t + 256 * I)), l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = tid + 256 * i, r = at >> 4, e = at & 15;
+          *(F*)(sm + G::oO + ((r >> 4) * 2 + (e >> 3)) * 512 + 8 * (16 * (e & 3) + (r & 15)) +
+                4 * ((e >> 2) & 1)) = r < m ? o[i] : F{};
+        }
+      }
+      __syncthreads();
+      // ---- Y = T Z, column block J
+      {
+        f32x4 y[4], yl[4];
+#pragma unroll
+        for (int I = 0; I < 4; ++I) y[I] = yl[I] = zero4();
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int I = 2 * p; I < 4; ++I)
+            mma_both<true>(load_terms<F>(sm + G::oT, t_slot(I, p), l), z[p], y[I], yl[I]);
+#pragma unroll
+        for (int I = 0; I < 4; ++I)
+          store_half<F>(sm + G::oY, 2 * I + (wv >> 1), wv & 1, split_half<F>(y[I] + yl[I]), l);
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int p = 0; p < 2; ++p) {
+        // S and dS, then dP and E while they are on their way
+        const int at = blk_at(col / 16, 4 * vh + 2 * p, NJ) + 4 * l;
+        const float *S = ws + ws_S(DV) + at, *dS = ws + ws_dS(DK, DV) + at;
+        f32x4 s_[2][2], d_[2][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            s_[b][hf] = at4(S + blk_at(b, hf, NJ));
+            d_[b][hf] = at4(dS + blk_at(b, hf, NJ));
+          }
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+          const Terms<F> y = load_terms<F>(sm + G::oY, 2 * bk[i].J + p, l);
+          const int at = 2 * bk[i].I + p;
+          if (i < 2 || (i == 2 && wv < 2)) {
+            f32x4 low = zero4();
+            mma_both<false>(load_terms<F>(sm + G::oZ, at, l), y, pe[i], low);
+            pe[i] += low;
+          } else {
+            pe[i] = mma_in<false>(slot_load<F>(sm + G::oO + at * 512, l), y, pe[i]);
+          }
+        }
+        // ---- dO S^T, dZ S^T, Y dS^T and <S, dS>; one state's terms at a time
+        constexpr int tx[6] = {0, 1, 2, 1, 0, 0}, ty[6] = {2, 1, 0, 0, 1, 0};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) ss = __builtin_fmaf(s_[b][hf][v], d_[b][hf][v], ss);
+        {
+          const Terms<F> sv[2] = {split<F>(s_[0][0], s_[0][1]), split<F>(s_[1][0], s_[1][1])};
+#pragma unroll
+          for (int i = 0; i < NR; ++i) {
+            const int at = 2 * (I0 + i) + p;
+            const Pair<F> o = slot_load<F>(sm + G::oO + at * 512, l);
+            const Terms<F> z = load_terms<F>(sm + G::oZ, at, l);
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+#pragma unroll
+              for (int b = 0; b < 2; ++b) {
+                zs[b][i] = Pair<F>::template mma<true>(z.t[tx[k]], sv[b].t[ty[k]], zs[b][i]);
+                if (k >= 3) dq[b][i] = Pair<F>::template mma<true>(o, sv[b].t[5 - k], dq[b][i]);
+              }
+          }
+        }
+        {
+          const Terms<F> dv[2] = {split<F>(d_[0][0], d_[0][1]), split<F>(d_[1][0], d_[1][1])};
+#pragma unroll
+          for (int i = 0; i < NR; ++i) {
+            const Terms<F> y = load_terms<F>(sm + G::oY, 2 * (I0 + i) + p, l);
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                yd[b][i] = Pair<F>::template mma<true>(y.t[tx[k]], dv[b].t[ty[k]], yd[b][i]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      const int r0 = 16 * bk[i].I + 4 * g, j = 16 * bk[i].J + c;
+      const float s = bk[i].kind ? -1.f : a.scale;
+      const int lo = bk[i].kind ? j + 1 : j;  // the first row that has this column
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float d = __expf((sr[3][r0 + v] - sr[3][j]) + (sr[4][r0 + v] - sr[4][j]));
+        pe[i][v] = r0 + v >= lo ? s * d * pe[i][v] : 0.f;
+      }
+    }
+    constexpr int CPR = DK / 8, KN = BC * CPR / 256;
+    Vec kv[KN], qv[KN];
+#pragma unroll
+    for (int i = 0; i < KN; ++i) {
+      const int at = tid + 256 * i;
+      const uint32_t from = (uint32_t)min(at / CPR, m - 1) * kld + (uint32_t)(at % CPR * 8);
+      kv[i] = *(const Vec*)((const T*)a.K + kat + from);
+      qv[i] = *(const Vec*)((const T*)a.Q + kat + from);
+    }
+    // the blocks of one kind as left operands: along their rows, and down them (E with beta)
+    auto lay = [&](int kind) __attribute__((always_inline)) {
+      float* t = (float*)(sm + G::oTr) + 256 * wv;
+#pragma unroll
+      for (int i = 0; i < 5; ++i) {
+        if (bk[i].kind != kind) continue;
+        const int I = bk[i].I, J = bk[i].J;
+        turn_in(t, pe[i]);
+        lds_sync<true>();
+        store_half<F>(sm + G::oR, t_slot(I, J >> 1), J & 1, split_half<F>(turn_out(t)), l);
+        lds_sync<true>();
+        store_half<F>(sm + G::oC, tt_slot(J, I >> 1), I & 1,
+                      split_half<F>(kind ? at4(&sr[0][16 * I + 4 * g]) * pe[i] : pe[i]), l);
+        if (I == J) {  // the block beside the diagonal that its pair takes along: zeros
+          if (I % 2 == 0)
+            store_half<F>(sm + G::oR, t_slot(I, I >> 1), 1, split_half<F>(zero4()), l);
+          else
+            store_half<F>(sm + G::oC, tt_slot(I, I >> 1), 0, split_half<F>(zero4()), l);
+        }
+      }
+    };
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KN; ++i) {
+      const int at = tid + 256 * i, r = at / CPR, e = at % CPR * 8;
+      *(Vec*)(sm + G::oK + r * LDK + e) = r < m ? kv[i] : Vec{};
+      *(Vec*)(sm + G::oQ + r * LDK + e) = r < m ? qv[i] : Vec{};
+    }
+    lay(0);
+    __syncthreads();
+    // ---- dP K and dP^T Q; then E K and E^T beta K
+    Pair<F> kf[2][2];
+    float end = 0.f;
+    {
+      Pair<F> qf[2][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          kf[b][p] = col_pair<LDK>(sm + G::oK, 32 * p, col + 16 * b, ln);
+          qf[b][p] = col_pair<LDK>(sm + G::oQ, 32 * p, col + 16 * b, ln);
+        }
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const int I = I0 + i, r = 16 * I + c;
+        const float eg = sr[1][r] * a.scale, er = sr[2][r];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const f32x4 k = load4(sm + G::oK + r * LDK + col + 16 * b + 4 * g);
+          dq[b][i] *= eg;
+          yd[b][i] *= er;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) end = __builtin_fmaf(k[v], yd[b][i][v], end);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          if (p <= I / 2) {
+            const Terms<F> P = load_terms<F>(sm + G::oR, t_slot(I, p), l);
+#pragma unroll
+            for (int t = 2; t >= 0; --t)
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                dq[b][i] = Pair<F>::template mma<true>(P.t[t], kf[b][p], dq[b][i]);
+          }
+          if (p >= I / 2) {
+            const Terms<F> P = load_terms<F>(sm + G::oC, tt_slot(I, p), l);
+#pragma unroll
+            for (int t = 2; t >= 0; --t)
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                yd[b][i] = Pair<F>::template mma<true>(P.t[t], qf[b][p], yd[b][i]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    lay(1);
+    __syncthreads();
+    // The sums over the value heads of a key head, as above.
+    float* acc = a.ws + ((int64_t)slot * a.Hv + hk * gr) * ws_tile(DK, DV) + ws_S(DV) + 4 * tid;
+    T* const dQp = (T*)a.dQ + kat;
+    T* const dKp = (T*)a.dK + kat;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int I = I0 + i, r = 16 * I + c;
+      const float bt = sr[0][r], eg = sr[1][r];
+      f32x4 F_[2] = {zero4(), zero4()};
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        if (p <= I / 2) {
+          const Terms<F> Er = load_terms<F>(sm + G::oR, t_slot(I, p), l);
+#pragma unroll
+          for (int t = 2; t >= 0; --t)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+              F_[b] = Pair<F>::template mma<true>(Er.t[t], kf[b][p], F_[b]);
+        }
+        if (p >= I / 2) {
+          const Terms<F> Ec = load_terms<F>(sm + G::oC, tt_slot(I, p), l);
+#pragma unroll
+          for (int t = 2; t >= 0; --t)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+              yd[b][i] = Pair<F>::template mma<true>(Ec.t[t], kf[b][p], yd[b][i]);
+        }
+      }
+      float dotF = 0.f, dotG = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 k = load4(sm + G::oK + r * LDK + col + 16 * b + 4 * g);
+        const f32x4 q = load4(sm + G::oQ + r * LDK + col + 16 * b + 4 * g);
+        const f32x4 kp = bt * (F_[b] - eg * zs[b][i]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          dotF = __builtin_fmaf(k[v], F_[b][v], dotF);
+          dotG += q[v] * dq[b][i][v] + k[v] * (kp[v] - yd[b][i][v]);
+        }
+        f32x4 sq = dq[b][i], sk = kp + yd[b][i];
+        float* at = acc + (b * NR + i) * 2 * 1024;
+        if (h > hk * gr) {
+          sq += at4(at);
+          sk += at4(at + 1024);
+        }
+        if (h + 1 < (hk + 1) * gr) {
+          *(f32x4*)at = sq;
+          *(f32x4*)(at + 1024) = sk;
+        } else if (r < m) {
+          const uint32_t to = (uint32_t)r * kld + (uint32_t)(col + 16 * b + 4 * g);
+          store4(dQp + to, sq);
+          store4(dKp + to, sk);
+        }
+      }
+      dotF = sum_apart32(sum_apart16(dotF));
+      dotG = sum_apart32(sum_apart16(dotG));
+      if (g == 0) {
+        red[0][wv % G::NC][r] = dotF;
+        red[1][wv % G::NC][r] = dotG;
+      }
+    }
+    // (every row group has formed the same <S, dS> of its columns)
+    if (I0 == 0) end = __builtin_fmaf(sr[1][BC - 1], ss, end);
+    end = sum_lanes<64>(end);
+    if (l == 0) send[wv] = end;
+    __syncthreads();
+    if (tid < BC) {
+      const int r = tid;
+      float db = 0.f, dg = 0.f;
+#pragma unroll
+      for (int i = 0; i < NJ; ++i) db += sdb[i][r];
+#pragma unroll
+      for (int i = 0; i < G::NC; ++i) {
+        db += red[0][i][r];
+        dg += red[1][i][r];
+      }
+      if (r == m - 1) dg += (send[0] + send[1]) + (send[2] + send[3]);
+      sdg[r] = dg;
+      if (r < m) a.dbeta[(t0 + r) * a.Hv + h] = db;
+    }
+    __syncthreads();
+    if (tid < m) a.dg[(t0 + tid) * a.Hv + h] = part_sum(sdg, tid, m, a.C);
   }
 }
 
@@ -662,8 +1056,20 @@ static hipError_t run_backward(const BwdArgs& a, int64_t slots, hipStream_t st) 
     const hipError_t e = launch_walks(a, DK, DV, sizeof(T) == 4 ? 0 : 1, st);
     if (e != hipSuccess) return e;
   }
-  if (slots > 0)
-    hipLaunchKernelGGL((k_bwd_grads<DK, DV, T>), dim3((unsigned)(slots * a.Hk)), dim3(512), 0, st, a);
+  if (slots > 0) {
+    const unsigned tiles = (unsigned)(slots * a.Hk);
+    if constexpr (sizeof(T) == 2) {
+      // With no CU left over, two workgroups of four waves a CU; until then one of eight,
+      // which has a chunk done sooner: us of the two for DK = DV = 128, 64 chunks by key
+      // heads 24.6 and 19.5, 256 30.1 and 25.7, 320 37.7 and 43.1, 1024 83 and 101; 1024
+      // of 64 by 64 47 and 56.
+      if (tiles > 256) {
+        hipLaunchKernelGGL((k_bwd_grads_half<DK, DV>), dim3(tiles), dim3(256), 0, st, a);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((k_bwd_grads<DK, DV, T>), dim3(tiles), dim3(512), 0, st, a);
+  }
   return hipGetLastError();
 }
 

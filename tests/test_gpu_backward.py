@@ -132,6 +132,29 @@ def test_many_slices(dt, B, L, Hk, Hv, dk, dv, packed):
         compare(part + [got[5][s:s + 1, hv]], oracle(sub, [lens[s]], 64, 0.3), dt)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,Hk,Hv,dk,dv,C,packed", [
+    (3, 450, 12, 24, 128, 128, 64, False), (2, 321, 22, 22, 64, 64, 16, False),
+    (9, 129, 10, 30, 128, 64, 32, False), (1, 1100, 15, 15, 64, 128, 64, False),
+    (90, 80, 3, 6, 128, 128, 64, True)])
+def test_many_tiles(dt, B, L, Hk, Hv, dk, dv, C, packed):
+    """Past 256 chunks by key heads the per-chunk gradients run another way: sampled
+    sequences and key heads, among them the last."""
+    lens = [1 + s * (L - 1) // (B - 1) for s in range(B)] if packed else [L] * B
+    assert sum((m + 63) // 64 for m in lens) * Hk > 256
+    x = make(lens, Hk, Hv, dk, dv, C, dt, L + dv)
+    got = run(x, lens, C, 0.3, packed)
+    r = Hv // Hk
+    for s, hk in {(0, 0), (B - 1, Hk - 1), (B // 2, Hk // 2)}:
+        t = sum(lens[:s])
+        w, hv = slice(t, t + lens[s]), slice(hk * r, (hk + 1) * r)
+        sub = {k: (v[s:s + 1, hv] if k in ("S0", "dS") else
+                   v[w, hk:hk + 1] if k in ("Q", "K") else v[w, hv]) for k, v in x.items()}
+        flat = [a.reshape((-1,) + tuple(a.shape[2:])) for a in got[:5]]
+        part = [a[w, hk:hk + 1] if i < 2 else a[w, hv] for i, a in enumerate(flat)]
+        compare(part + [got[5][s:s + 1, hv]], oracle(sub, [lens[s]], C, 0.3), dt)
+
+
 def test_packed_is_each_sequence_alone_bit_for_bit():
     lens = [70, 3, 129]
     x = make(lens, 1, 2, 64, 64, 64, "bf16", 1)
