@@ -657,7 +657,8 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
 // to scratch (168 us became 185 and more).
 // Bound: vector instructions (36% of the cycles), matrix instructions (27%), LDS (27%) of
 // two waves a SIMD, and their waits for memory.  8192 tokens of 16 heads of 128 by 128 in
-// bf16 take 168 us, 290 KB a chunk and head at 3.5 TB/s; 4 x 8192 of 32 value heads 1.45 ms.
+// bf16 take 168 us, 290 KB a chunk and head at 3.5 TB/s; 4 x 8192 of 32 value heads 1.4 ms,
+// 4.2 TB/s.
 template <int DK, int DV>
 struct Halves {
   static constexpr int NC = DK / 32, RG = 4 / NC, NR = 4 / RG, LDK = DK + 8;
