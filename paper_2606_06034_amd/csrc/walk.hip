@@ -10,6 +10,8 @@
 // 128 in bf16 take 1.29 ms and move 6 GB, 4.7 TB/s.
 #include "backward.hpp"
 
+#include <algorithm>
+
 namespace gdn {
 
 namespace {
@@ -83,7 +85,7 @@ struct Flow {
 }  // namespace
 
 template <typename W>
-__device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& lds) {
+__device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& lds, unsigned bx) {
   constexpr int DK = W::KD, DV = W::VD, NSL = W::CW, R = W::RING;
   constexpr bool REV = W::BACK;
   typedef __bf16 T;
@@ -94,8 +96,8 @@ __device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& ld
   auto& tr = lds.tr;
   // Workgroups are dealt to the 8 XCDs in turn; all those of a head go to one, whose
   // L2 then reads the head's chunks once.
-  const unsigned xr = blockIdx.x >> 3;
-  const int64_t sh = (int64_t)(xr / W::NG) * 8 + (blockIdx.x & 7);
+  const unsigned xr = bx >> 3;
+  const int64_t sh = (int64_t)(xr / W::NG) * 8 + (bx & 7);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
   const int n0 = (int)(xr % W::NG) * 16 * NSL, s = (int)((uint32_t)sh / (uint32_t)a.Hv);
   const int h = (int)((uint32_t)sh - (uint32_t)s * (uint32_t)a.Hv), hk = h / a.gr;
@@ -109,6 +111,7 @@ __device__ __forceinline__ void lone_waves(const BwdArgs& a, typename W::Lds& ld
   auto chunk = [&](int i) { return REV ? nc - 1 - i : i; };  // of step i
 
   if (wv >= W::CW) {
+    if (wv >= W::CW + W::LW) return;  // (a workgroup of both kinds has two waves more)
     // ---- loader.  Step i's operands are read between the barrier that ends step
     // i - 1 and the one that ends step i.  Rows past a chunk's last token repeat it: their beta is 0, which takes them
     // out of Z and dX, and dO's are masked where they are used.  Steps past the
@@ -367,7 +370,7 @@ struct Team : Flow<DK, DV, 1, REV, 2> {
 };
 
 template <typename W>
-__device__ __forceinline__ void team(const BwdArgs& a, typename W::Lds& lds) {
+__device__ __forceinline__ void team(const BwdArgs& a, typename W::Lds& lds, unsigned bx) {
   constexpr int DK = W::KD, DV = W::VD;
   constexpr bool REV = W::BACK;
   typedef __bf16 T;
@@ -378,8 +381,8 @@ __device__ __forceinline__ void team(const BwdArgs& a, typename W::Lds& lds) {
   auto& tr = lds.tr;
   float* part = lds.part;
   T *sZ = lds.sZ, *sY = lds.sY, *sO = lds.sO;
-  const unsigned xr = blockIdx.x >> 3;  // all slices of a head on one XCD
-  const int64_t sh = (int64_t)(xr / NS) * 8 + (blockIdx.x & 7);
+  const unsigned xr = bx >> 3;  // all slices of a head on one XCD
+  const int64_t sh = (int64_t)(xr / NS) * 8 + (bx & 7);
   if (sh >= (int64_t)a.nseq * a.Hv) return;  // the whole workgroup, before any barrier
   const int J = (int)(xr % NS), s = (int)((uint32_t)sh / (uint32_t)a.Hv);
   const int h = (int)((uint32_t)sh - (uint32_t)s * (uint32_t)a.Hv), hk = h / a.gr;
@@ -1000,9 +1003,9 @@ __global__ __launch_bounds__(512) void k_bwd_teams(const BwdArgs a) {
     typename S::Lds s;
   } lds;
   if (blockIdx.y == 0)
-    team<R>(a, lds.r);
+    team<R>(a, lds.r, blockIdx.x);
   else
-    team<S>(a, lds.s);
+    team<S>(a, lds.s, blockIdx.x);
 }
 
 template <int DK, int DV>
@@ -1015,9 +1018,43 @@ __global__ __launch_bounds__(384) void k_bwd_lone(const BwdArgs a) {
     typename S::Lds s;
   } lds;
   if (blockIdx.y == 0)
-    lone_waves<R>(a, lds.r);
+    lone_waves<R>(a, lds.r, blockIdx.x);
   else
-    lone_waves<S>(a, lds.s);
+    lone_waves<S>(a, lds.s, blockIdx.x);
+}
+
+// Packed sequences: those of more than `longest` chunks by teams, first, the others by
+// lone waves; the workgroups of the other kind end at once.
+template <int DK, int DV>
+__global__ __launch_bounds__(512) void k_bwd_mixed(const BwdArgs a, int longest) {
+  typedef Team<DK, DV, true> TR;
+  typedef Team<DK, DV, false> TS;
+  typedef Flow<DK, DV, 4, true, 2> LR;
+  typedef Flow<DK, DV, 4, false, 3> LS;
+  __shared__ union __attribute__((aligned(16))) {
+    typename TR::Lds tr;
+    typename TS::Lds ts;
+    typename LR::Lds lr;
+    typename LS::Lds ls;
+  } lds;
+  const uint32_t heads = (uint32_t)a.nseq * (uint32_t)a.Hv, n = (heads + 7) / 8 * 8;
+  constexpr unsigned NT = DV / 16, NL = DV / 64;  // workgroups a head
+  unsigned bx = blockIdx.x;
+  const bool teams = bx < 2 * n * NT;
+  if (!teams) bx -= 2 * n * NT;
+  const unsigned per = teams ? NT : NL, dir = n * per;
+  const bool rev = bx < dir;
+  if (!rev) bx -= dir;
+  const uint32_t sh = (bx >> 3) / per * 8 + (bx & 7);
+  if (sh >= heads) return;
+  if ((Seq(a, (int)(sh / (uint32_t)a.Hv)).chunks() > longest) != teams) return;
+  if (teams) {
+    if (rev) team<TR>(a, lds.tr, bx);
+    else team<TS>(a, lds.ts, bx);
+  } else {
+    if (rev) lone_waves<LR>(a, lds.lr, bx);
+    else lone_waves<LS>(a, lds.ls, bx);
+  }
 }
 
 template <int DK, int DV>
@@ -1036,14 +1073,20 @@ static hipError_t run_walks(const BwdArgs& a, int dtype, hipStream_t st) {
   // A CU takes one team (a slice) or one workgroup of four lone waves (four slices).
   // A team's step takes 2.3 us at most, a workgroup's 4 to 6, so teams walk while both
   // directions' are two rounds: us for 32 chunks, DK = DV = 128, teams and lone waves:
-  // 128 slices 70 and 139, 256 133 and 148, 320 190 and 165, 512 281 and 187.  Packed
-  // sequences differ in length, and few of them walk side by side for long; 8192 tokens
-  // in 4 of them (512 slices) take 292 and 299, in 9 (1152) 298 and 179 to 299 and 320,
-  // in 22 (2816) 376 and 345; with half the heads in 11 (704) 155 and 255.
-  const int64_t chains = a.cu ? slices / 4 : slices;
+  // 128 slices 70 and 139, 256 133 and 148, 320 190 and 165, 512 281 and 187.
+  // Packed sequences differ in length, which the host does not know: all of them by lone
+  // waves would keep the CUs busy for about 0.0097 us a chunk and slice, and one of c
+  // chunks alone takes 6 c us.  Those that take longer than all together go to teams (the
+  // factor is the one that measured best).  8192 tokens of 16 heads by teams alone, lone
+  // waves alone, and so: 22 sequences 376, 345, 267 us; 31 372, 321, 277; 9 of at most 30
+  // chunks 298, 180, 187; 4 292, 299, 340; 8 heads in 11 sequences 155, 255, 144.
+  const int64_t longest = (int64_t)a.L * a.Hv * (DV / 16) / 30000;
   if (dtype == 0)
     hipLaunchKernelGGL((k_bwd_walks_f32<DK, DV>), dim3(n * (DV / 16), both), dim3(256), 0, st, a);
-  else if (chains <= 256)
+  else if (a.cu && a.L > 0)
+    hipLaunchKernelGGL((k_bwd_mixed<DK, DV>), dim3(2 * n * (DV / 16 + DV / 64)), dim3(512), 0, st,
+                       a, (int)std::min<int64_t>(longest, INT32_MAX));
+  else if (slices <= 256)
     hipLaunchKernelGGL((k_bwd_teams<DK, DV>), dim3(n * (DV / 16), both), dim3(512), 0, st, a);
   else
     hipLaunchKernelGGL((k_bwd_lone<DK, DV>), dim3(n * (DV / 64), both), dim3(384), 0, st, a);

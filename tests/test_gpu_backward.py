@@ -155,6 +155,17 @@ def test_many_tiles(dt, B, L, Hk, Hv, dk, dv, C, packed):
         compare(part + [got[5][s:s + 1, hv]], oracle(sub, [lens[s]], C, 0.3), dt)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv,Hk,Hv", [(128, 128, 3, 9), (64, 128, 8, 8), (128, 64, 5, 20)])
+def test_long_and_short_packed(dt, dk, dv, Hk, Hv):
+    """Long and short packed sequences are walked in different ways by one launch."""
+    lens = [5, 700, 0, 64, 321, 1, 130, 65]
+    longest = sum(lens) * Hv * (dv // 16) // 30000
+    assert 1 <= longest < 11
+    x = make(lens, Hk, Hv, dk, dv, 64, dt, dk + dv)
+    compare(run(x, lens, 64, 0.2, True), oracle(x, lens, 64, 0.2), dt)
+
+
 def test_packed_is_each_sequence_alone_bit_for_bit():
     lens = [70, 3, 129]
     x = make(lens, 1, 2, 64, 64, 64, "bf16", 1)
