@@ -98,3 +98,11 @@ def test_fp32_one_slice_workgroups_share_a_cu(kernels):
             assert per_cu(k) >= 2, (NB, DK, DV, packed)
             seen += 1
     assert seen == 12
+
+
+def test_backward_gradients_share_a_cu(kernels):
+    # past 256 chunks by key heads, two workgroups of four waves
+    half = {n: k for n, k in kernels.items() if "k_bwd_grads_half" in n}
+    assert len(half) == 4  # widths
+    for name, k in half.items():
+        assert per_cu(k) >= 2 and k[".vgpr_spill_count"] == 0, name
