@@ -42,9 +42,12 @@ _device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _dev(t: torch.Tensor, name: str, dtype=None, numel: Optional[int] = None) -> int:
-    if (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and
-            (dtype is None or t.dtype is dtype) and (numel is None or t.numel() == numel)):
-        return t.data_ptr()
+    try:
+        if (t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype is dtype) and
+                (numel is None or t.numel() == numel)):
+            return t.data_ptr()
+    except AttributeError:  # not a tensor
+        pass
     return _dev_checked(t, name, dtype, numel)
 
 
@@ -215,7 +218,7 @@ def gdn_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     y = torch.empty_like(x) if y is None else y
     mean = rstd = None
     if want_stats:
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
         mean = torch.empty_like(rstd) if k == GDN_NORM_LAYER else None
     wp, bp, wdt = _params(weight, bias, D)
     _check("gdn_norm_forward", lib.gdn_norm_forward(
