@@ -1,4 +1,8 @@
-"""ctypes marshalling for libgdninv.so (see include/gdninv.h for the contract)."""
+"""ctypes marshalling for libgdninv.so (see include/gdninv.h for the contract).
+
+stream: a torch stream to run on, the current one where none is given.  Its caller orders it
+with the streams that make the inputs and use the results.
+"""
 
 from __future__ import annotations
 
@@ -137,6 +141,24 @@ def _fdtype(t: torch.Tensor, name: str) -> int:
 def _stream(stream) -> int:
     s = torch.cuda.current_stream() if stream is None else stream
     return s.cuda_stream
+
+
+def _on_stream(stream, fn, args: dict):
+    """fn(**args) with `stream` current, for a call that names one: what the call allocates
+    (and drops, a workspace) then belongs to the stream that its kernels run on, so that the
+    allocator does not hand it to other work before they end.  The results are marked as used
+    on the stream that was current too, which is where the caller goes on with them."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    before = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        out = fn(**{**args, "stream": None})
+    if stream == before:
+        return out
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(before)
+    return out
 
 
 def _tiles(A: torch.Tensor) -> Tuple[int, int]:
