@@ -172,6 +172,8 @@ def gdn_build_A(K: torch.Tensor, beta: torch.Tensor, g: torch.Tensor, C: int,
                 a_dtype: Optional[torch.dtype] = None, A: Optional[torch.Tensor] = None,
                 stream=None) -> torch.Tensor:
     """A [B, H, L/C, C, C] from K [B, L, H, dk], beta, g [B, L, H] (fp32)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_build_A, locals())
     B, L, H, dk = K.shape
     kdt = _fdtype(K, "K")
     adt = _FDT[a_dtype] if a_dtype is not None else (_fdtype(A, "A") if A is not None else kdt)
@@ -188,6 +190,8 @@ def gdn_build_A(K: torch.Tensor, beta: torch.Tensor, g: torch.Tensor, C: int,
 def gdn_chunk_inverse_neumann(A: torch.Tensor, N: int, S: int, Tinv: Optional[torch.Tensor] = None,
                               stream=None) -> torch.Tensor:
     """T_hat(N, S) of every C x C tile of A (same shape and dtype)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_neumann, locals())
     n, C = _tiles(A)
     dt = _fdtype(A, "A")
     if Tinv is None:
@@ -200,6 +204,8 @@ def gdn_chunk_inverse_neumann(A: torch.Tensor, N: int, S: int, Tinv: Optional[to
 def gdn_chunk_inverse_fwdsub(A: torch.Tensor, Tinv: Optional[torch.Tensor] = None,
                              stream=None) -> torch.Tensor:
     """Exact (I + A)^-1 of every tile by forward substitution."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_fwdsub, locals())
     n, C = _tiles(A)
     dt = _fdtype(A, "A")
     if Tinv is None:
@@ -212,6 +218,8 @@ def gdn_chunk_inverse_fwdsub(A: torch.Tensor, Tinv: Optional[torch.Tensor] = Non
 def gdn_chunk_inverse_blockwise(A: torch.Tensor, Tinv: Optional[torch.Tensor] = None,
                                 stream=None) -> torch.Tensor:
     """Exact (I + A)^-1 of every tile by 16 x 16 block recursion (products only)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_blockwise, locals())
     n, C = _tiles(A)
     dt = _fdtype(A, "A")
     if Tinv is None:
@@ -225,6 +233,8 @@ def gdn_wy_apply(Tinv: torch.Tensor, K: torch.Tensor, V: torch.Tensor, beta: tor
                  W: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
                  stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """W = T diag(beta) K, U = T diag(beta) V per chunk."""
+    if stream is not None:
+        return _on_stream(stream, gdn_wy_apply, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
     dt = _fdtype(K, "K")
@@ -244,6 +254,8 @@ def gdn_chunk_wy_fused(K: torch.Tensor, V: torch.Tensor, beta: torch.Tensor, g: 
                        W: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
                        Tinv: Optional[torch.Tensor] = None, stream=None):
     """Fused build A -> T_hat(N, S) -> (W, U[, Tinv])."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_wy_fused, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
     dt = _fdtype(K, "K")
@@ -266,6 +278,8 @@ def gdn_chunk_wy_fused_blockwise(K: torch.Tensor, V: torch.Tensor, beta: torch.T
                                  W: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
                                  Tinv: Optional[torch.Tensor] = None, stream=None):
     """Fused build A -> exact inverse (block-wise) -> (W, U[, Tinv])."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_wy_fused_blockwise, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
     dt = _fdtype(K, "K")
@@ -292,6 +306,8 @@ def gdn_quantize_tiles_i8(A: torch.Tensor, Aq: Optional[torch.Tensor] = None,
                           eA: Optional[torch.Tensor] = None, stream=None):
     """(Aq int8 tiles, eA int32 per tile) with A ~ Aq * 2^eA; C = 128:
     eA [n, 3], one exponent per block (11, 21, 22)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_quantize_tiles_i8, locals())
     n, C = _tiles(A)
     ne = _nexp(C)
     Aq = torch.empty(A.shape, dtype=torch.int8, device=A.device) if Aq is None else Aq
@@ -311,6 +327,8 @@ def gdn_chunk_inverse_neumann_i8(Aq: torch.Tensor, eA: torch.Tensor, N: int, S: 
     """(Tq int8, eT int32[, Tdeq fp32]) with T_hat = I + Tq * 2^eT (plain:
     T_hat = Tq * 2^eT, the diagonal in the codes; GDN_INT_PLAIN); C = 128:
     block-wise, eA and eT [n, 3] (blocks 11, 21, 22)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_neumann_i8, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
     eT = torch.empty_like(eA) if eT is None else eT
@@ -333,6 +351,8 @@ def gdn_chunk_inverse_neumann_i8_fused(K: torch.Tensor, beta: torch.Tensor, g: t
                                        Tdeq: Optional[torch.Tensor] = None, stream=None):
     """K [B, L, H, dk] -> (Tq int8 [B, H, L/C, C, C], eT int32[, Tdeq fp32]):
     build A, quantise and invert in one launch."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_neumann_i8_fused, locals())
     B, L, H, dk = K.shape
     nc = L // C if C else 0
     shape = (B, H, nc, C, C)
@@ -357,6 +377,8 @@ def gdn_quantize_tiles_i16(A: torch.Tensor, Aq: Optional[torch.Tensor] = None,
                            eA: Optional[torch.Tensor] = None, stream=None):
     """(Aq int16 tiles, eA int32 per tile) with A ~ Aq * 2^eA; C = 128:
     eA [n, 3], one exponent per block (11, 21, 22)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_quantize_tiles_i16, locals())
     n, C = _tiles(A)
     ne = _nexp(C)
     Aq = torch.empty(A.shape, dtype=torch.int16, device=A.device) if Aq is None else Aq
@@ -376,6 +398,8 @@ def gdn_chunk_inverse_neumann_i16(Aq: torch.Tensor, eA: torch.Tensor, N: int, S:
     """(Tq int16, eT int32[, Tdeq fp32]) with T_hat = I + Tq * 2^eT (plain:
     T_hat = Tq * 2^eT, the diagonal in the codes; GDN_INT_PLAIN); C = 128:
     block-wise, eA and eT [n, 3] (blocks 11, 21, 22)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_neumann_i16, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
     eT = torch.empty_like(eA) if eT is None else eT
@@ -397,6 +421,8 @@ def gdn_chunk_inverse_fwdsub_i16(Aq: torch.Tensor, eA: torch.Tensor, want_deq: b
                                  Tdeq: Optional[torch.Tensor] = None, stream=None):
     """(Tq int16, eT int32[, Tdeq fp32]): integer forward substitution,
     T = I + Tq * 2^eT."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_fwdsub_i16, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
     eT = torch.empty_like(eA) if eT is None else eT
@@ -417,6 +443,8 @@ def gdn_chunk_inverse_fwdsub_i8(Aq: torch.Tensor, eA: torch.Tensor, want_deq: bo
                                 Tdeq: Optional[torch.Tensor] = None, stream=None):
     """(Tq int8, eT int32[, Tdeq fp32]): integer forward substitution,
     T = I + Tq * 2^eT."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_fwdsub_i8, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
     eT = torch.empty_like(eA) if eT is None else eT
@@ -438,6 +466,8 @@ def gdn_chunk_inverse_neumann_i16_fused(K: torch.Tensor, beta: torch.Tensor, g: 
                                         Tdeq: Optional[torch.Tensor] = None, stream=None):
     """K [B, L, H, dk] -> (Tq int16 [B, H, L/C, C, C], eT int32[, Tdeq fp32]):
     build A, quantise and invert in one launch."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_inverse_neumann_i16_fused, locals())
     B, L, H, dk = K.shape
     nc = L // C if C else 0
     shape = (B, H, nc, C, C)
@@ -493,6 +523,8 @@ def gdn_chunk_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, beta: t
     workspace (a byte tensor of gdn_chunk_forward_workspace() bytes) is allocated when
     not given.  inverse: "neumann" (default), "exact" (as exact=True), "int16" or "int8"
     (the integer T_hat(N, S) inside the layer)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_forward, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
     dt = _fdtype(K, "K")
@@ -579,6 +611,8 @@ def gdn_chunk_forward_state(Q: torch.Tensor, g: torch.Tensor, C: int, workspace:
                             O: Optional[torch.Tensor] = None,
                             S_final: Optional[torch.Tensor] = None, stream=None):
     """Second phase of gdn_chunk_forward: the state pass over a prepared workspace."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_forward_state, locals())
     B, L, H, dk = Q.shape
     dt = _fdtype(Q, "Q")
     scale = dk ** -0.5 if scale is None else float(scale)
@@ -617,6 +651,8 @@ def gdn_chunk_wy_fused_varlen(K: torch.Tensor, V: torch.Tensor, beta: torch.Tens
                               Tinv: Optional[torch.Tensor] = None, stream=None):
     """Fused build A -> inverse -> (W, U[, Tinv]) over packed sequences;
     tables = gdn_varlen_tables(cu_seqlens, C)."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_wy_fused_varlen, locals())
     dcu, doff, n_chunks = tables
     B, T, H, dk = K.shape
     if B != 1:
@@ -655,6 +691,8 @@ def gdn_chunk_forward_varlen(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
     """Layer forward over packed sequences: (O [1, T, H, dv], S_final
     [nseq, H, dk, dv] fp32 or None); tables = gdn_varlen_tables(cu_seqlens, C).
     Defaults and inverse modes as gdn_chunk_forward."""
+    if stream is not None:
+        return _on_stream(stream, gdn_chunk_forward_varlen, locals())
     dcu, doff, n_chunks = tables
     B, T, H, dk = K.shape
     if B != 1:

@@ -103,13 +103,56 @@ def layer_calls(x):
     }
 
 
+def chunk_calls(x):
+    """The same of the chunk-wise forward and the inverses."""
+    seq = [x[k] for k in ("Q", "K", "V", "beta", "g")]
+    K, V, beta, g = seq[1:]
+    dev = K.device
+    A = 0.1 * torch.tril(torch.ones(3, 64, 64, device=dev), -1)
+    codes = torch.zeros(3, 64, 64, dtype=torch.int8, device=dev)
+    e = torch.zeros(3, dtype=torch.int32, device=dev)
+    packed = G.gdn_varlen_tables([0, 100, 128], 64, device=dev)
+    T = torch.zeros(K.shape[0], K.shape[2], 2, 64, 64, dtype=K.dtype, device=dev)
+    ws = torch.zeros(1 << 22, dtype=torch.uint8, device=dev)
+    return {
+        "forward": lambda s: G.gdn_chunk_forward(*seq, 64, stream=s),
+        "forward_varlen": lambda s: G.gdn_chunk_forward_varlen(*seq, packed, 64, stream=s),
+        "forward_state": lambda s: G.gdn_chunk_forward_state(
+            seq[0], g, 64, G.gdn_chunk_forward_prepare(*seq, 64, ws, stream=s), V.shape[-1],
+            stream=s),
+        "build_A": lambda s: (G.gdn_build_A(K, beta, g, 64, stream=s),),
+        "neumann": lambda s: (G.gdn_chunk_inverse_neumann(A, 3, 8, stream=s),),
+        "fwdsub": lambda s: (G.gdn_chunk_inverse_fwdsub(A, stream=s),),
+        "blockwise": lambda s: (G.gdn_chunk_inverse_blockwise(A, stream=s),),
+        "wy_apply": lambda s: G.gdn_wy_apply(T, K, V, beta, 64, stream=s),
+        "wy_fused": lambda s: G.gdn_chunk_wy_fused(K, V, beta, g, 64, 3, 8, stream=s),
+        "wy_fused_blockwise": lambda s: G.gdn_chunk_wy_fused_blockwise(K, V, beta, g, 64, stream=s),
+        "wy_fused_varlen": lambda s: G.gdn_chunk_wy_fused_varlen(K, V, beta, g, packed, 64,
+                                                                 stream=s),
+        "quantize_i8": lambda s: G.gdn_quantize_tiles_i8(A, stream=s),
+        "inverse_i8": lambda s: G.gdn_chunk_inverse_neumann_i8(codes, e, 3, 8, stream=s),
+        "fused_i8": lambda s: G.gdn_chunk_inverse_neumann_i8_fused(K, beta, g, 64, 3, 8, stream=s),
+        "fwdsub_i8": lambda s: G.gdn_chunk_inverse_fwdsub_i8(codes, e, stream=s),
+        "quantize_i16": lambda s: G.gdn_quantize_tiles_i16(A, stream=s),
+        "inverse_i16": lambda s: G.gdn_chunk_inverse_neumann_i16(codes.short(), e, 3, 8, stream=s),
+        "fused_i16": lambda s: G.gdn_chunk_inverse_neumann_i16_fused(K, beta, g, 64, 3, 8,
+                                                                     stream=s),
+        "fwdsub_i16": lambda s: G.gdn_chunk_inverse_fwdsub_i16(codes.short(), e, stream=s),
+    }
+
+
+def calls(x):
+    return {**layer_calls(x), **chunk_calls(x)}
+
+
 LAYER = sorted(layer_calls(operands()))
+ALL = sorted(calls(operands()))
 
 
-@pytest.mark.parametrize("name", LAYER)
+@pytest.mark.parametrize("name", ALL)
 def test_a_call_allocates_on_the_stream_it_names(played, name):
     lib, log, marked = played
-    call = layer_calls(operands())[name]
+    call = calls(operands())[name]
     log.clear()
     out = [t for t in call(Stream(2)) if t is not None]
     assert set(lib.launched) == {2}
@@ -118,23 +161,23 @@ def test_a_call_allocates_on_the_stream_it_names(played, name):
     assert {t.data_ptr() for t in out} == {p for p, s in marked if s == 1}
 
 
-@pytest.mark.parametrize("name", LAYER)
+@pytest.mark.parametrize("name", ALL)
 def test_a_call_without_a_stream_stays_on_the_current_one(played, name):
     lib, log, marked = played
-    call = layer_calls(operands())[name]
+    call = calls(operands())[name]
     log.clear()
     call(None)
     assert set(lib.launched) == {1} and log and all(s == 1 for _, s in log) and not marked
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("name", LAYER)
+@pytest.mark.parametrize("name", LAYER + ["forward", "forward_varlen"])
 def test_results_on_a_named_stream(name):
     """Bit for bit those of the current stream; the memory of a dropped workspace is not
     what the caller's stream gets next."""
     x = operands("cuda", torch.bfloat16, 2, 128, 4, 128) if "varlen" not in name else \
         operands("cuda", torch.bfloat16, 1, 128, 4, 128)
-    call = layer_calls(x)[name]
+    call = calls(x)[name]
     want = [t for t in call(None) if t is not None]
     torch.cuda.synchronize()
     torch.cuda.empty_cache()  # (want's own workspace goes back)
