@@ -69,9 +69,12 @@ int gdn_chunk_backward(const void* Q, const void* K, const void* V, const float*
 /* The same over packed sequences, as gdn_chunk_forward_varlen runs them: the
  * tensors hold T tokens, sequence s those of cu_seqlens[s] .. cu_seqlens[s +
  * 1] - 1 (nseq + 1 int32 offsets on the device, non-decreasing, within
- * 0 .. T); the states are [nseq, Hv, dk, dv].  A sequence whose offsets are
- * out of range is taken as empty (dS0 = dS_final); tokens outside every
- * sequence get no gradients written. */
+ * 0 .. T); the states are [nseq, Hv, dk, dv].  A sequence with an offset out
+ * of range, or ending before it begins, is taken as empty (dS0 = dS_final),
+ * whichever of the sequences it is; tokens outside every sequence get no
+ * gradients written.  Offsets within range have to be non-decreasing: nothing
+ * outside the arrays is touched where they are not, but the gradients are
+ * undefined. */
 int gdn_chunk_backward_varlen(const void* Q, const void* K, const void* V, const float* beta,
                               const float* g, const void* dO, const float* S0,
                               const float* dS_final, void* dQ, void* dK, void* dV, float* dbeta,

@@ -73,10 +73,14 @@ struct Seq {
 __device__ __forceinline__ int chunk_at(const BwdArgs& a, uint32_t slot, int64_t& t0) {
   int s;
   if (a.cu) {
-    int lo = 0, hi = a.nseq;  // the last s with base(s) <= slot
+    // the last s with base(s) <= slot; a sequence that begins out of range has no chunks,
+    // and its offset says nothing of the others': the next one in range is looked at
+    int lo = 0, hi = a.nseq;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.cu[mid] / BC + mid <= (int)slot) lo = mid; else hi = mid;
+      int at = mid, b = a.cu[at];
+      while ((b < 0 || b > a.L) && ++at < hi) b = a.cu[at];
+      if (at < hi && b / BC + at <= (int)slot) lo = at; else hi = mid;
     }
     s = lo;
   } else {

@@ -297,3 +297,35 @@ def test_on_another_stream_in_a_graph_and_the_same_every_time():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, ref)), i
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cu,valid", [
+    ([0, 200, 9999, 300, 400], (0, 3)), ([0, 200, -1, 300, 400], (0, 3)),
+    ([0, 200, 401, 300, 400], (0, 3)), ([-5, 200, 300, 400], (1, 2)),
+    ([0, -7, 2 ** 31 - 1, -(2 ** 31), 200, 300, 400], (4, 5))])
+def test_a_bad_offset_leaves_the_other_sequences(dt, cu, valid):
+    """Wherever in the table it is.  What is not formed keeps the 7 it had, and what would be
+    read without having been formed is NaN."""
+    x = make([200, 100, 100], 2, 4, 64, 128, 64, dt, 9, S0=False, dS=False)
+    n = len(cu) - 1
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x["S0"], x["dS"] = torch.randn(2, n, 4, 64, 128, generator=gen, device="cuda")
+    y = [x[k][None] for k in ("Q", "K", "V", "beta", "g", "dO")]
+    out = [torch.full_like(t, 7.0) for t in y[:5]] + [None]
+    ws = torch.full((G.gdn_chunk_backward_workspace(n, 400, 4, 64, 128, True),), 255,
+                    dtype=torch.uint8, device="cuda")
+    offsets = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    got = G.gdn_chunk_backward_varlen(*y, (offsets, None, 0), 64, S0=x["S0"], dS_final=x["dS"],
+                                      scale=0.3, want_dS0=True, out=out, workspace=ws)
+    rest = torch.ones(400, dtype=torch.bool)
+    for s in valid:
+        w = slice(cu[s], cu[s + 1])
+        rest[w] = False
+        sub = {k: v[s:s + 1] if k in ("S0", "dS") else v[w] for k, v in x.items()}
+        compare([a[:, w] for a in got[:5]] + [got[5][s:s + 1]],
+                oracle(sub, [cu[s + 1] - cu[s]], 64, 0.3), dt)
+    for a in got[:5]:
+        assert (a[0][rest] == 7).all()
+    for s in set(range(n)) - set(valid):
+        assert torch.equal(got[5][s], x["dS"][s])
