@@ -91,6 +91,9 @@ int backward(const void* Q, const void* K, const void* V, const float* beta, con
   if (int r = gdn_chunk_backward_workspace(nseq, L, Hv, dk, dv, packed, &need)) return r;
   if (!grid_ok(((int64_t)nseq * Hv + 7) / 8 * 8 * (dv / 16), 512)) return GDN_ERR_SHAPE;
   if (!fdtype(dtype)) return GDN_ERR_DTYPE;
+  if (packed && L > 0 && dtype == GDN_BF16 &&
+      !grid_ok(gdn::packed_walk_groups(nseq, Hv, dv), 512))
+    return GDN_ERR_SHAPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
   if (packed && !cu) return GDN_ERR_NULL;
   const int64_t tok = packed ? (int64_t)L : (int64_t)nseq * L, es = esize(dtype);

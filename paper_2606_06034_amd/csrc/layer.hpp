@@ -27,6 +27,11 @@ int norm_backward_parts(int64_t rows, int D);
 // then L is the number of all tokens, else of each sequence's.
 int64_t backward_slots(int nseq, int L, bool packed);
 int64_t backward_tile_bytes(int dk, int dv);
+// workgroups (of 512 work items) of the walks of packed sequences of bf16: of both kinds,
+// in both directions, of nseq * Hv heads rounded up to eights
+constexpr int64_t packed_walk_groups(int nseq, int Hv, int dv) {
+  return ((int64_t)nseq * Hv + 7) / 8 * 8 * 2 * (dv / 16 + dv / 64);
+}
 hipError_t launch_backward(const void* Q, const void* K, const void* V, const float* beta,
                            const float* g, const void* dO, const float* S0, const float* dSf,
                            void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS0,

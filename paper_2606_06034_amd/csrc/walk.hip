@@ -1084,8 +1084,8 @@ static hipError_t run_walks(const BwdArgs& a, int dtype, hipStream_t st) {
   if (dtype == 0)
     hipLaunchKernelGGL((k_bwd_walks_f32<DK, DV>), dim3(n * (DV / 16), both), dim3(256), 0, st, a);
   else if (a.cu && a.L > 0)
-    hipLaunchKernelGGL((k_bwd_mixed<DK, DV>), dim3(2 * n * (DV / 16 + DV / 64)), dim3(512), 0, st,
-                       a, (int)std::min<int64_t>(longest, INT32_MAX));
+    hipLaunchKernelGGL((k_bwd_mixed<DK, DV>), dim3((unsigned)packed_walk_groups(a.nseq, a.Hv, DV)),
+                       dim3(512), 0, st, a, (int)std::min<int64_t>(longest, INT32_MAX));
   else if (slices <= 256)
     hipLaunchKernelGGL((k_bwd_teams<DK, DV>), dim3(n * (DV / 16), both), dim3(512), 0, st, a);
   else

@@ -124,6 +124,31 @@ def test_packed_backward_refusals(change, code):
     assert call(L.gdn_chunk_backward_varlen, a, **change) == code
 
 
+def packed_args(**change):
+    a = {}
+    for k, v in BWD.items():
+        if k == "B":
+            a.update(cu=P[15], nseq=3)
+        else:
+            a[k] = v
+    return dict(a, **change)
+
+
+@pytest.mark.parametrize("dv,most", [(64, 838856), (128, 419424)])
+def test_packed_backward_s_largest_launch(dv, most):
+    """Both kinds of walk, both ways, are workgroups of one launch of 512 work items each:
+    2 heads (dv / 16 + dv / 64) of them, heads rounded up to eights, have to fit 2^32 - 1.
+    What fits gets as far as the missing workspace, here."""
+    args = packed_args(nseq=most // 8, Hk=8, Hv=8, dk=64, dv=dv, ws=None)
+    assert call(L.gdn_chunk_backward_varlen, args) == NULL
+    args.update(nseq=most // 8 + 1)
+    assert call(L.gdn_chunk_backward_varlen, args) == SHAPE
+    # fp32 and equal lengths launch fewer
+    assert call(L.gdn_chunk_backward_varlen, args, dtype=0) == NULL
+    assert call(L.gdn_chunk_backward, dict(BWD, B=most // 8 + 1, L=1, Hk=8, Hv=8, dk=64, dv=dv,
+                                           ws=None)) == NULL
+
+
 def test_backward_workspace():
     tile = 4 * (6 * 768 + 5 * 64 + 2 * 64 * 128 + 2 * 128 * 128)
     assert G.gdn_chunk_backward_workspace(2, 100, 3, 128, 128) == 2 * 2 * 3 * tile
