@@ -59,7 +59,9 @@ int gdn_recurrent_forward(const void* Q, const void* K, const void* V, const flo
  * enter unrounded) and rounded once at the end, in a fixed order: the same
  * call gives the same bits.
  * workspace: at least gdn_chunk_backward_workspace() bytes, contents
- * undefined on return.  dk, dv in {64, 128}.  Three launches on `stream`. */
+ * undefined on return.  dk, dv in {64, 128}; the rows of all heads of 64 tokens
+ * (of L where that is less) of Q and of V hold 4 GiB at most.  Three launches
+ * on `stream`. */
 int gdn_chunk_backward(const void* Q, const void* K, const void* V, const float* beta,
                        const float* g, const void* dO, const float* S0, const float* dS_final,
                        void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS0,

@@ -5,6 +5,8 @@
 
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "checks.hpp"
 #include "layer.hpp"
 
@@ -94,9 +96,12 @@ int backward(const void* Q, const void* K, const void* V, const float* beta, con
   if (packed && L > 0 && dtype == GDN_BF16 &&
       !grid_ok(gdn::packed_walk_groups(nseq, Hv, dv), 512))
     return GDN_ERR_SHAPE;
+  // (rows of a chunk of 64 tokens lie at 32-bit byte offsets from its first)
+  const int64_t tok = packed ? (int64_t)L : (int64_t)nseq * L, es = esize(dtype);
+  const int64_t row = std::max((int64_t)Hk * dk, (int64_t)Hv * dv) * es;
+  if (std::min(L, 64) * row > 1ll << 32) return GDN_ERR_SHAPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
   if (packed && !cu) return GDN_ERR_NULL;
-  const int64_t tok = packed ? (int64_t)L : (int64_t)nseq * L, es = esize(dtype);
   if (tok > 0) {
     if (!Q || !K || !V || !beta || !g || !dO || !dQ || !dK || !dV || !dbeta || !dg || !workspace)
       return GDN_ERR_NULL;

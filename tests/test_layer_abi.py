@@ -149,6 +149,23 @@ def test_packed_backward_s_largest_launch(dv, most):
                                            ws=None)) == NULL
 
 
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype,d,most", [(0, 128, 131072), (0, 64, 262144), (1, 128, 262144)])
+def test_backward_s_widest_rows(packed, dtype, d, most):
+    """A chunk's rows are reached by 32-bit byte offsets from its first: the rows of all heads
+    of the tokens of a chunk hold 2^32 bytes at most, of Q and K and of V."""
+    f = L.gdn_chunk_backward_varlen if packed else L.gdn_chunk_backward
+    base = packed_args(nseq=1) if packed else dict(BWD, B=1)
+    for wide in ("keys", "values"):
+        def code(heads, tokens):  # NULL: as far as the missing workspace
+            dims = dict(dk=d, dv=64, Hk=heads) if wide == "keys" else dict(dk=64, dv=d, Hk=1)
+            return call(f, dict(base, **dims, Hv=heads, L=tokens, dtype=dtype, ws=None))
+
+        assert (code(most, 64), code(most, 1000)) == (NULL, NULL)
+        assert (code(most + 1, 64), code(most + 1, 1000)) == (SHAPE, SHAPE)
+        assert code(most + 1, 63) == NULL  # the rows that there are
+
+
 def test_backward_workspace():
     tile = 4 * (6 * 768 + 5 * 64 + 2 * 64 * 128 + 2 * 128 * 128)
     assert G.gdn_chunk_backward_workspace(2, 100, 3, 128, 128) == 2 * 2 * 3 * tile
