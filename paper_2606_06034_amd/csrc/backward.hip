@@ -1045,7 +1045,7 @@ __global__ __launch_bounds__(256, 2) void k_bwd_grads_half(const BwdArgs a) {
 }
 
 int64_t backward_slots(int nseq, int L, bool packed) {
-  return packed ? (int64_t)L / BC + nseq : (int64_t)nseq * ((L + BC - 1) / BC);
+  return packed ? (int64_t)L / BC + nseq : nseq * (((int64_t)L + BC - 1) / BC);
 }
 int64_t backward_tile_bytes(int dk, int dv) { return ws_tile(dk, dv) * 4; }
 

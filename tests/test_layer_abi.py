@@ -176,6 +176,14 @@ def test_backward_workspace():
         G.gdn_chunk_backward_workspace(2, 100, 3, 96, 128)
 
 
+def test_backward_workspace_of_the_longest_lengths():
+    n = ctypes.c_int64(7)
+    for L_, Hv, packed, code in [(2 ** 31 - 1, 1, 0, SHAPE), (2 ** 31 - 1, 1, 1, SHAPE),
+                                 (2 ** 31 - 1, 0, 0, OK), (2 ** 29 - 64, 1, 0, OK)]:
+        assert L.gdn_chunk_backward_workspace(1, L_, Hv, 64, 64, packed, ctypes.byref(n)) == code
+    assert n.value == (2 ** 23 - 1) * 4 * (6 * 768 + 5 * 64 + 2 * 64 * 64 + 2 * 64 * 64)
+
+
 def test_binding_refuses_before_the_library():
     k, v = torch.zeros(2, 1, 2, 64), torch.zeros(2, 1, 4, 64)
     b = torch.zeros(2, 1, 4)
