@@ -58,6 +58,12 @@ int gdn_recurrent_forward(const void* Q, const void* K, const void* V, const flo
  * over its group of value heads.  Everything is formed in fp32 (bf16 inputs
  * enter unrounded) and rounded once at the end, in a fixed order: the same
  * call gives the same bits.
+ * A value that is not finite, of the inputs or by overflow on the way, makes
+ * what it reaches not finite either, an infinity NaN where bf16 inputs are
+ * multiplied (their products with fp32 values run as sums of bf16 terms, the
+ * second of which is inf - inf; so do finite ones from 2^128 - 2^119 on).  It
+ * reaches no other sequence, and no other value head but through dQ and dK of
+ * its key head.
  * workspace: at least gdn_chunk_backward_workspace() bytes, contents
  * undefined on return.  dk, dv in {64, 128}; the rows of all heads of 64 tokens
  * (of L where that is less) of Q and of V hold 4 GiB at most.  Three launches

@@ -7,6 +7,8 @@
 // below 2^-24 of the largest are left out), at 16 times the rate of the fp32
 // instruction: 5.3 and 2.7 times its speed at its accuracy.  With fp32 inputs
 // (F = f32x4) the same code runs on the fp32 instructions, one term each.
+// An infinity, or a value that rounds to one in bf16, leaves a second term of inf -
+// inf: products with it are NaN.
 #pragma once
 
 #include "tile16.hpp"

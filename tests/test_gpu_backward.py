@@ -329,3 +329,30 @@ def test_a_bad_offset_leaves_the_other_sequences(dt, cu, valid):
         assert (a[0][rest] == 7).all()
     for s in set(range(n)) - set(valid):
         assert torch.equal(got[5][s], x["dS"][s])
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("name,value", [
+    ("V", float("inf")), ("dO", -float("inf")), ("S0", float("inf")), ("dS", float("inf")),
+    ("S0", float(np.finfo(np.float32).max)), ("Q", float("inf")), ("beta", float("nan"))])
+def test_what_is_not_finite_stays_in_its_heads(dt, name, value):
+    x = make([130, 130], 2, 4, 64, 64, 64, dt, 10)
+    clean = run(x, [130, 130], 64, 0.5, False)
+    if name in ("S0", "dS"):
+        x[name][1, 1, 5, 7] = value  # sequence 1, value head 1 (key head 0)
+    elif name == "beta":
+        x[name][140, 1] = value
+    else:
+        x[name][140, 0 if name == "Q" else 1, 7] = value
+    got = run(x, [130, 130], 64, 0.5, False)
+    kept = (2, 3) if name == "Q" else (0, 2, 3)  # value heads that do not have it
+    for n, a, b in zip(NAMES, got, clean):
+        assert torch.equal(a[0], b[0]), n
+        if n in ("dQ", "dK"):
+            assert torch.equal(a[1][:, 1], b[1][:, 1]), n
+        else:
+            heads = a[1].movedim(-3, 0) if n == "dS0" else a[1].movedim(1, 0)
+            was = b[1].movedim(-3, 0) if n == "dS0" else b[1].movedim(1, 0)
+            assert all(torch.equal(heads[h], was[h]) for h in kept), n
+    if value != np.finfo(np.float32).max:
+        assert not all(torch.isfinite(a).all() for a in got)
