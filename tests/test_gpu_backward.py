@@ -299,6 +299,46 @@ def test_on_another_stream_in_a_graph_and_the_same_every_time():
         assert all(torch.equal(a, b) for a, b in zip(out, ref)), i
 
 
+def check_heads(x, lens, C, got, dt, picks):
+    """Sequences s and key heads hk of `picks` with their value heads, against the oracle."""
+    r = x["V"].shape[1] // x["K"].shape[1]
+    for s, hk in picks:
+        t = sum(lens[:s])
+        w, hv = slice(t, t + lens[s]), slice(hk * r, (hk + 1) * r)
+        sub = {k: (v[s:s + 1, hv] if k in ("S0", "dS") else
+                   v[w, hk:hk + 1] if k in ("Q", "K") else v[w, hv]) for k, v in x.items()}
+        flat = [a.reshape((-1,) + tuple(a.shape[2:])) for a in got[:5]]
+        part = [a[w, hk:hk + 1] if i < 2 else a[w, hv] for i, a in enumerate(flat)]
+        compare(part + [got[5][s:s + 1, hv]], oracle(sub, [lens[s]], C, 0.3), dt)
+
+
+@pytest.mark.parametrize("B,L,Hk,Hv,dk,dv", [
+    (4, 130, 4, 8, 128, 128), (3, 130, 11, 11, 128, 128), (16, 65, 4, 4, 64, 64),
+    (5, 65, 13, 13, 64, 64), (8, 65, 4, 4, 128, 128), (16, 65, 8, 8, 64, 64),
+    (1, 65, 129, 129, 64, 64)])
+def test_either_side_of_the_launch_rules(B, L, Hk, Hv, dk, dv):
+    """Equal lengths in bf16: up to 256 slices of 16 value columns are walked by teams, more
+    by lone waves; up to 256 chunks by key heads have their gradients from workgroups of
+    eight waves, more from ones of four.  Both sides of both, as near as whole heads come."""
+    slices, tiles = B * Hv * dv // 16, B * ((L + 63) // 64) * Hk
+    assert slices in (256, 260, 264, 512, 516) and tiles in (48, 64, 99, 128, 130, 256, 258)
+    x = make([L] * B, Hk, Hv, dk, dv, 64, "bf16", B + Hv)
+    got = run(x, [L] * B, 64, 0.3, False)
+    check_heads(x, [L] * B, 64, got, "bf16", [(0, 0), (B - 1, Hk - 1), (B // 2, Hk // 2)])
+
+
+@pytest.mark.parametrize("dk,dv,Hv", [(128, 128, 12), (64, 64, 24), (128, 64, 24)])
+def test_packed_sequences_at_the_length_that_parts_the_walks(dk, dv, Hv):
+    """In bf16, sequences of more than tokens * slices a sequence / 30000 chunks are walked by
+    teams and the others by lone waves: exactly that many, one more, and their neighbours."""
+    lens = [192, 193, 129, 256, 1, 229]
+    assert sum(lens) * Hv * (dv // 16) // 30000 == 3
+    assert sorted((m + 63) // 64 for m in lens) == [1, 3, 3, 4, 4, 4]
+    x = make(lens, Hv // 3, Hv, dk, dv, 64, "bf16", dk + Hv)
+    got = run(x, lens, 64, 0.3, True)
+    check_heads(x, lens, 64, got, "bf16", [(s, s % (Hv // 3)) for s in range(len(lens))])
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("cu,valid", [
     ([0, 200, 9999, 300, 400], (0, 3)), ([0, 200, -1, 300, 400], (0, 3)),

@@ -106,3 +106,14 @@ def test_backward_gradients_share_a_cu(kernels):
     assert len(half) == 4  # widths
     for name, k in half.items():
         assert per_cu(k) >= 2 and k[".vgpr_spill_count"] == 0, name
+
+
+def test_backward_keeps_its_values_in_registers(kernels):
+    """Of the backward pass only the packed walks have scratch: two values of a lane that
+    the walk's loop does not use, stored before and read again beside it."""
+    names = {n for n in kernels if "k_bwd_" in n}
+    assert len(names) == 36  # 4 widths: 2 of fp32's and bf16's, 4 of bf16's and one of fp32's own
+    for n in names:
+        k, most = kernels[n], 12 if "k_bwd_mixedILi128E" in n else 0
+        assert k[".private_segment_fixed_size"] <= most, n
+        assert k[".vgpr_spill_count"] <= most // 6, n
