@@ -144,17 +144,26 @@ def _stream(stream) -> int:
 
 
 def _on_stream(stream, fn, args: dict):
-    """fn(**args) with `stream` current, for a call that names one: what the call allocates
-    (and drops, a workspace) then belongs to the stream that its kernels run on, so that the
-    allocator does not hand it to other work before they end.  The results are marked as used
-    on the stream that was current too, which is where the caller goes on with them."""
+    """fn(**args) with `stream` current, for a call that names one and allocates: what it
+    allocates (and drops, a workspace) then belongs to the stream that its kernels run on, so
+    that the allocator does not hand it to other work before they end.  The results are marked
+    as used on the stream that was current too, which is where the caller goes on with them.
+    (Set and set back by hand: the context manager takes 6 us.)"""
+    args = {**args, "stream": None}
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(stream.cuda_stream)
     before = torch.cuda.current_stream()
-    with torch.cuda.stream(stream):
-        out = fn(**{**args, "stream": None})
     if stream == before:
-        return out
+        return fn(**args)
+    same = stream.device_index == before.device_index
+    there = before if same else torch.cuda.current_stream(stream.device)
+    torch.cuda.set_stream(stream)
+    try:
+        out = fn(**args)
+    finally:
+        torch.cuda.set_stream(there)
+        if not same:
+            torch.cuda.set_stream(before)  # and the device with it
     for t in out if isinstance(out, tuple) else (out,):
         if t is not None:
             t.record_stream(before)
@@ -172,7 +181,7 @@ def gdn_build_A(K: torch.Tensor, beta: torch.Tensor, g: torch.Tensor, C: int,
                 a_dtype: Optional[torch.dtype] = None, A: Optional[torch.Tensor] = None,
                 stream=None) -> torch.Tensor:
     """A [B, H, L/C, C, C] from K [B, L, H, dk], beta, g [B, L, H] (fp32)."""
-    if stream is not None:
+    if stream is not None and A is None:
         return _on_stream(stream, gdn_build_A, locals())
     B, L, H, dk = K.shape
     kdt = _fdtype(K, "K")
@@ -190,7 +199,7 @@ def gdn_build_A(K: torch.Tensor, beta: torch.Tensor, g: torch.Tensor, C: int,
 def gdn_chunk_inverse_neumann(A: torch.Tensor, N: int, S: int, Tinv: Optional[torch.Tensor] = None,
                               stream=None) -> torch.Tensor:
     """T_hat(N, S) of every C x C tile of A (same shape and dtype)."""
-    if stream is not None:
+    if stream is not None and Tinv is None:
         return _on_stream(stream, gdn_chunk_inverse_neumann, locals())
     n, C = _tiles(A)
     dt = _fdtype(A, "A")
@@ -204,7 +213,7 @@ def gdn_chunk_inverse_neumann(A: torch.Tensor, N: int, S: int, Tinv: Optional[to
 def gdn_chunk_inverse_fwdsub(A: torch.Tensor, Tinv: Optional[torch.Tensor] = None,
                              stream=None) -> torch.Tensor:
     """Exact (I + A)^-1 of every tile by forward substitution."""
-    if stream is not None:
+    if stream is not None and Tinv is None:
         return _on_stream(stream, gdn_chunk_inverse_fwdsub, locals())
     n, C = _tiles(A)
     dt = _fdtype(A, "A")
@@ -218,7 +227,7 @@ def gdn_chunk_inverse_fwdsub(A: torch.Tensor, Tinv: Optional[torch.Tensor] = Non
 def gdn_chunk_inverse_blockwise(A: torch.Tensor, Tinv: Optional[torch.Tensor] = None,
                                 stream=None) -> torch.Tensor:
     """Exact (I + A)^-1 of every tile by 16 x 16 block recursion (products only)."""
-    if stream is not None:
+    if stream is not None and Tinv is None:
         return _on_stream(stream, gdn_chunk_inverse_blockwise, locals())
     n, C = _tiles(A)
     dt = _fdtype(A, "A")
@@ -233,7 +242,7 @@ def gdn_wy_apply(Tinv: torch.Tensor, K: torch.Tensor, V: torch.Tensor, beta: tor
                  W: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
                  stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """W = T diag(beta) K, U = T diag(beta) V per chunk."""
-    if stream is not None:
+    if stream is not None and (W is None or U is None):
         return _on_stream(stream, gdn_wy_apply, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
@@ -254,7 +263,7 @@ def gdn_chunk_wy_fused(K: torch.Tensor, V: torch.Tensor, beta: torch.Tensor, g: 
                        W: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
                        Tinv: Optional[torch.Tensor] = None, stream=None):
     """Fused build A -> T_hat(N, S) -> (W, U[, Tinv])."""
-    if stream is not None:
+    if stream is not None and (W is None or U is None or want_T and Tinv is None):
         return _on_stream(stream, gdn_chunk_wy_fused, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
@@ -278,7 +287,7 @@ def gdn_chunk_wy_fused_blockwise(K: torch.Tensor, V: torch.Tensor, beta: torch.T
                                  W: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
                                  Tinv: Optional[torch.Tensor] = None, stream=None):
     """Fused build A -> exact inverse (block-wise) -> (W, U[, Tinv])."""
-    if stream is not None:
+    if stream is not None and (W is None or U is None or want_T and Tinv is None):
         return _on_stream(stream, gdn_chunk_wy_fused_blockwise, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
@@ -306,7 +315,7 @@ def gdn_quantize_tiles_i8(A: torch.Tensor, Aq: Optional[torch.Tensor] = None,
                           eA: Optional[torch.Tensor] = None, stream=None):
     """(Aq int8 tiles, eA int32 per tile) with A ~ Aq * 2^eA; C = 128:
     eA [n, 3], one exponent per block (11, 21, 22)."""
-    if stream is not None:
+    if stream is not None and (Aq is None or eA is None):
         return _on_stream(stream, gdn_quantize_tiles_i8, locals())
     n, C = _tiles(A)
     ne = _nexp(C)
@@ -327,7 +336,7 @@ def gdn_chunk_inverse_neumann_i8(Aq: torch.Tensor, eA: torch.Tensor, N: int, S: 
     """(Tq int8, eT int32[, Tdeq fp32]) with T_hat = I + Tq * 2^eT (plain:
     T_hat = Tq * 2^eT, the diagonal in the codes; GDN_INT_PLAIN); C = 128:
     block-wise, eA and eT [n, 3] (blocks 11, 21, 22)."""
-    if stream is not None:
+    if stream is not None and (Tq is None or eT is None or want_deq and Tdeq is None):
         return _on_stream(stream, gdn_chunk_inverse_neumann_i8, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
@@ -351,7 +360,7 @@ def gdn_chunk_inverse_neumann_i8_fused(K: torch.Tensor, beta: torch.Tensor, g: t
                                        Tdeq: Optional[torch.Tensor] = None, stream=None):
     """K [B, L, H, dk] -> (Tq int8 [B, H, L/C, C, C], eT int32[, Tdeq fp32]):
     build A, quantise and invert in one launch."""
-    if stream is not None:
+    if stream is not None and (Tq is None or eT is None or want_deq and Tdeq is None):
         return _on_stream(stream, gdn_chunk_inverse_neumann_i8_fused, locals())
     B, L, H, dk = K.shape
     nc = L // C if C else 0
@@ -377,7 +386,7 @@ def gdn_quantize_tiles_i16(A: torch.Tensor, Aq: Optional[torch.Tensor] = None,
                            eA: Optional[torch.Tensor] = None, stream=None):
     """(Aq int16 tiles, eA int32 per tile) with A ~ Aq * 2^eA; C = 128:
     eA [n, 3], one exponent per block (11, 21, 22)."""
-    if stream is not None:
+    if stream is not None and (Aq is None or eA is None):
         return _on_stream(stream, gdn_quantize_tiles_i16, locals())
     n, C = _tiles(A)
     ne = _nexp(C)
@@ -398,7 +407,7 @@ def gdn_chunk_inverse_neumann_i16(Aq: torch.Tensor, eA: torch.Tensor, N: int, S:
     """(Tq int16, eT int32[, Tdeq fp32]) with T_hat = I + Tq * 2^eT (plain:
     T_hat = Tq * 2^eT, the diagonal in the codes; GDN_INT_PLAIN); C = 128:
     block-wise, eA and eT [n, 3] (blocks 11, 21, 22)."""
-    if stream is not None:
+    if stream is not None and (Tq is None or eT is None or want_deq and Tdeq is None):
         return _on_stream(stream, gdn_chunk_inverse_neumann_i16, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
@@ -421,7 +430,7 @@ def gdn_chunk_inverse_fwdsub_i16(Aq: torch.Tensor, eA: torch.Tensor, want_deq: b
                                  Tdeq: Optional[torch.Tensor] = None, stream=None):
     """(Tq int16, eT int32[, Tdeq fp32]): integer forward substitution,
     T = I + Tq * 2^eT."""
-    if stream is not None:
+    if stream is not None and (Tq is None or eT is None or want_deq and Tdeq is None):
         return _on_stream(stream, gdn_chunk_inverse_fwdsub_i16, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
@@ -443,7 +452,7 @@ def gdn_chunk_inverse_fwdsub_i8(Aq: torch.Tensor, eA: torch.Tensor, want_deq: bo
                                 Tdeq: Optional[torch.Tensor] = None, stream=None):
     """(Tq int8, eT int32[, Tdeq fp32]): integer forward substitution,
     T = I + Tq * 2^eT."""
-    if stream is not None:
+    if stream is not None and (Tq is None or eT is None or want_deq and Tdeq is None):
         return _on_stream(stream, gdn_chunk_inverse_fwdsub_i8, locals())
     n, C = _tiles(Aq)
     Tq = torch.empty_like(Aq) if Tq is None else Tq
@@ -466,7 +475,7 @@ def gdn_chunk_inverse_neumann_i16_fused(K: torch.Tensor, beta: torch.Tensor, g: 
                                         Tdeq: Optional[torch.Tensor] = None, stream=None):
     """K [B, L, H, dk] -> (Tq int16 [B, H, L/C, C, C], eT int32[, Tdeq fp32]):
     build A, quantise and invert in one launch."""
-    if stream is not None:
+    if stream is not None and (Tq is None or eT is None or want_deq and Tdeq is None):
         return _on_stream(stream, gdn_chunk_inverse_neumann_i16_fused, locals())
     B, L, H, dk = K.shape
     nc = L // C if C else 0
@@ -523,7 +532,7 @@ def gdn_chunk_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, beta: t
     workspace (a byte tensor of gdn_chunk_forward_workspace() bytes) is allocated when
     not given.  inverse: "neumann" (default), "exact" (as exact=True), "int16" or "int8"
     (the integer T_hat(N, S) inside the layer)."""
-    if stream is not None:
+    if stream is not None and (O is None or workspace is None or want_state and S_final is None):
         return _on_stream(stream, gdn_chunk_forward, locals())
     B, L, H, dk = K.shape
     dv = V.shape[-1]
@@ -611,7 +620,7 @@ def gdn_chunk_forward_state(Q: torch.Tensor, g: torch.Tensor, C: int, workspace:
                             O: Optional[torch.Tensor] = None,
                             S_final: Optional[torch.Tensor] = None, stream=None):
     """Second phase of gdn_chunk_forward: the state pass over a prepared workspace."""
-    if stream is not None:
+    if stream is not None and (O is None or want_state and S_final is None):
         return _on_stream(stream, gdn_chunk_forward_state, locals())
     B, L, H, dk = Q.shape
     dt = _fdtype(Q, "Q")
@@ -651,7 +660,7 @@ def gdn_chunk_wy_fused_varlen(K: torch.Tensor, V: torch.Tensor, beta: torch.Tens
                               Tinv: Optional[torch.Tensor] = None, stream=None):
     """Fused build A -> inverse -> (W, U[, Tinv]) over packed sequences;
     tables = gdn_varlen_tables(cu_seqlens, C)."""
-    if stream is not None:
+    if stream is not None and (W is None or U is None or want_T and Tinv is None):
         return _on_stream(stream, gdn_chunk_wy_fused_varlen, locals())
     dcu, doff, n_chunks = tables
     B, T, H, dk = K.shape
@@ -691,7 +700,7 @@ def gdn_chunk_forward_varlen(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
     """Layer forward over packed sequences: (O [1, T, H, dv], S_final
     [nseq, H, dk, dv] fp32 or None); tables = gdn_varlen_tables(cu_seqlens, C).
     Defaults and inverse modes as gdn_chunk_forward."""
-    if stream is not None:
+    if stream is not None and (O is None or workspace is None or want_state and S_final is None):
         return _on_stream(stream, gdn_chunk_forward_varlen, locals())
     dcu, doff, n_chunks = tables
     B, T, H, dk = K.shape

@@ -81,7 +81,7 @@ def gdn_recurrent_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, bet
     (int32 [nseq] on the device) they are pools [n_states, Hv, dk, dv], sequence s reads and
     writes state slots[s], an index outside the pool marks a padded sequence (O zeros), and
     S_final has to be given (S0 itself, for a pool updated in place)."""
-    if stream is not None:
+    if stream is not None and (O is None or want_state and S_final is None):
         return _on_stream(stream, gdn_recurrent_forward, locals())
     B, T, Hk, dk = K.shape
     Hv, dv = V.shape[-2:]
@@ -172,7 +172,7 @@ def gdn_chunk_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, beta: 
     dO [B, L, Hv, dv], beta, g [B, L, Hv]; L need not be a multiple of C.  out: the six outputs
     (None where one is to be allocated).  The workspace (a byte tensor of
     gdn_chunk_backward_workspace() bytes) is allocated when not given."""
-    if stream is not None:
+    if stream is not None and (workspace is None or out is None or any(t is None for t in out)):
         return _on_stream(stream, gdn_chunk_backward, locals())
     return _backward("gdn_chunk_backward", Q, K, V, beta, g, dO, C, None, S0, dS_final, scale,
                      want_dS0, out, workspace, stream)
@@ -186,7 +186,7 @@ def gdn_chunk_backward_varlen(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
                               workspace: Optional[torch.Tensor] = None, stream=None):
     """The same over packed sequences (B = 1): tables = gdn_varlen_tables(cu_seqlens, C), of
     which the token offsets are read; S0, dS_final, dS0 [nseq, Hv, dk, dv]."""
-    if stream is not None:
+    if stream is not None and (workspace is None or out is None or any(t is None for t in out)):
         return _on_stream(stream, gdn_chunk_backward_varlen, locals())
     if K.shape[0] != 1:
         raise ValueError("packed sequences use B = 1")
@@ -219,7 +219,7 @@ def gdn_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     """(y, mean, rstd): the norm of x over its last dimension ("layer" or "rms"), times weight,
     plus bias, times silu(gate).  mean (None for "rms") and rstd, fp32 [x.shape[:-1]], are what
     gdn_norm_backward takes (None with want_stats=False)."""
-    if stream is not None:
+    if stream is not None and (y is None or want_stats):
         return _on_stream(stream, gdn_norm_forward, locals())
     k, D = _kind(kind), x.shape[-1]
     dt = _fdtype(x, "x")

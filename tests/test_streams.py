@@ -6,8 +6,6 @@ call returns and drops it, while the kernels still use it.  On the CPU the calls
 run up to the library with the streams played by a stack; on the GPU the memory
 of a dropped workspace is looked for in what the caller's stream gets next."""
 
-import contextlib
-
 import pytest
 import torch
 
@@ -33,6 +31,8 @@ class Library:
 
 
 class Stream:
+    device_index, device = 0, "cuda:0"
+
     def __init__(self, number):
         self.cuda_stream = number
 
@@ -40,23 +40,17 @@ class Stream:
 @pytest.fixture
 def played(monkeypatch):
     """Streams without a GPU: every allocation and launch with the stream it was made on."""
-    stack, log = [Stream(1)], []
-
-    @contextlib.contextmanager
-    def on(stream):
-        stack.append(stream)
-        yield
-        stack.pop()
+    now, log = [Stream(1)], []
 
     def noting(make):
         def f(*a, **k):
             t = make(*a, **k)
-            log.append((t.data_ptr(), stack[-1].cuda_stream))
+            log.append((t.data_ptr(), now[-1].cuda_stream))
             return t
 
         return f
 
-    lib = Library(lambda: stack[-1])
+    lib = Library(lambda: now[-1])
     marked = []
     for name in ("empty", "empty_like"):
         monkeypatch.setattr(torch, name, noting(getattr(torch, name)))
@@ -65,8 +59,8 @@ def played(monkeypatch):
     monkeypatch.setattr(torch.Tensor, "record_stream",
                         lambda t, s: marked.append((t.data_ptr(), s.cuda_stream)))
     monkeypatch.setattr(torch.cuda, "Stream", Stream)
-    monkeypatch.setattr(torch.cuda, "stream", on)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda: stack[-1])
+    monkeypatch.setattr(torch.cuda, "set_stream", now.append)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: now[-1])
     monkeypatch.setattr(_layer, "_raw_stream", None)
     for m in (_binding, _layer):
         monkeypatch.setattr(m, "lib", lib)
@@ -222,3 +216,19 @@ def test_a_stream_from_outside_torch():
     got = call(Foreign())
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, call(None)))
+
+
+def test_a_call_that_allocates_nothing_changes_no_stream(played, monkeypatch):
+    lib, log, marked = played
+    x = operands()
+    seq = [x[k] for k in ("Q", "K", "V", "beta", "g")]
+    O, S = torch.zeros_like(x["V"]), torch.zeros(1, 2, 64, 64)
+    out = [torch.zeros_like(t) for t in seq] + [S]
+    ws = torch.zeros(G.gdn_chunk_backward_workspace(1, 128, 2, 64, 64), dtype=torch.uint8)
+    monkeypatch.setattr(torch.cuda, "set_stream", None)
+    log.clear()
+    G.gdn_recurrent_forward(*seq, S0=S, S_final=S, O=O, stream=Stream(2))
+    G.gdn_chunk_backward(*seq, x["dO"], 64, want_dS0=True, out=out, workspace=ws, stream=Stream(2))
+    G.gdn_norm_forward(x["V"], y=O, want_stats=False, stream=Stream(2))
+    G.gdn_chunk_forward(*seq, 64, O=O, S_final=S, workspace=ws, stream=Stream(2))
+    assert lib.launched == [2] * 4 and not log and not marked
