@@ -233,7 +233,7 @@ __device__ __forceinline__ float part_sum(const float* dgamma, int r, int m, int
 // products with the states are done, and then take the place of dO and dZ.
 // Bound: the instructions of two waves a SIMD (a workgroup fills a CU's LDS), which are in
 // the same phase, so that one's vector work hides little of the other's matrix work:
-// 45000 cycles a chunk, 20 us.  (Asking for the next chunk's operands a chunk ahead, and
+// 20 us a chunk.  (Asking for the next chunk's operands a chunk ahead, and
 // the two waves at different priorities, changed nothing.)
 template <int DK, int DV, typename T>
 struct Grads {
@@ -655,10 +655,10 @@ __global__ __launch_bounds__(512) void k_bwd_grads(const BwdArgs a) {
 // place of what they were formed from one after the other.  The states' terms are those
 // of S, then those of dS: both at once, or the next pair's states asked for ahead, went
 // to scratch (168 us became 185 and more).
-// Bound: vector instructions (36% of the cycles), matrix instructions (27%), LDS (27%) of
+// Bound: vector instructions (37% of the cycles), matrix instructions (27%), LDS (28%) of
 // two waves a SIMD, and their waits for memory.  8192 tokens of 16 heads of 128 by 128 in
-// bf16 take 168 us, 290 KB a chunk and head at 3.5 TB/s; 4 x 8192 of 32 value heads 1.4 ms,
-// 4.2 TB/s.
+// bf16 take 173 us, 300 KB a chunk and head at 3.6 TB/s; 4 x 8192 of 32 value heads 1.33 ms,
+// 4.3 TB/s (42, 31 and 31%).
 template <int DK, int DV>
 struct Halves {
   static constexpr int NC = DK / 32, RG = 4 / NC, NR = 4 / RG, LDK = DK + 8;

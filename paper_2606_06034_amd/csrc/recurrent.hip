@@ -15,9 +15,11 @@
 //
 // Bound: the state is read and written once a call, 8 bytes for 7 flops a token.
 // One token is HBM traffic: 256 sequences of 32 heads of 128 by 128, 1.08 GB, take
-// 199 us, 5.4 TB/s.  A further token is 350 vector instructions of a wave: 48
-// sequences of 1 to 8 tokens, 21 heads of 128 by 64 (two waves a SIMD), 68 MB, take
-// 19 us, of which the tokens are 9.
+// 199 us, 5.4 TB/s.  A further token is 413 vector instructions of a wave, which
+// take 432 slots of 4 cycles: 48 sequences of 21 heads of 128 by 64 (two waves a
+// SIMD) take 10 us for a token each, 21 for 8 and 191 for 128, where the vector
+// units are busy all the time and a token is 1.4 us.  1 to 8 tokens of them, 68 MB,
+// take 19 us.
 #include "lanes.hpp"
 #include "launch.hpp"
 #include "layer.hpp"

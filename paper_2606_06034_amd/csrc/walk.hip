@@ -5,8 +5,8 @@
 //
 // Bound: a chunk's step is a chain of three dependent products, K S, T Z and K^T Y
 // (K dS, T^T dY and K^T dX), a hundred kilobytes of operands apart from the next,
-// in the one wave or two that own the slice's state; past as many slices as SIMDs,
-// HBM (the states themselves: 64 KB a chunk): 4 x 8192 tokens of 32 heads of 128 by
+// in the one wave or the team of four that owns the slice's state; past as many
+// slices as SIMDs, HBM (the states themselves: 64 KB a chunk): 4 x 8192 tokens of 32 heads of 128 by
 // 128 in bf16 take 1.29 ms and move 6 GB, 4.7 TB/s.
 #include "backward.hpp"
 
@@ -1024,7 +1024,9 @@ __global__ __launch_bounds__(384) void k_bwd_lone(const BwdArgs a) {
 }
 
 // Packed sequences: those of more than `longest` chunks by teams, first, the others by
-// lone waves; the workgroups of the other kind end at once.
+// lone waves; the workgroups of the other kind end at once.  (One allocation of registers
+// for both: at DK = 128 two values of a lone wave lie in scratch while its loop runs, which
+// does not use them.)
 template <int DK, int DV>
 __global__ __launch_bounds__(512) void k_bwd_mixed(const BwdArgs a, int longest) {
   typedef Team<DK, DV, true> TR;
@@ -1079,7 +1081,8 @@ static hipError_t run_walks(const BwdArgs& a, int dtype, hipStream_t st) {
   // chunks alone takes 6 c us.  Those that take longer than all together go to teams (the
   // factor is the one that measured best).  8192 tokens of 16 heads by teams alone, lone
   // waves alone, and so: 22 sequences 376, 345, 267 us; 31 372, 321, 277; 9 of at most 30
-  // chunks 298, 180, 187; 4 292, 299, 340; 8 heads in 11 sequences 155, 255, 144.
+  // chunks 298, 180, 187; 4 292, 299, 340 (so of few long ones the worst of the three); 8
+  // heads in 11 sequences 155, 255, 144.  (Measured for DK = DV = 128.)
   const int64_t longest = (int64_t)a.L * a.Hv * (DV / 16) / 30000;
   if (dtype == 0)
     hipLaunchKernelGGL((k_bwd_walks_f32<DK, DV>), dim3(n * (DV / 16), both), dim3(256), 0, st, a);
