@@ -172,7 +172,7 @@ int gdn_norm_forward(const void* x, const void* w, const void* b, const void* z,
 int gdn_norm_backward_workspace(int64_t rows, int D, int64_t* bytes) {
   if (!bytes) return GDN_ERR_NULL;
   if (int r = check_norm(rows, D, GDN_NORM_RMS, GDN_F32, GDN_F32)) return r;
-  *bytes = (int64_t)gdn::norm_backward_parts(rows, D) * D * 2 * 4;
+  *bytes = (int64_t)gdn::norm_backward_parts(rows) * D * 2 * 4;
   return GDN_OK;
 }
 

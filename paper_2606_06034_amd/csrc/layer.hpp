@@ -20,7 +20,7 @@ hipError_t launch_norm_backward(const void* dy, const void* x, const void* w, co
                                 float* dw, float* db, void* dz, float* ws, int64_t rows, int D,
                                 bool rms, int dtype, int w_dtype, hipStream_t st);
 // rows of partial sums of dw (and as many of db) that launch_norm_backward writes
-int norm_backward_parts(int64_t rows, int D);
+int norm_backward_parts(int64_t rows);
 
 // Chunk-wise backward pass; ws holds backward_slots() * Hv tiles of
 // backward_tile_bytes().  cu (nullable): nseq + 1 token offsets on the device,

@@ -505,7 +505,7 @@ __global__ __launch_bounds__(256) void k_norm_parts(const float* __restrict__ ws
   }
 }
 
-int norm_backward_parts(int64_t rows, int) { return (int)(rows < kParts ? rows : kParts); }
+int norm_backward_parts(int64_t rows) { return (int)(rows < kParts ? rows : kParts); }
 
 // TPR threads and NV pieces a thread for a row of n 16-byte pieces: a short
 // row takes part of a wave, so that a wave's loads stay 16 bytes a lane
@@ -533,7 +533,7 @@ static hipError_t norm_forward(const NormArgs& a, hipStream_t st) {
 template <typename T>
 static hipError_t norm_backward(const NormArgs& a, int want, hipStream_t st) {
   const int n = (a.D + Piece<T>::E - 1) / Piece<T>::E;
-  const int parts = norm_backward_parts(a.rows, a.D);
+  const int parts = norm_backward_parts(a.rows);
   const bool bias = a.b || (want & 2);
 #define GDN_G(TPR, NV, GATE, BIAS)                                                          \
   hipLaunchKernelGGL((k_norm_grad<T, TPR, NV, 1024, GATE, BIAS>), dim3((unsigned)parts),    \
@@ -582,7 +582,7 @@ hipError_t launch_norm_backward(const void* dy, const void* x, const void* w, co
   }
   if (want) {
     hipLaunchKernelGGL(k_norm_parts, dim3((unsigned)((D + 15) / 16), 2), dim3(256), 0, st, ws, dw,
-                       db, norm_backward_parts(rows, D), D);
+                       db, norm_backward_parts(rows), D);
     return hipGetLastError();
   }
   return hipSuccess;
