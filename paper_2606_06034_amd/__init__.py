@@ -59,3 +59,17 @@ from ._layer import (  # noqa: F401
     gdn_recurrent_forward,
     layer_abi_symbols,
 )
+from ._linear import (  # noqa: F401
+    GDN_ACT_NONE,
+    GDN_ACT_SILU,
+    gdn_group_norm_backward,
+    gdn_group_norm_backward_workspace,
+    gdn_group_norm_forward,
+    gdn_group_norm_forward_workspace,
+    gdn_linear_backward,
+    gdn_linear_backward_workspace,
+    gdn_linear_forward,
+    gdn_linear_forward_workspace,
+    gdn_linear_recurrent,
+    linear_abi_symbols,
+)

@@ -10,38 +10,7 @@
 #include "checks.hpp"
 #include "layer.hpp"
 
-namespace {
-
 using namespace gdn::checks;
-
-// a device array of the call: its address and bytes
-struct Span {
-  const void* p;
-  int64_t bytes;
-};
-
-// every array aligned; no output overlaps an input or another output, but for
-// output same_out and input same_in where these are one array
-int check_spans(const Span* in, int ni, const Span* out, int no, int same_out = -1,
-                int same_in = -1) {
-  for (int i = 0; i < ni; ++i)
-    if (in[i].p && !aligned(in[i].p)) return GDN_ERR_ALIGN;
-  for (int o = 0; o < no; ++o)
-    if (out[o].p && !aligned(out[o].p)) return GDN_ERR_ALIGN;
-  for (int o = 0; o < no; ++o) {
-    for (int i = 0; i < ni; ++i) {
-      if (o == same_out && i == same_in && out[o].p == in[i].p) continue;
-      if (overlap(out[o].p, out[o].bytes, in[i].p, in[i].bytes)) return GDN_ERR_ALIAS;
-    }
-    for (int q = o + 1; q < no; ++q)
-      if (overlap(out[o].p, out[o].bytes, out[q].p, out[q].bytes)) return GDN_ERR_ALIAS;
-  }
-  return GDN_OK;
-}
-
-bool valid_heads(int Hk, int Hv) { return Hk >= 0 && Hv >= 0 && (Hk ? Hv % Hk == 0 : Hv == 0); }
-
-}  // namespace
 
 extern "C" {
 

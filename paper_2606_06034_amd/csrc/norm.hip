@@ -20,6 +20,7 @@
 #include "lanes.hpp"
 #include "launch.hpp"
 #include "layer.hpp"
+#include "norm.hpp"
 #include "tile16.hpp"
 
 namespace gdn {
@@ -98,13 +99,6 @@ __device__ __forceinline__ void load_param(float (&x)[E], const void* p, bool bf
   } else {
     load_piece<float, E>(x, (const float*)p, e, D);
   }
-}
-
-// 1 / (1 + e^-z).  The exponential and the reciprocal are the hardware's (1
-// ulp, and |z| 6e-8 from the scaled argument): the exact ones made the
-// vector operations as long as the memory traffic.
-__device__ __forceinline__ float sigmoid(float z) {
-  return __builtin_amdgcn_rcpf(1.f + __expf(-z));
 }
 
 // Sums over the TPR threads of a row, the same in each of them.  Past one wave
