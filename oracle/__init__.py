@@ -27,6 +27,8 @@ Modules:
         (token recurrence, and the chunk-wise form around the inverse).
   layer  float64 oracle of the operators around the layer: the recurrence over
         states, its gradients, the norms and theirs.
+  linear  float64 oracle of linear attention with a decay for each head and of
+        group norm, channels last, with their gradients.
   varlen  the chunk path over packed variable-length sequences (partial last
         chunks).
 """
@@ -35,4 +37,5 @@ from . import gdn  # noqa: F401
 from . import int8  # noqa: F401
 from . import gdn_forward  # noqa: F401
 from . import layer  # noqa: F401
+from . import linear  # noqa: F401
 from . import varlen  # noqa: F401

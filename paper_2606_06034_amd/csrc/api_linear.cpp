@@ -220,6 +220,7 @@ int gdn_group_norm_backward(const void* dy, const void* x, const void* w, const 
   if (!fdtype(w_dtype)) return GDN_ERR_DTYPE;
   if (act != GDN_ACT_NONE && act != GDN_ACT_SILU) return GDN_ERR_PARAM;
   if (!grid_ok(gdn::group_backward_blocks(N, S, G, C / G, dtype), 256)) return GDN_ERR_SHAPE;
+  if (N == 0 && !dw && !db) return GDN_OK;
   int64_t need = 4 * gdn::group_backward_workspace(N, S, G, C / G, dtype);
   if (N > 0) {
     if (!dy || !x || !mean || !rstd || !dx || (z && !dz) || !workspace) return GDN_ERR_NULL;

@@ -9,11 +9,16 @@
 //   dK: Q <- V, K <- dO, V <- Q and dV: Q <- K, K <- Q, V <- dO in reversed time, states dS^T
 //   and dS (the gradient of the state leaving the chunk), s_out = 1, s_in = scale.
 // Reversed, row r is the chunk's token m - 1 - r, and with H the sum of g over the rows
-// before r all of the above holds as it stands.  The gradient of g is
-//   dg_t = sum over i >= t of (q_i . dQ_i - k_i . dK_i) + <S, dS> at the end of the segment.
-// What tokens of one chunk give each other cancels in that sum past the chunk, so that only
-// what came through the states is carried from chunk to chunk (else the roundings of a whole
-// segment pile up on the gradients of fast-forgetting heads).
+// before r all of the above holds as it stands.  The gradient of a token's g is
+// the sum over what passes the token: pairs of tokens i >= t > j of its chunk, what the state
+// that enters the chunk gives tokens i >= t, what tokens j < t give the state that leaves, and
+// what passes the chunk:
+//   dg_t = sum_{i >= t > j} M_ij + sum_{i >= t} q_i . dQs_i + sum_{j < t} k_j . dKs_j + X,
+//   M = ((Q K^T) (.) (scale dO V^T) (.) D), X = e^total <S, dS>, dQs and dKs the states' shares.
+// From chunk to chunk X + sum q . dQs = X' + sum k . dKs (the pairs that pass the border), so
+// that X is formed once a segment, at its last chunk.  (Sums of q . dQ - k . dK alone, which
+// the same pairs cancel in, leave the roundings of all later tokens on a head that has long
+// forgotten them.)
 //
 // A sequence is cut into segments, which workgroups walk chunk by chunk with the state in
 // registers.  More than one segment: k_lin_state forms what each adds to the state,
@@ -35,6 +40,11 @@ namespace {
 
 template <typename T> struct FragFor { typedef f32x4 type; };
 template <> struct FragFor<__bf16> { typedef bf16x4 type; };
+
+// Terms of states and of P where they go into outputs in bf16 alone.  (One would add as much
+// again to the outputs' own rounding.)
+constexpr int kOut = 2;
+constexpr int kMostChunks = 16;  // of a segment of the backward pass
 
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -103,10 +113,26 @@ __device__ __forceinline__ double form_gates(Gates* s, float g, bool per_token, 
   return total;
 }
 
-// A chunk's rows of one head on the way from memory to LDS: 16-byte pieces, 256 threads.
+// A chunk's rows of one head in LDS: D values a row in 16-byte pieces, piece p of row r at
+// position p ^ turn(r).  The 16 rows of a run fragment and the 4 x 4 blocks of a transposing
+// read both meet 16 different groups of 4 banks (rows padded to 136 values met 2 to 4 times
+// the same in the second: half of the LDS cycles were conflicts).
+template <int D, typename T>
+struct Tile {
+  static constexpr int E = 16 / sizeof(T), CPR = D / E;
+  static __device__ __forceinline__ int turn(int r) {
+    return CPR == 8 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
+  }
+  static __device__ __forceinline__ int at(int r, int c) {
+    return r * D + ((c / E) ^ turn(r)) * E + c % E;
+  }
+};
+
+// The same on the way from memory, 256 threads.
 template <int D, typename T>
 struct Rows {
-  static constexpr int E = 16 / sizeof(T), CPR = D / E, N = LC * CPR / 256, LD = D + E;
+  typedef Tile<D, T> L;
+  static constexpr int E = L::E, CPR = L::CPR, N = LC * CPR / 256;
   typedef T Vec __attribute__((ext_vector_type(E)));
   Vec v[N];
   // p: the chunk's first token, ld values a token; rows past m repeat one of its own
@@ -121,34 +147,40 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int at = threadIdx.x + 256 * i, r = at / CPR;
-      *(Vec*)(s + r * LD + at % CPR * E) = r < m ? v[i] : Vec{};
+      *(Vec*)(s + L::at(r, at % CPR * E)) = r < m ? v[i] : Vec{};
     }
   }
 };
 
-// Fragments from LDS rows, LD values apart.  Along a row: slot s of lane (g, c) is value
-// 8g + s of the run at c0 of row r0 + c.  Down the rows: slot s is row r0 + 16 (s / 4) + 4g +
-// s % 4 of column c0 + GS (c / 4) + c % 4.
-template <int LD>
+// Fragments of a tile.  Along a row: slot s of lane (g, c) is value 8g + s of the run at c0 of
+// row r0 + c.  Down the rows: slot s is row r0 + 16 (s / 4) + 4g + s % 4 of column c0 +
+// GS (c / 4) + c % 4.
+template <int D>
 __device__ __forceinline__ Pair<bf16x4> run_frag(const __bf16* s, int r0, int c0, Lane ln) {
-  return Pair<bf16x4>{*(const bf16x8*)(s + (r0 + ln.c()) * LD + c0 + 8 * ln.g())};
+  return Pair<bf16x4>{*(const bf16x8*)(s + Tile<D, __bf16>::at(ln.c(), c0 + 8 * ln.g()) + r0 * D)};
 }
-template <int LD>
+template <int D>
 __device__ __forceinline__ Pair<f32x4> run_frag(const float* s, int r0, int c0, Lane ln) {
-  const float* p = s + (r0 + ln.c()) * LD + c0 + 8 * ln.g();
-  return join(*(const f32x4*)p, *(const f32x4*)(p + 4));
+  typedef Tile<D, float> L;
+  const int c = c0 + 8 * ln.g();
+  return join(*(const f32x4*)(s + L::at(ln.c(), c) + r0 * D),
+              *(const f32x4*)(s + L::at(ln.c(), c + 4) + r0 * D));
 }
-template <int LD, int GS>
+template <int D, int GS>
 __device__ __forceinline__ Pair<bf16x4> down_frag(const __bf16* s, int r0, int c0, Lane ln) {
-  const __bf16* p = s + (r0 + 4 * ln.g() + (ln.c() >> 2)) * LD + c0 + GS * (ln.c() & 3);
-  return join(read_transposed(p), read_transposed(p + 16 * LD));
+  const __bf16* p = s + Tile<D, __bf16>::at(4 * ln.g() + (ln.c() >> 2), c0 + GS * (ln.c() & 3)) +
+                    r0 * D;
+  return join(read_transposed(p), read_transposed(p + 16 * D));
 }
-template <int LD, int GS>
+template <int D, int GS>
 __device__ __forceinline__ Pair<f32x4> down_frag(const float* s, int r0, int c0, Lane ln) {
-  const float* p = s + (r0 + 4 * ln.g()) * LD + c0 + GS * (ln.c() >> 2) + (ln.c() & 3);
   f32x4 a, b;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) a[v] = p[v * LD], b[v] = p[(16 + v) * LD];
+  for (int v = 0; v < 4; ++v) {
+    const float* p =
+        s + Tile<D, float>::at(4 * ln.g() + v, c0 + GS * (ln.c() >> 2) + (ln.c() & 3)) + r0 * D;
+    a[v] = p[0], b[v] = p[16 * D];
+  }
   return join(a, b);
 }
 
@@ -175,8 +207,8 @@ __device__ __forceinline__ auto some(f32x4 lo, f32x4 hi) {
 
 // A wave's part of a [DK, DV] state: all rows, NS blocks of 16 columns.  Block m = 2q + h,
 // block row 4g + v holds state row 32q + 8g + 4h + v, so that two blocks are the pair that
-// meets a run of 8 values of a row; column c of block n is 16 NS w + 4 NS (c / 4) + 4n + c % 4,
-// so that a row-form result has 4 NS neighbouring columns a lane.
+// meets a run of 8 values of a row; column c of block n of wave w is 16 NS w + 4 NS (c / 4) + 4n +
+// c % 4, so that a row-form result has 4 NS neighbouring columns a lane.
 template <int DK, int DV>
 struct StateOf {
   static constexpr int NS = DV / 64, NQ = DK / 32;
@@ -198,15 +230,13 @@ struct StateOf {
 #pragma unroll
     for (int m = 0; m < 2 * NQ; ++m)
 #pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        const int r = row(m, ln), c = col(n, w, ln);
-        if (flip) {
-          b[m][n] = *(const f32x4*)(p + c * DK + r);
-        } else {
-#pragma unroll
-          for (int v = 0; v < 4; ++v) b[m][n][v] = p[(r + v) * DV + c];
-        }
-      }
+      for (int n = 0; n < NS; ++n) b[m][n] = block(p, flip, m, n, w, ln);
+  }
+  static __device__ __forceinline__ f32x4 block(const float* p, bool flip, int m, int n, int w,
+                                                Lane ln) {
+    const int r = row(m, ln), c = col(n, w, ln);
+    if (flip) return *(const f32x4*)(p + c * DK + r);
+    return f32x4{p[r * DV + c], p[(r + 1) * DV + c], p[(r + 2) * DV + c], p[(r + 3) * DV + c]};
   }
   __device__ __forceinline__ void store(float* p, bool flip, int w, Lane ln) const {
 #pragma unroll
@@ -227,7 +257,6 @@ struct StateOf {
   __device__ __forceinline__ void update(const T* sK, const T* sV, const Gates* gt, int w,
                                          Lane ln) {
     typedef typename FragFor<T>::type F;
-    constexpr int LDK = Rows<DK, T>::LD, LDV = Rows<DV, T>::LD;
     const float el = gt->el;
 #pragma unroll
     for (int m = 0; m < 2 * NQ; ++m)
@@ -240,17 +269,22 @@ struct StateOf {
       Some<F, kTerms<F, TS>> y[NS];
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
-        const Pair<F> x = down_frag<LDV, 4 * NS>(sV, 32 * p, 16 * NS * w + 4 * n, ln);
+        const Pair<F> x = down_frag<DV, 4 * NS>(sV, 32 * p, 16 * NS * w + 4 * n, ln);
         y[n] = some<F, TS>(x.lo() * wl, x.hi() * wh);
       }
 #pragma unroll
-      for (int m = 0; m < 2 * NQ; ++m) {
-        const Pair<F> k = down_frag<LDK, 8>(sK, 32 * p, 32 * (m >> 1) + 4 * (m & 1), ln);
+      for (int m0 = 0; m0 < 2 * NQ; m0 += 2) {  // 2 NS sums side by side
+        Pair<F> k[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+          k[m] = down_frag<DK, 8>(sK, 32 * p, 16 * m0 + 4 * m, ln);
 #pragma unroll
         for (int i = kTerms<F, TS> - 1; i >= 0; --i)
 #pragma unroll
-          for (int n = 0; n < NS; ++n)
-            b[m][n] = Pair<F>::template mma<false>(k, y[n].t[i], b[m][n]);
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+              b[m0 + m][n] = Pair<F>::template mma<false>(k[m], y[n].t[i], b[m0 + m][n]);
       }
     }
   }
@@ -274,6 +308,47 @@ struct Segment {
   }
 };
 
+// Its chunks in the order of the walk
+struct Chunks {
+  int n, len;
+  bool rev;
+  __device__ Chunks(const Segment& sg, bool r) : n((sg.len + LC - 1) / LC), len(sg.len), rev(r) {}
+  __device__ __forceinline__ int at(int i) const { return (rev ? n - 1 - i : i) * LC; }
+  __device__ __forceinline__ int size(int i) const { return min(LC, len - at(i)); }
+  // token of row r
+  __device__ __forceinline__ int token(int i, int r) const {
+    return at(i) + (rev ? size(i) - 1 - r : r);
+  }
+};
+
+// The gates of a walk's chunks, formed by one wave a chunk ahead (two tables in turn): on the
+// way of all waves they were 60 dependent instructions, half of them in 64 bits.
+struct GateStream {
+  const LinArgs& a;
+  const Chunks& ch;
+  const float* g;  // the segment's first token's
+  float now;
+  bool mine;
+  float s_out, s_in;
+  double total = 0.0;
+  __device__ GateStream(const LinArgs& a_, const Segment& sg, const Chunks& c, int h, bool m, float so,
+                        float si)
+      : a(a_), ch(c), g(a_.g + (a_.per_token ? sg.t0 * a_.Hv + h : h)), mine(m), s_out(so), s_in(si) {
+    now = mine && !a.per_token ? *g : 0.f;
+    fetch(0);
+  }
+  __device__ __forceinline__ void fetch(int i) {
+    if (mine && a.per_token && i < ch.n)
+      now = g[(int64_t)ch.token(i, min(lane_id(), ch.size(i) - 1)) * a.Hv];
+  }
+  // those of chunk i, at the buffer that chunk i - 2 has left
+  __device__ __forceinline__ void form(Gates* two, int i) {
+    if (!mine || i >= ch.n) return;
+    total += form_gates(two + (i & 1), now, a.per_token, ch.size(i), ch.rev, s_out, s_in);
+    fetch(i + 1);
+  }
+};
+
 // work item of a workgroup: neighbours on one XCD (workgroups go round the 8 in turn)
 __device__ __forceinline__ uint32_t work_item(uint32_t b, uint32_t n) {
   return (b & 7) * ((n + 7) >> 3) + (b >> 3);
@@ -289,37 +364,32 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
   const uint32_t ldk = (uint32_t)a.Hk * DK, ldv = (uint32_t)a.Hv * DV;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane ln = lane_here();
-  const int nc = (sg.len + LC - 1) / LC;
+  const Chunks ch(sg, rev);
   StateOf<DK, DV> S;
   S.zero();
   Rows<DK, T> k;
   Rows<DV, T> v;
-  float g = a.per_token ? 0.f : a.g[h];
   auto fetch = [&](int i) __attribute__((always_inline)) {
-    const int at = (rev ? nc - 1 - i : i) * LC, m = min(LC, sg.len - at);
+    const int at = ch.at(i), m = ch.size(i);
     k.load(K + (int64_t)at * ldk, ldk, m, rev);
     v.load(V + (int64_t)at * ldv, ldv, m, rev);
-    if (a.per_token && w == 0) {
-      const int r = min(ln.id, m - 1);
-      g = a.g[(sg.t0 + at + (rev ? m - 1 - r : r)) * a.Hv + h];
-    }
   };
-  double total = 0.0;
+  GateStream gates(a, sg, ch, h, w == 2, 1.f, rev ? a.scale : 1.f);
   fetch(0);
-  for (int i = 0; i < nc; ++i) {
-    const int m = min(LC, sg.len - (rev ? nc - 1 - i : i) * LC);
+  gates.form(gt, 0);
+  for (int i = 0; i < ch.n; ++i) {
     lds_only_barrier();
-    k.store(sK, m);
-    v.store(sV, m);
-    if (w == 0) total += form_gates(gt, g, a.per_token, m, rev, 1.f, rev ? a.scale : 1.f);
-    if (i + 1 < nc) fetch(i + 1);
+    k.store(sK, ch.size(i));
+    v.store(sV, ch.size(i));
+    if (i + 1 < ch.n) fetch(i + 1);
     lds_only_barrier();
-    S.template update<TS>(sK, sV, gt, w, ln);
+    gates.form(gt, i + 1);
+    S.template update<TS>(sK, sV, gt + (i & 1), w, ln);
   }
   float* to = (rev ? a.R : a.U) + ((int64_t)slot * a.Hv + h) * DK * DV;
   S.store(to, false, w, ln);
-  if (threadIdx.x == 0 && (!rev || sg.j == sg.n - 1))  // (once for each segment)
-    a.dec[(int64_t)slot * a.Hv + h] = exp2_of(total);
+  if (threadIdx.x == 128 && (!rev || sg.j == sg.n - 1))  // (once for each segment)
+    a.dec[(int64_t)slot * a.Hv + h] = exp2_of(gates.total);
 }
 
 }  // namespace
@@ -327,8 +397,8 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
 // `both`: the gradients' states too, in the second half of the work items
 template <int DK, int DV, typename T, int TS>
 __global__ __launch_bounds__(256) void k_lin_state(const LinArgs a, uint32_t n, bool both) {
-  __shared__ __attribute__((aligned(16))) T sK[LC * Rows<DK, T>::LD], sV[LC * Rows<DV, T>::LD];
-  __shared__ __attribute__((aligned(16))) Gates gt;
+  __shared__ __attribute__((aligned(16))) T sK[LC * DK], sV[LC * DV];
+  __shared__ __attribute__((aligned(16))) Gates gt[2];
   uint32_t w = work_item(blockIdx.x, n * (both ? 2 : 1));
   if (w >= n * (both ? 2 : 1)) return;
   const bool rev = w >= n;
@@ -338,7 +408,7 @@ __global__ __launch_bounds__(256) void k_lin_state(const LinArgs a, uint32_t n, 
   const Segment sg(a.q, slot);
   // (the last segment's share ends in S_final, the first one's in dS0: the walks form those)
   if (sg.len == 0 || (rev ? sg.j == 0 : sg.j == sg.n - 1)) return;
-  add_of_segment<DK, DV, T, TS>(a, sg, slot, h, rev, sK, sV, &gt);
+  add_of_segment<DK, DV, T, TS>(a, sg, slot, h, rev, sK, sV, gt);
 }
 
 // The states carried over the segments of each sequence, in place: U from what a segment
@@ -387,117 +457,172 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinArgs a, int parts) {
 
 namespace {
 
-template <typename T, int N> struct RunType { typedef T type __attribute__((ext_vector_type(N))); };
-template <typename T, int N> using RunOf = typename RunType<T, N>::type;
-
 // One pass along a segment for one value head.
 struct Pass {
-  const void *q, *k, *v, *x;   // x: rows whose products with the result are kept (or null)
-  uint32_t ldq, ldk, ldv, ldo; // values a token
+  const void *q, *k, *v, *x;    // x: rows for the gradient of g (or null)
+  uint32_t ldq, ldk, ldv, ldo;  // values a token
   void* out;
-  float* acc;                  // sums of a group's heads (null: one head)
-  bool first, last;            // of the group
-  float* dot;                  // of each row, at the segment's first token
-  float* far;                  // of each chunk, of what came from the state
-  const float* start;          // the state that enters (or null: zeros)
-  float* fin;                  // the state that leaves (or null)
-  const float* against;        // [product with the state that leaves] (or null)
-  float* anchor;
-  bool flip, rev;              // flip: the state's transposed in memory
+  float* acc;                   // sums of a group's heads (null: one head)
+  bool first, last;             // of the group
+  float* rows;                  // x's products of each token, at the segment's first
+  const float* start;           // the state that enters (or null: zeros)
+  float* fin;                   // the state that leaves (or null)
+  const float* against;         // the gradient of the state that leaves (or null: zeros)
+  float* anchor;                // X of the last chunk (or null)
+  bool flip, rev;               // flip: the state's transposed in memory
+  bool pairs;                   // rows: with the sums of M
   float s_out, s_in;
 };
 
-template <int DK, int DV, typename T, int TO>
+template <int DK, int DV, typename T, int TP>
 struct PassLds {
   typedef typename FragFor<T>::type F;
-  T q[LC * Rows<DK, T>::LD], k[LC * Rows<DK, T>::LD], v[LC * Rows<DV, T>::LD];
-  T p[6 * kTerms<F, TO> * 512];
-  float dot[4][LC], far[4];
-  Gates gt;
+  T q[LC * DK], k[LC * DK], v[LC * DV];
+  T p[6 * kTerms<F, TP> * 512];
+  float far[4][LC];              // the waves' shares of x . (what came from the state)
+  float row[4][LC], col[4][LC];  // sums of M's blocks (I, J): along rows at J, down columns at I
+  float part[4];
+  Gates gt[2];
 };
 
+// P's fragments of row block I: pair p of column blocks
 __host__ __device__ constexpr int p_slot(int I, int p) { return (I == 3 ? 4 : I) + p; }
 
-template <int DK, int DV, typename T, int TS, int TO>
+template <typename T, int N> struct RunType { typedef T type __attribute__((ext_vector_type(N))); };
+template <typename T, int N> using RunOf = typename RunType<T, N>::type;
+
+// Terms: TS of the decayed values that the state takes up, TO of the state, TP of P.
+template <int DK, int DV, typename T, int TS, int TO, int TP>
 __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h, const Pass& ps,
-                                     PassLds<DK, DV, T, TO>* lds) {
+                                     PassLds<DK, DV, T, TP>* lds) {
   typedef typename FragFor<T>::type F;
-  constexpr int LDK = Rows<DK, T>::LD, LDV = Rows<DV, T>::LD, NS = DV / 64, NQ = DK / 32;
-  constexpr int M = kTerms<F, TO>;
+  constexpr int NQ = DK / 32, NS = DV / 64, MO = kTerms<F, TO>, MP = kTerms<F, TP>;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane ln = lane_here();
-  const int g4 = 4 * ln.g(), c = ln.c(), nc = (sg.len + LC - 1) / LC;
+  const int g4 = 4 * ln.g(), c = ln.c();
   const bool rev = ps.rev;
+  const Chunks ch(sg, rev);
   StateOf<DK, DV> S;
   if (ps.start) S.load(ps.start, ps.flip, w, ln); else S.zero();
   Rows<DK, T> q, k;
   Rows<DV, T> v;
-  float g = a.per_token ? 0.f : a.g[h];
   auto fetch = [&](int i) __attribute__((always_inline)) {
-    const int at = (rev ? nc - 1 - i : i) * LC, m = min(LC, sg.len - at);
+    const int at = ch.at(i), m = ch.size(i);
     q.load((const T*)ps.q + (int64_t)at * ps.ldq, ps.ldq, m, rev);
     k.load((const T*)ps.k + (int64_t)at * ps.ldk, ps.ldk, m, rev);
     v.load((const T*)ps.v + (int64_t)at * ps.ldv, ps.ldv, m, rev);
-    if (a.per_token && w == 0) {
-      const int r = min(ln.id, m - 1);
-      g = a.g[(sg.t0 + at + (rev ? m - 1 - r : r)) * a.Hv + h];
+  };
+  // what the gradient of g takes of a chunk: the waves' shares meet in LDS
+  auto write_rows = [&](int i) __attribute__((always_inline)) {
+    if (!ps.x || w != 3 || i < 0 || ln.id >= ch.size(i)) return;
+    float f = (lds->far[0][ln.id] + lds->far[1][ln.id]) + (lds->far[2][ln.id] + lds->far[3][ln.id]);
+    if (ps.pairs) {
+      float e = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (u <= ln.id >> 4) e += lds->row[u][ln.id];
+        if (u >= ln.id >> 4) e -= lds->col[u][ln.id];
+      }
+      f += e;
     }
+    ps.rows[ch.token(i, ln.id)] = f;
   };
-  // the rows' products with x, of the chunk before: the waves' shares meet in LDS
-  auto write_dot = [&](int at, int m) __attribute__((always_inline)) {
-    if (ps.dot && w == 1 && ln.id < m)
-      ps.dot[at + (rev ? m - 1 - ln.id : ln.id)] =
-          (lds->dot[0][ln.id] + lds->dot[1][ln.id]) + (lds->dot[2][ln.id] + lds->dot[3][ln.id]);
-    if (ps.dot && threadIdx.x == 0 && m > 0)
-      ps.far[at / LC] = (lds->far[0] + lds->far[1]) + (lds->far[2] + lds->far[3]);
-  };
+  GateStream gates(a, sg, ch, h, w == 2, ps.s_out, ps.s_in);
   fetch(0);
-  int before = 0, mb = 0;
-  for (int i = 0; i < nc; ++i) {
-    const int at = (rev ? nc - 1 - i : i) * LC, m = min(LC, sg.len - at);
+  gates.form(lds->gt, 0);
+  // P's blocks above the diagonal that share a pair with one on it
+  if (w < 2) {
+    T* to = lds->p + p_slot(2 * w, w) * MP * 512;
+#pragma unroll
+    for (int t = 0; t < MP; ++t) {
+      if constexpr (sizeof(T) == 4)
+        *(f32x4*)(to + 256 + 4 * ln.id) = zero4();
+      else
+        *(uint64_t*)(to + t * 512 + 8 * ln.id + 4) = 0;
+    }
+  }
+  for (int i = 0; i < ch.n; ++i) {
+    const int at = ch.at(i), m = ch.size(i);
+    const bool end = i == ch.n - 1;
+    const Gates* gt = lds->gt + (i & 1);
     lds_only_barrier();
     q.store(lds->q, m);
     k.store(lds->k, m);
     v.store(lds->v, m);
-    if (w == 0) form_gates(&lds->gt, g, a.per_token, m, rev, ps.s_out, ps.s_in);
-    write_dot(before, mb);
-    before = at, mb = m;
-    if (i + 1 < nc) fetch(i + 1);
+    write_rows(i - 1);
     lds_only_barrier();
-    // P's row block w, in row form: lane (g, c) has columns 16 J + 4g .. of row 16 w + c
-    {
-      Pair<F> x[NQ];
+    if (ps.anchor && end) {
+      float x = 0.f;
+      if (ps.against) {
 #pragma unroll
-      for (int s = 0; s < NQ; ++s) x[s] = run_frag<LDK>(lds->q, 16 * w, 32 * s, ln);
-      const float hi = lds->gt.hi[16 * w + c], lo = lds->gt.lo[16 * w + c];
-      for (int J = 0; J <= (w | 1); ++J) {
-        f32x4 p = zero4();
-        if (J <= w) {
+        for (int u = 0; u < 2 * NQ; ++u)
 #pragma unroll
-          for (int s = 0; s < NQ; ++s)
-            p = Pair<F>::template mma<true>(x[s], run_frag<LDK>(lds->k, 16 * J, 32 * s, ln), p);
-          const f32x4 hj = *(const f32x4*)(lds->gt.hi + 16 * J + g4);
-          const f32x4 lj = *(const f32x4*)(lds->gt.lo + 16 * J + g4);
+          for (int n = 0; n < NS; ++n) {
+            const f32x4 y = StateOf<DK, DV>::block(ps.against, ps.flip, u, n, w, ln);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float d = __builtin_amdgcn_exp2f((hi - hj[u]) + (lo - lj[u]));
-            p[u] = 16 * J + g4 + u <= 16 * w + c ? a.scale * p[u] * d : 0.f;
+            for (int e = 0; e < 4; ++e) x = __builtin_fmaf(S.b[u][n][e], y[e], x);
           }
-        }
-        T* to = lds->p + p_slot(w, J >> 1) * M * 512;
-        if constexpr (M == 1 && sizeof(T) == 4) {
-          *(f32x4*)(to + 256 * (J & 1) + 4 * ln.id) = p;
-        } else {
-          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-          float p0 = p[0], p1 = p[1], p2 = p[2], p3 = p[3];
+        x = sum_lanes<64>(x);
+      }
+      if (ln.id == 0) lds->part[w] = x;
+    }
+    // P's blocks in row form: lane (g, c) has columns 16 J + 4g .. of row 16 I + c
+    for (int b = w; b < 10; b += 4) {
+      const int I = b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3, J = b - I * (I + 1) / 2;
+      const int r = 16 * I + c;
+      f32x4 p = zero4(), p1 = zero4();
 #pragma unroll
-          for (int t = 0; t < M; ++t) {
-            const u32x2 b{take2(p0, p1), take2(p2, p3)};
-            *(u32x2*)(to + t * 512 + 8 * ln.id + 4 * (J & 1)) = b;
-          }
+      for (int s = 0; s < NQ; s += 2) {
+        p = Pair<F>::template mma<true>(run_frag<DK>(lds->q, 16 * I, 32 * s, ln),
+                                        run_frag<DK>(lds->k, 16 * J, 32 * s, ln), p);
+        p1 = Pair<F>::template mma<true>(run_frag<DK>(lds->q, 16 * I, 32 * s + 32, ln),
+                                         run_frag<DK>(lds->k, 16 * J, 32 * s + 32, ln), p1);
+      }
+      const float hi = gt->hi[r], lo = gt->lo[r];
+      const f32x4 hj = *(const f32x4*)(gt->hi + 16 * J + g4);
+      const f32x4 lj = *(const f32x4*)(gt->lo + 16 * J + g4);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float d = __builtin_amdgcn_exp2f((hi - hj[u]) + (lo - lj[u]));
+        p[u] = 16 * J + g4 + u <= r ? a.scale * (p[u] + p1[u]) * d : 0.f;
+      }
+      T* to = lds->p + p_slot(I, J >> 1) * MP * 512;
+      if constexpr (sizeof(T) == 4) {
+        *(f32x4*)(to + 256 * (J & 1) + 4 * ln.id) = p;
+      } else {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        float p0 = p[0], p1 = p[1], p2 = p[2], p3 = p[3];
+#pragma unroll
+        for (int t = 0; t < MP; ++t) {
+          const uint32_t x = take2(p0, p1), y = take2(p2, p3);
+          *(u32x2*)(to + t * 512 + 8 * ln.id + 4 * (J & 1)) = u32x2{x, y};
         }
       }
+      if (ps.pairs) {  // M, of i > j: P (.) (X V^T)
+        f32x4 y = zero4();
+        const T* xp = (const T*)ps.x + (int64_t)ch.token(i, min(r, m - 1)) * ps.ldo;
+#pragma unroll
+        for (int s = 0; s < DV / 32; ++s) {
+          Pair<F> x;
+          if constexpr (sizeof(T) == 4)
+            x = join(*(const f32x4*)(xp + 32 * s + 2 * g4), *(const f32x4*)(xp + 32 * s + 2 * g4 + 4));
+          else
+            x.v = *(const bf16x8*)(xp + 32 * s + 2 * g4);
+          y = Pair<F>::template mma<true>(x, run_frag<DV>(lds->v, 16 * J, 32 * s, ln), y);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          y[u] = 16 * J + g4 + u < r ? y[u] * p[u] : 0.f;
+          sum += y[u];
+          y[u] = sum16(y[u]);
+        }
+        sum = sum_apart32(sum_apart16(sum));
+        if (ln.g() == 0) lds->row[J][r] = sum;
+        if (c == 0) *(f32x4*)(lds->col[I] + 16 * J + g4) = y;
+      }
     }
+    gates.form(lds->gt, i + 1);
     // what comes from the state
     f32x4 o[4][NS];
 #pragma unroll
@@ -506,122 +631,92 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       for (int n = 0; n < NS; ++n) o[I][n] = zero4();
 #pragma unroll
     for (int s = 0; s < NQ; ++s) {
-      Some<F, M> y[NS];
+      Some<F, MO> y[NS];
 #pragma unroll
       for (int n = 0; n < NS; ++n) y[n] = some<F, TO>(S.b[2 * s][n], S.b[2 * s + 1][n]);
 #pragma unroll
-      for (int I = 0; I < 4; ++I) {
-        const Pair<F> x = run_frag<LDK>(lds->q, 16 * I, 32 * s, ln);
+      for (int I0 = 0; I0 < 4; I0 += 2) {
+        Pair<F> x[2];
 #pragma unroll
-        for (int t = M - 1; t >= 0; --t)
+        for (int I = 0; I < 2; ++I) x[I] = run_frag<DK>(lds->q, 16 * (I0 + I), 32 * s, ln);
 #pragma unroll
-          for (int n = 0; n < NS; ++n) o[I][n] = Pair<F>::template mma<true>(x, y[n].t[t], o[I][n]);
+        for (int t = MO - 1; t >= 0; --t)
+#pragma unroll
+          for (int I = 0; I < 2; ++I)
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+              o[I0 + I][n] = Pair<F>::template mma<true>(x[I], y[n].t[t], o[I0 + I][n]);
       }
     }
+    // lane (g, c): columns 16 NS w + NS g4 .. of row 16 I + c
+    const uint32_t row0 = (uint32_t)(rev ? m - 1 - c : c) * ps.ldo + 16 * NS * w + NS * g4;
+    const uint32_t down = (rev ? -16 : 16) * ps.ldo;
+    const int64_t chunk = (int64_t)at * ps.ldo;
 #pragma unroll
     for (int I = 0; I < 4; ++I) {
-      const float f = lds->gt.out[16 * I + c];
+      const float f = gt->out[16 * I + c];
 #pragma unroll
       for (int n = 0; n < NS; ++n) o[I][n] *= f;
     }
-    // lane (g, c): columns 16 NS w + 4 NS g + 0 .. 4 NS - 1 of row 16 I + c
-    const int col = 16 * NS * w + NS * g4;
-    auto row_of = [&](int I) { return (int64_t)(at + (rev ? m - 1 - 16 * I - c : 16 * I + c)); };
-    RunOf<T, 4 * NS> x[4];
-    float far = 0.f;
-    if (ps.x) {
+    if (ps.x)
 #pragma unroll
-      for (int I = 0; I < 4; ++I)
+      for (int I = 0; I < 4; ++I) {
+        float far = 0.f;
         if (16 * I + c < m) {
-          x[I] = *(const RunOf<T, 4 * NS>*)((const T*)ps.x + row_of(I) * ps.ldo + col);
+          const auto x = *(const RunOf<T, 4 * NS>*)((const T*)ps.x + chunk + (row0 + I * down));
 #pragma unroll
           for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-              far = __builtin_fmaf((float)x[I][4 * n + u], o[I][n][u], far);
+            for (int u = 0; u < 4; ++u) far = __builtin_fmaf((float)x[4 * n + u], o[I][n][u], far);
         }
-    }
-    S.template update<TS>(lds->k, lds->v, &lds->gt, w, ln);
+        far = sum_apart32(sum_apart16(far));
+        if (ln.g() == 0) lds->far[w][16 * I + c] = far;
+      }
+    if (!end) fetch(i + 1);
+    S.template update<TS>(lds->k, lds->v, gt, w, ln);
     lds_only_barrier();
+    if (ps.anchor && end && threadIdx.x == 0)
+      *ps.anchor = gt->el * ((lds->part[0] + lds->part[1]) + (lds->part[2] + lds->part[3]));
     // and from the chunk's tokens
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       Pair<F> y[NS];
 #pragma unroll
       for (int n = 0; n < NS; ++n)
-        y[n] = down_frag<LDV, 4 * NS>(lds->v, 32 * p, 16 * NS * w + 4 * n, ln);
+        y[n] = down_frag<DV, 4 * NS>(lds->v, 32 * p, 16 * NS * w + 4 * n, ln);
 #pragma unroll
-      for (int I = 2 * p; I < 4; ++I) {
-        const T* from = lds->p + p_slot(I, p) * M * 512;
+      for (int t = MP - 1; t >= 0; --t)
 #pragma unroll
-        for (int t = M - 1; t >= 0; --t) {
+        for (int I = 2 * p; I < 4; ++I) {
+          const T* from = lds->p + (p_slot(I, p) * MP + t) * 512;
           Pair<F> x;
           if constexpr (sizeof(T) == 4)
             x = join(*(const f32x4*)(from + 4 * ln.id), *(const f32x4*)(from + 256 + 4 * ln.id));
           else
-            x.v = *(const bf16x8*)(from + t * 512 + 8 * ln.id);
+            x.v = *(const bf16x8*)(from + 8 * ln.id);
 #pragma unroll
           for (int n = 0; n < NS; ++n) o[I][n] = Pair<F>::template mma<true>(x, y[n], o[I][n]);
         }
-      }
     }
+    typedef T Out __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int I = 0; I < 4; ++I) {
-      float dot = 0.f;
-      if (16 * I + c < m) {
-        const int64_t to = row_of(I) * ps.ldo + col;
-        if (ps.x) {
-#pragma unroll
-          for (int n = 0; n < NS; ++n)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              dot = __builtin_fmaf((float)x[I][4 * n + u], o[I][n][u], dot);
-        }
+    for (int I = 0; I < 4; ++I)
+      if (16 * I + c < m)
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
+          const uint32_t to = row0 + I * down + 4 * n;
           f32x4 y = o[I][n];
-          if (ps.acc && !ps.first) y += *(const f32x4*)(ps.acc + to + 4 * n);
-          if (ps.acc && !ps.last) {
-            *(f32x4*)(ps.acc + to + 4 * n) = y;
-          } else {
-            typedef T Out __attribute__((ext_vector_type(4)));
-            *(Out*)((T*)ps.out + to + 4 * n) = __builtin_convertvector(y, Out);
-          }
+          if (ps.acc && !ps.first) y += *(const f32x4*)(ps.acc + chunk + to);
+          if (ps.acc && !ps.last)
+            *(f32x4*)(ps.acc + chunk + to) = y;
+          else
+            *(Out*)((T*)ps.out + chunk + to) = __builtin_convertvector(y, Out);
         }
-      }
-      if (ps.x) {
-        dot = sum_apart32(sum_apart16(dot));
-        if (ln.g() == 0) lds->dot[w][16 * I + c] = dot;
-      }
-    }
-    if (ps.x) {
-      far = sum_lanes<64>(far);
-      if (ln.id == 0) lds->far[w] = far;
-    }
   }
   if (ps.fin) S.store(ps.fin, ps.flip, w, ln);
   if (!ps.x) return;
   lds_only_barrier();
-  write_dot(before, mb);
-  if (ps.anchor) {  // <S, dS> at the segment's end
-    float x = 0.f;
-    if (ps.against) {
-      StateOf<DK, DV> y;
-      y.load(ps.against, ps.flip, w, ln);
-#pragma unroll
-      for (int m = 0; m < 2 * NQ; ++m)
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-#pragma unroll
-          for (int u = 0; u < 4; ++u) x = __builtin_fmaf(S.b[m][n][u], y.b[m][n][u], x);
-      x = sum_lanes<64>(x);
-    }
-    lds_only_barrier();
-    if (ln.id == 0) lds->dot[0][w] = x;
-    lds_only_barrier();
-    if (threadIdx.x == 0)
-      *ps.anchor = (lds->dot[0][0] + lds->dot[0][1]) + (lds->dot[0][2] + lds->dot[0][3]);
-  }
+  write_rows(ch.n - 1);
 }
 
 // sequences without tokens: the state stays what it was
@@ -637,10 +732,10 @@ __device__ __forceinline__ void copy_state(const LinArgs& a, int s, const float*
 
 }  // namespace
 
-template <int DK, int DV, typename T, int TS, int TO>
+template <int DK, int DV, typename T, int TS, int TO, int TP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_forward(const LinArgs a,
                                                                             uint32_t n) {
-  __shared__ __attribute__((aligned(16))) PassLds<DK, DV, T, TO> lds;
+  __shared__ __attribute__((aligned(16))) PassLds<DK, DV, T, TP> lds;
   const uint32_t blocks = (n + 7) & ~7u;
   if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.S0, a.Sf);
   const uint32_t w = work_item(blockIdx.x, n);
@@ -659,17 +754,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_forward(con
   ps.start = a.U ? a.U + ((int64_t)slot * a.Hv + h) * size : a.S0 ? a.S0 + own : nullptr;
   ps.fin = a.Sf && sg.j == sg.n - 1 ? a.Sf + own : nullptr;
   ps.s_out = a.scale, ps.s_in = 1.f;
-  walk<DK, DV, T, TS, TO>(a, sg, h, ps, &lds);
+  walk<DK, DV, T, TS, TO, TP>(a, sg, h, ps, &lds);
 }
 
 // Three passes: dQ and dK by key heads (the heads of a group one after the other), dV by
 // value heads.
-template <int DK, int DV, typename T, int TS, int TO>
+template <int DK, int DV, typename T, int TS, int TO, int TP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(const LinArgs a,
                                                                              uint32_t slots) {
   union Lds {
-    PassLds<DV, DK, T, TO> qk;
-    PassLds<DK, DV, T, TO> v;
+    PassLds<DV, DK, T, TP> qk;
+    PassLds<DK, DV, T, TP> v;
   };
   __shared__ __attribute__((aligned(16))) Lds lds;
   const uint32_t nk = slots * (uint32_t)a.Hk, nv = slots * (uint32_t)a.Hv;
@@ -704,8 +799,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(co
       ps.flip = true, ps.rev = rev;
       if (a.want_dg) {
         ps.x = (const T*)(rev ? a.K : a.Q) + tk;
-        ps.dot = (rev ? a.rows_k : a.rows_q) + h * tokens + sg.t0;
-        ps.far = (rev ? a.far_k : a.far_q) + ((int64_t)slot * a.Hv + h) * (a.q.seg / LC);
+        ps.rows = (rev ? a.rows_k : a.rows_q) + h * tokens + sg.t0;
+        ps.pairs = !rev;
       }
       if (rev) {
         ps.start = dS;
@@ -715,7 +810,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(co
         ps.s_out = a.scale, ps.s_in = 1.f;
         if (a.want_dg) ps.against = dS, ps.anchor = a.anchor + (int64_t)slot * a.Hv + h;
       }
-      walk<DV, DK, T, TS, TO>(a, sg, h, ps, &lds.qk);
+      walk<DV, DK, T, TS, TO, TP>(a, sg, h, ps, &lds.qk);
       lds_only_barrier();
     }
   } else {
@@ -735,13 +830,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(co
     ps.fin = a.dS0 && sg.j == 0 ? a.dS0 + own : nullptr;
     ps.rev = true;
     ps.s_out = 1.f, ps.s_in = a.scale;
-    walk<DK, DV, T, TS, TO>(a, sg, h, ps, &lds.v);
+    walk<DK, DV, T, TS, kOut, TP>(a, sg, h, ps, &lds.v);
   }
 }
 
-// ---- the gradient of g: sums over a segment's rows from its end; a wave takes a chunk
+// ---- the gradient of g from the rows' sums; a wave takes a chunk
 __global__ __launch_bounds__(256) void k_lin_decay(const LinArgs a) {
-  __shared__ float wave[4];
+  __shared__ float sq[kMostChunks], sk[kMostChunks], wave[4];
   const uint32_t slot = blockIdx.x / (uint32_t)a.Hv;
   const int h = (int)(blockIdx.x - slot * (uint32_t)a.Hv);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane_id();
@@ -750,21 +845,25 @@ __global__ __launch_bounds__(256) void k_lin_decay(const LinArgs a) {
   const int64_t tokens = a.q.cu ? (int64_t)a.q.T : (int64_t)a.q.nseq * a.q.T;
   const float* rq = a.rows_q + h * tokens + sg.t0;
   const float* rk = a.rows_k + h * tokens + sg.t0;
-  const float* fq = a.far_q + at * (a.q.seg / LC);
-  const float* fk = a.far_k + at * (a.q.seg / LC);
   const int nc = (sg.len + LC - 1) / LC;
+  for (int c = w; c < nc; c += 4) {
+    const int t = c * LC + l;
+    const float q = sum_lanes<64>(t < sg.len ? rq[t] : 0.f);
+    const float k = sum_lanes<64>(t < sg.len ? rk[t] : 0.f);
+    if (l == 0) sq[c] = q, sk[c] = k;
+  }
+  __syncthreads();
   float all = 0.f;
   for (int c = w; c < nc; c += 4) {
-    float z = 0.f;  // <S, dS> at the chunk's end
-    for (int i = c + 1 + l; i < nc; i += 64) z += fq[i] - fk[i];
-    z = sum_lanes<64>(z) + a.anchor[at];
-    // lane l has the l-th token from the chunk's end
-    const int m = min(LC, sg.len - c * LC), t = c * LC + m - 1 - l;
-    const float d = l < m ? rq[t] - rk[t] : 0.f;
-    z += (float)prefix64(d);
-    if (l < m) {
-      if (a.per_token) a.dg[(sg.t0 + t) * a.Hv + h] = z;
-      all += z;
+    float x = a.anchor[at];  // X of the last chunk, and from there X of this one
+    for (int i = nc - 1; i > c; --i) x += sq[i] - sk[i - 1];
+    const int t = c * LC + l;
+    const float q = t < sg.len ? rq[t] : 0.f, k = t < sg.len ? rk[t] : 0.f;
+    const double pq = prefix64((double)q), pk = prefix64((double)k);
+    x += (float)((lane63(pq) - (pq - q)) + (pk - k));
+    if (t < sg.len) {
+      if (a.per_token) a.dg[(sg.t0 + t) * a.Hv + h] = x;
+      all += x;
     }
   }
   if (a.per_token) return;
@@ -795,7 +894,7 @@ int lin_segment(int nseq, int T, int heads, bool packed, bool backward) {
   // about 512 workgroups of work: two a CU
   int64_t seg = tokens * heads / 512 / LC * LC;
   if (seg < 256) seg = 256;
-  const int64_t most = backward ? 1024 : 4096;
+  const int64_t most = backward ? LC * kMostChunks : 4096;
   if (seg > most) seg = most;
   return seg >= whole ? std::max(whole, LC) : (int)seg;
 }
@@ -815,8 +914,6 @@ int64_t lin_workspace(LinArgs& a, bool backward, float* ws) {
   const bool dg = backward && a.want_dg;
   take(a.rows_q, dg ? a.Hv * tokens : 0);
   take(a.rows_k, dg ? a.Hv * tokens : 0);
-  take(a.far_q, dg ? slots * a.Hv * (a.q.seg / LC) : 0);
-  take(a.far_k, dg ? slots * a.Hv * (a.q.seg / LC) : 0);
   take(a.anchor, dg ? slots * a.Hv : 0);
   take(a.part, dg && !a.per_token ? slots * a.Hv : 0);
   const bool acc = backward && a.Hv > a.Hk;
@@ -855,9 +952,10 @@ hipError_t launch_linear_forward(const LinArgs& a, int dtype, hipStream_t st) {
   if (grid == 0) return hipSuccess;
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
     if (dtype == 0)
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, float, 1, 1>), dim3(grid), dim3(256), 0, st, a, n);
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, float, 1, 1, 1>), dim3(grid), dim3(256), 0, st, a, n);
     else
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, __bf16, 3, 2>), dim3(grid), dim3(256), 0, st, a, n);
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, __bf16, 3, kOut, kOut>), dim3(grid), dim3(256), 0,
+                         st, a, n);
     return hipGetLastError();
   }))
   return hipErrorNotSupported;
@@ -872,11 +970,14 @@ hipError_t launch_linear_backward(const LinArgs& a, int dtype, hipStream_t st) {
   if (grid > 0) {
     GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
       if (dtype == 0)
-        hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1>), dim3(grid), dim3(256), 0, st, a,
-                           slots);
-      else
-        hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, 3>), dim3(grid), dim3(256), 0, st,
+        hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1>), dim3(grid), dim3(256), 0, st,
                            a, slots);
+      else if (a.want_dg)
+        hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, 3, kOut>), dim3(grid), dim3(256), 0,
+                           st, a, slots);
+      else
+        hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, kOut, kOut>), dim3(grid), dim3(256),
+                           0, st, a, slots);
       break;
     }) break;)
     if (hipError_t e = hipGetLastError()) return e;

@@ -71,9 +71,8 @@ struct LinArgs {
   // workspace (all null where every sequence is one segment and no dg is wanted)
   float *U, *R;           // [slots, Hv, dk, dv]: states entering, their gradients leaving
   float* dec;             // [slots, Hv]: decay over a segment
-  float *rows_q, *rows_k;  // [Hv, tokens]: q . dQ, k . dK
-  float *far_q, *far_k;    // [slots, Hv, seg / LC]: a chunk's sums of them, of what the state gave
-  float *anchor, *part;   // [slots, Hv]: <S, dS> at a segment's end; sums of dg
+  float *rows_q, *rows_k;  // [Hv, tokens]: what dg takes of each token (linear.hip)
+  float *anchor, *part;   // [slots, Hv]: X of a segment's last chunk; sums of dg
   float *acc_q, *acc_k;   // [tokens, Hk, dk]: sums of dQ, dK over a group's first heads
 };
 
