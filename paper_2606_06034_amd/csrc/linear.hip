@@ -15,8 +15,8 @@
 // what passes the chunk:
 //   dg_t = sum_{i >= t > j} M_ij + sum_{i >= t} q_i . dQs_i + sum_{j < t} k_j . dKs_j + X,
 //   M = ((Q K^T) (.) (scale dO V^T) (.) D), X = e^total <S, dS>, dQs and dKs the states' shares.
-// From chunk to chunk X + sum q . dQs = X' + sum k . dKs (the pairs that pass the border), so
-// that X is formed once a segment, at its last chunk.  (Sums of q . dQ - k . dK alone, which
+// From a chunk to the one before it X + sum q . dQs = X' + sum k . dKs' (the pairs that pass the
+// border), so that X is formed once a segment, at its first chunk.  (Sums of q . dQ - k . dK alone, which
 // the same pairs cancel in, leave the roundings of all later tokens on a head that has long
 // forgotten them.)
 //
@@ -44,6 +44,7 @@ template <> struct FragFor<__bf16> { typedef bf16x4 type; };
 // Terms of states and of P where they go into outputs in bf16 alone.  (One would add as much
 // again to the outputs' own rounding.)
 constexpr int kOut = 2;
+constexpr int kStateBlocks = 1, kWalkBlocks = 2;
 constexpr int kMostChunks = 16;  // of a segment of the backward pass
 
 constexpr double kLog2e = 1.4426950408889634074;
@@ -128,25 +129,25 @@ struct Tile {
   }
 };
 
-// The same on the way from memory, 256 threads.
-template <int D, typename T>
+// The same on the way from memory, NT threads.
+template <int D, int NT, typename T>
 struct Rows {
   typedef Tile<D, T> L;
-  static constexpr int E = L::E, CPR = L::CPR, N = LC * CPR / 256;
+  static constexpr int E = L::E, CPR = L::CPR, N = LC * CPR / NT;
   typedef T Vec __attribute__((ext_vector_type(E)));
   Vec v[N];
   // p: the chunk's first token, ld values a token; rows past m repeat one of its own
   __device__ __forceinline__ void load(const T* __restrict__ p, uint32_t ld, int m, bool rev) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + 256 * i, r = min(at / CPR, m - 1);
+      const int at = threadIdx.x + NT * i, r = min(at / CPR, m - 1);
       v[i] = *(const Vec*)(p + ((uint32_t)(rev ? m - 1 - r : r) * ld + at % CPR * E));
     }
   }
   __device__ __forceinline__ void store(T* s, int m) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + 256 * i, r = at / CPR;
+      const int at = threadIdx.x + NT * i, r = at / CPR;
       *(Vec*)(s + L::at(r, at % CPR * E)) = r < m ? v[i] : Vec{};
     }
   }
@@ -184,6 +185,16 @@ __device__ __forceinline__ Pair<f32x4> down_frag(const float* s, int r0, int c0,
   return join(a, b);
 }
 
+// 8 values of a row
+template <typename F>
+__device__ __forceinline__ Pair<F> load_run8(const __bf16* p) {
+  return Pair<F>{*(const bf16x8*)p};
+}
+template <typename F>
+__device__ __forceinline__ Pair<F> load_run8(const float* p) {
+  return Pair<F>{*(const f32x4*)p, *(const f32x4*)(p + 4)};
+}
+
 // The first N terms of a split value (fp32: the value)
 template <typename F, int N> struct Some { Pair<F> t[N]; };
 template <typename F, int N> constexpr int kTerms = TermsOf<F>::N == 1 ? 1 : N;
@@ -209,9 +220,9 @@ __device__ __forceinline__ auto some(f32x4 lo, f32x4 hi) {
 // block row 4g + v holds state row 32q + 8g + 4h + v, so that two blocks are the pair that
 // meets a run of 8 values of a row; column c of block n of wave w is 16 NS w + 4 NS (c / 4) + 4n +
 // c % 4, so that a row-form result has 4 NS neighbouring columns a lane.
-template <int DK, int DV>
+template <int DK, int DV, int NS>
 struct StateOf {
-  static constexpr int NS = DV / 64, NQ = DK / 32;
+  static constexpr int NQ = DK / 32;
   f32x4 b[2 * NQ][NS];
   static __device__ __forceinline__ int row(int m, Lane ln) {
     return 32 * (m >> 1) + 8 * ln.g() + 4 * (m & 1);
@@ -355,7 +366,7 @@ __device__ __forceinline__ uint32_t work_item(uint32_t b, uint32_t n) {
 }
 
 // ---- what a segment adds to the state
-template <int DK, int DV, typename T, int TS>
+template <int DK, int DV, int NS, typename T, int TS>
 __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& sg, uint32_t slot,
                                                int h, bool rev, T* sK, T* sV, Gates* gt) {
   const int gr = a.Hv / a.Hk;
@@ -365,10 +376,11 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane ln = lane_here();
   const Chunks ch(sg, rev);
-  StateOf<DK, DV> S;
+  constexpr int NT = 4 * DV / NS;
+  StateOf<DK, DV, NS> S;
   S.zero();
-  Rows<DK, T> k;
-  Rows<DV, T> v;
+  Rows<DK, NT, T> k;
+  Rows<DV, NT, T> v;
   auto fetch = [&](int i) __attribute__((always_inline)) {
     const int at = ch.at(i), m = ch.size(i);
     k.load(K + (int64_t)at * ldk, ldk, m, rev);
@@ -395,8 +407,8 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
 }  // namespace
 
 // `both`: the gradients' states too, in the second half of the work items
-template <int DK, int DV, typename T, int TS>
-__global__ __launch_bounds__(256) void k_lin_state(const LinArgs a, uint32_t n, bool both) {
+template <int DK, int DV, int NS, typename T, int TS>
+__global__ __launch_bounds__(4 * DV / NS) void k_lin_state(const LinArgs a, uint32_t n, bool both) {
   __shared__ __attribute__((aligned(16))) T sK[LC * DK], sV[LC * DV];
   __shared__ __attribute__((aligned(16))) Gates gt[2];
   uint32_t w = work_item(blockIdx.x, n * (both ? 2 : 1));
@@ -408,7 +420,7 @@ __global__ __launch_bounds__(256) void k_lin_state(const LinArgs a, uint32_t n, 
   const Segment sg(a.q, slot);
   // (the last segment's share ends in S_final, the first one's in dS0: the walks form those)
   if (sg.len == 0 || (rev ? sg.j == 0 : sg.j == sg.n - 1)) return;
-  add_of_segment<DK, DV, T, TS>(a, sg, slot, h, rev, sK, sV, gt);
+  add_of_segment<DK, DV, NS, T, TS>(a, sg, slot, h, rev, sK, sV, gt);
 }
 
 // The states carried over the segments of each sequence, in place: U from what a segment
@@ -459,30 +471,46 @@ namespace {
 
 // One pass along a segment for one value head.
 struct Pass {
-  const void *q, *k, *v, *x;    // x: rows for the gradient of g (or null)
-  uint32_t ldq, ldk, ldv, ldo;  // values a token
+  const void *q, *k, *v;        // its tiles in LDS
+  const void* x;                // rows for the gradient of g, in memory or a tile
+  uint32_t ldo;                 // values a token of x and of the result
   void* out;
-  float* acc;                   // sums of a group's heads (null: one head)
+  float* acc;                   // sums of a group's heads (null: one head, or two side by side)
   bool first, last;             // of the group
   float* rows;                  // x's products of each token, at the segment's first
   const float* start;           // the state that enters (or null: zeros)
   float* fin;                   // the state that leaves (or null)
-  const float* against;         // the gradient of the state that leaves (or null: zeros)
-  float* anchor;                // X of the last chunk (or null)
-  bool flip, rev;               // flip: the state's transposed in memory
-  bool pairs;                   // rows: with the sums of M
-  float s_out, s_in;
+  const float* against;         // dK: the state that enters (or null: zeros)
+  float* anchor;                // dK: X of the segment's first chunk
 };
 
-template <int DK, int DV, typename T, int TP>
-struct PassLds {
-  typedef typename FragFor<T>::type F;
-  T q[LC * DK], k[LC * DK], v[LC * DV];
-  T p[6 * kTerms<F, TP> * 512];
-  float far[4][LC];              // the waves' shares of x . (what came from the state)
+// What a pass forms, and how.
+enum Kind { kO, kDQ, kDK, kDV };
+template <Kind P> constexpr bool kReversed = P == kDK || P == kDV;
+template <Kind P> constexpr bool kFlipped = P == kDQ || P == kDK;  // the state, in memory
+
+// What the waves of a pass share, beside its tiles.
+template <int NW, typename T, int TP>
+struct TeamLds {
+  T p[6 * kTerms<typename FragFor<T>::type, TP> * 512];
+  float far[NW][LC];             // the waves' shares of x . (what came from the state)
   float row[4][LC], col[4][LC];  // sums of M's blocks (I, J): along rows at J, down columns at I
-  float part[4];
+  float part[NW];
   Gates gt[2];
+};
+
+// The tiles of a workgroup, from where they come to LDS, and the passes that read them.
+template <int D, int NT, typename T>
+struct Source {
+  const T* p;
+  uint32_t ld;
+  T* s;
+  Rows<D, NT, T> r;
+  __device__ Source(const T* from, int heads, T* to) : p(from), ld((uint32_t)heads * D), s(to) {}
+  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
+    r.load(p + (int64_t)at * ld, ld, m, rev);
+  }
+  __device__ __forceinline__ void store(int m) const { r.store(s, m); }
 };
 
 // P's fragments of row block I: pair p of column blocks
@@ -492,31 +520,33 @@ template <typename T, int N> struct RunType { typedef T type __attribute__((ext_
 template <typename T, int N> using RunOf = typename RunType<T, N>::type;
 
 // Terms: TS of the decayed values that the state takes up, TO of the state, TP of P.
-template <int DK, int DV, typename T, int TS, int TO, int TP>
+// DG: with the rows that the gradient of g takes (of dQ and dK).  A team of NW waves walks;
+// two teams of a workgroup walk side by side on tiles that all of them bring, with the same
+// barriers.  other: what a second team gives a first one to add to its result (null: none).
+// XS: x is a tile (with dK), else rows in memory.
+template <int DK, int DV, int NS, typename T, int TS, int TO, int TP, Kind P, bool DG, bool XS,
+          typename Tiles>
 __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h, const Pass& ps,
-                                     PassLds<DK, DV, T, TP>* lds) {
+                                     Tiles& tiles, TeamLds<DV / 16 / NS, T, TP>* lds,
+                                     float* other = nullptr) {
   typedef typename FragFor<T>::type F;
-  constexpr int NQ = DK / 32, NS = DV / 64, MO = kTerms<F, TO>, MP = kTerms<F, TP>;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int NQ = DK / 32, NW = DV / 16 / NS, MO = kTerms<F, TO>, MP = kTerms<F, TP>;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % NW;
   const Lane ln = lane_here();
   const int g4 = 4 * ln.g(), c = ln.c();
-  const bool rev = ps.rev;
+  constexpr bool rev = kReversed<P>, flip = kFlipped<P>;
+  constexpr bool far_rows = DG && flip, pairs = DG && P == kDK;
   const Chunks ch(sg, rev);
-  StateOf<DK, DV> S;
-  if (ps.start) S.load(ps.start, ps.flip, w, ln); else S.zero();
-  Rows<DK, T> q, k;
-  Rows<DV, T> v;
-  auto fetch = [&](int i) __attribute__((always_inline)) {
-    const int at = ch.at(i), m = ch.size(i);
-    q.load((const T*)ps.q + (int64_t)at * ps.ldq, ps.ldq, m, rev);
-    k.load((const T*)ps.k + (int64_t)at * ps.ldk, ps.ldk, m, rev);
-    v.load((const T*)ps.v + (int64_t)at * ps.ldv, ps.ldv, m, rev);
-  };
+  StateOf<DK, DV, NS> S;
+  if (ps.start) S.load(ps.start, flip, w, ln); else S.zero();
+  const T *sq = (const T*)ps.q, *sk = (const T*)ps.k, *sv = (const T*)ps.v;
   // what the gradient of g takes of a chunk: the waves' shares meet in LDS
   auto write_rows = [&](int i) __attribute__((always_inline)) {
-    if (!ps.x || w != 3 || i < 0 || ln.id >= ch.size(i)) return;
-    float f = (lds->far[0][ln.id] + lds->far[1][ln.id]) + (lds->far[2][ln.id] + lds->far[3][ln.id]);
-    if (ps.pairs) {
+    if (!far_rows || w != 3 || i < 0 || ln.id >= ch.size(i)) return;
+    float f = 0.f;
+#pragma unroll
+    for (int u = 0; u < NW; ++u) f += lds->far[u][ln.id];
+    if (pairs) {
       float e = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -527,8 +557,8 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     }
     ps.rows[ch.token(i, ln.id)] = f;
   };
-  GateStream gates(a, sg, ch, h, w == 2, ps.s_out, ps.s_in);
-  fetch(0);
+  GateStream gates(a, sg, ch, h, w == 2, rev ? 1.f : a.scale, rev ? a.scale : 1.f);
+  tiles.fetch(ch.at(0), ch.size(0), rev);
   gates.form(lds->gt, 0);
   // P's blocks above the diagonal that share a pair with one on it
   if (w < 2) {
@@ -546,19 +576,17 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     const bool end = i == ch.n - 1;
     const Gates* gt = lds->gt + (i & 1);
     lds_only_barrier();
-    q.store(lds->q, m);
-    k.store(lds->k, m);
-    v.store(lds->v, m);
+    tiles.store(m);
     write_rows(i - 1);
     lds_only_barrier();
-    if (ps.anchor && end) {
+    if (pairs && end) {
       float x = 0.f;
       if (ps.against) {
 #pragma unroll
         for (int u = 0; u < 2 * NQ; ++u)
 #pragma unroll
           for (int n = 0; n < NS; ++n) {
-            const f32x4 y = StateOf<DK, DV>::block(ps.against, ps.flip, u, n, w, ln);
+            const f32x4 y = StateOf<DK, DV, NS>::block(ps.against, flip, u, n, w, ln);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x = __builtin_fmaf(S.b[u][n][e], y[e], x);
           }
@@ -566,25 +594,55 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       }
       if (ln.id == 0) lds->part[w] = x;
     }
-    // P's blocks in row form: lane (g, c) has columns 16 J + 4g .. of row 16 I + c
-    for (int b = w; b < 10; b += 4) {
-      const int I = b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3, J = b - I * (I + 1) / 2;
-      const int r = 16 * I + c;
-      f32x4 p = zero4(), p1 = zero4();
+    // rows of x at the results' places
+    RunOf<T, 4 * NS> xr[4];
+    if constexpr (far_rows && !XS)
+#pragma unroll
+      for (int I = 0; I < 4; ++I)
+        xr[I] = *(const RunOf<T, 4 * NS>*)((const T*)ps.x +
+                                           (int64_t)ch.token(i, min(16 * I + c, m - 1)) * ps.ldo +
+                                           16 * NS * w + NS * g4);
+    // P's blocks in row form: lane (g, c) has columns 16 J + 4g .. of row 16 I + c; two of them
+    // at a time
+    auto products = [&](int I, int J) __attribute__((always_inline)) {
+      f32x4 p0 = zero4(), p1 = zero4();
 #pragma unroll
       for (int s = 0; s < NQ; s += 2) {
-        p = Pair<F>::template mma<true>(run_frag<DK>(lds->q, 16 * I, 32 * s, ln),
-                                        run_frag<DK>(lds->k, 16 * J, 32 * s, ln), p);
-        p1 = Pair<F>::template mma<true>(run_frag<DK>(lds->q, 16 * I, 32 * s + 32, ln),
-                                         run_frag<DK>(lds->k, 16 * J, 32 * s + 32, ln), p1);
+        p0 = Pair<F>::template mma<true>(run_frag<DK>(sq, 16 * I, 32 * s, ln),
+                                         run_frag<DK>(sk, 16 * J, 32 * s, ln), p0);
+        p1 = Pair<F>::template mma<true>(run_frag<DK>(sq, 16 * I, 32 * s + 32, ln),
+                                         run_frag<DK>(sk, 16 * J, 32 * s + 32, ln), p1);
       }
+      return p0 + p1;
+    };
+    // X V^T, for M
+    auto more_products = [&](int I, int J) __attribute__((always_inline)) {
+      f32x4 p0 = zero4(), p1 = zero4();
+#pragma unroll
+      for (int s = 0; s < DV / 32; s += 2) {
+        Pair<F> x0, x1;
+        if constexpr (XS) {
+          x0 = run_frag<DV>((const T*)ps.x, 16 * I, 32 * s, ln);
+          x1 = run_frag<DV>((const T*)ps.x, 16 * I, 32 * s + 32, ln);
+        } else {
+          const T* xp = (const T*)ps.x + (int64_t)ch.token(i, min(16 * I + c, m - 1)) * ps.ldo +
+                        32 * s + 2 * g4;
+          x0 = load_run8<F>(xp), x1 = load_run8<F>(xp + 32);
+        }
+        p0 = Pair<F>::template mma<true>(x0, run_frag<DV>(sv, 16 * J, 32 * s, ln), p0);
+        p1 = Pair<F>::template mma<true>(x1, run_frag<DV>(sv, 16 * J, 32 * s + 32, ln), p1);
+      }
+      return p0 + p1;
+    };
+    auto finish = [&](f32x4 p, f32x4 y, int I, int J) __attribute__((always_inline)) {
+      const int r = 16 * I + c;
       const float hi = gt->hi[r], lo = gt->lo[r];
       const f32x4 hj = *(const f32x4*)(gt->hi + 16 * J + g4);
       const f32x4 lj = *(const f32x4*)(gt->lo + 16 * J + g4);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const float d = __builtin_amdgcn_exp2f((hi - hj[u]) + (lo - lj[u]));
-        p[u] = 16 * J + g4 + u <= r ? a.scale * (p[u] + p1[u]) * d : 0.f;
+        p[u] = 16 * J + g4 + u <= r ? a.scale * p[u] * d : 0.f;
       }
       T* to = lds->p + p_slot(I, J >> 1) * MP * 512;
       if constexpr (sizeof(T) == 4) {
@@ -594,32 +652,39 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
         float p0 = p[0], p1 = p[1], p2 = p[2], p3 = p[3];
 #pragma unroll
         for (int t = 0; t < MP; ++t) {
-          const uint32_t x = take2(p0, p1), y = take2(p2, p3);
-          *(u32x2*)(to + t * 512 + 8 * ln.id + 4 * (J & 1)) = u32x2{x, y};
+          const uint32_t x = take2(p0, p1), z = take2(p2, p3);
+          *(u32x2*)(to + t * 512 + 8 * ln.id + 4 * (J & 1)) = u32x2{x, z};
         }
       }
-      if (ps.pairs) {  // M, of i > j: P (.) (X V^T)
-        f32x4 y = zero4();
-        const T* xp = (const T*)ps.x + (int64_t)ch.token(i, min(r, m - 1)) * ps.ldo;
-#pragma unroll
-        for (int s = 0; s < DV / 32; ++s) {
-          Pair<F> x;
-          if constexpr (sizeof(T) == 4)
-            x = join(*(const f32x4*)(xp + 32 * s + 2 * g4), *(const f32x4*)(xp + 32 * s + 2 * g4 + 4));
-          else
-            x.v = *(const bf16x8*)(xp + 32 * s + 2 * g4);
-          y = Pair<F>::template mma<true>(x, run_frag<DV>(lds->v, 16 * J, 32 * s, ln), y);
-        }
+      if constexpr (pairs) {  // M, of rows below the diagonal
         float sum = 0.f;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          y[u] = 16 * J + g4 + u < r ? y[u] * p[u] : 0.f;
+          y[u] = 16 * J + g4 + u < r && r < m ? y[u] * p[u] : 0.f;
           sum += y[u];
           y[u] = sum16(y[u]);
         }
         sum = sum_apart32(sum_apart16(sum));
         if (ln.g() == 0) lds->row[J][r] = sum;
         if (c == 0) *(f32x4*)(lds->col[I] + 16 * J + g4) = y;
+      }
+    };
+    auto row_of = [](int b) { return b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3; };
+    static_assert(NW >= 4, "two blocks a wave and two over");
+    {
+      const int b1 = w + NW < 10 ? w + NW : w;  // (of eight waves six repeat their block)
+      const int I0 = row_of(w), J0 = w - I0 * (I0 + 1) / 2, I1 = row_of(b1), J1 = b1 - I1 * (I1 + 1) / 2;
+      const f32x4 p0 = products(I0, J0), p1 = products(I1, J1);
+      f32x4 y0 = zero4(), y1 = zero4();
+      if constexpr (pairs) y0 = more_products(I0, J0), y1 = more_products(I1, J1);
+      finish(p0, y0, I0, J0);
+      if (b1 != w) finish(p1, y1, I1, J1);
+      if (NW == 4 && w < 2) {
+        const int J = w + 2;  // blocks 8 and 9
+        f32x4 y = zero4();
+        const f32x4 p = products(3, J);
+        if constexpr (pairs) y = more_products(3, J);
+        finish(p, y, 3, J);
       }
     }
     gates.form(lds->gt, i + 1);
@@ -638,7 +703,7 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       for (int I0 = 0; I0 < 4; I0 += 2) {
         Pair<F> x[2];
 #pragma unroll
-        for (int I = 0; I < 2; ++I) x[I] = run_frag<DK>(lds->q, 16 * (I0 + I), 32 * s, ln);
+        for (int I = 0; I < 2; ++I) x[I] = run_frag<DK>(sq, 16 * (I0 + I), 32 * s, ln);
 #pragma unroll
         for (int t = MO - 1; t >= 0; --t)
 #pragma unroll
@@ -658,32 +723,37 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
 #pragma unroll
       for (int n = 0; n < NS; ++n) o[I][n] *= f;
     }
-    if (ps.x)
+    if constexpr (far_rows)
 #pragma unroll
       for (int I = 0; I < 4; ++I) {
+        if constexpr (XS)
+          xr[I] = *(const RunOf<T, 4 * NS>*)((const T*)ps.x + 16 * I * DV +
+                                             Tile<DV, T>::at(c, 16 * NS * w + NS * g4));
         float far = 0.f;
-        if (16 * I + c < m) {
-          const auto x = *(const RunOf<T, 4 * NS>*)((const T*)ps.x + chunk + (row0 + I * down));
 #pragma unroll
-          for (int n = 0; n < NS; ++n)
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) far = __builtin_fmaf((float)x[4 * n + u], o[I][n][u], far);
-        }
+          for (int u = 0; u < 4; ++u)
+            far = __builtin_fmaf((float)xr[I][4 * n + u], o[I][n][u], far);
         far = sum_apart32(sum_apart16(far));
         if (ln.g() == 0) lds->far[w][16 * I + c] = far;
       }
-    if (!end) fetch(i + 1);
-    S.template update<TS>(lds->k, lds->v, gt, w, ln);
+    if (!end) tiles.fetch(ch.at(i + 1), ch.size(i + 1), rev);
+    S.template update<TS>(sk, sv, gt, w, ln);
     lds_only_barrier();
-    if (ps.anchor && end && threadIdx.x == 0)
-      *ps.anchor = gt->el * ((lds->part[0] + lds->part[1]) + (lds->part[2] + lds->part[3]));
+    if (pairs && end && w == 0 && ln.id == 0) {
+      float x = 0.f;
+#pragma unroll
+      for (int u = 0; u < NW; ++u) x += lds->part[u];
+      *ps.anchor = gt->el * x;
+    }
     // and from the chunk's tokens
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       Pair<F> y[NS];
 #pragma unroll
       for (int n = 0; n < NS; ++n)
-        y[n] = down_frag<DV, 4 * NS>(lds->v, 32 * p, 16 * NS * w + 4 * n, ln);
+        y[n] = down_frag<DV, 4 * NS>(sv, 32 * p, 16 * NS * w + 4 * n, ln);
 #pragma unroll
       for (int t = MP - 1; t >= 0; --t)
 #pragma unroll
@@ -698,6 +768,21 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
           for (int n = 0; n < NS; ++n) o[I][n] = Pair<F>::template mma<true>(x, y[n], o[I][n]);
         }
     }
+    if (other) {
+      if (wave >= NW)
+#pragma unroll
+        for (int I = 0; I < 4; ++I)
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+            *(f32x4*)(other + (((w * 4 + I) * NS + n) * 64 + ln.id) * 4) = o[I][n];
+      lds_only_barrier();
+      if (wave >= NW) continue;
+#pragma unroll
+      for (int I = 0; I < 4; ++I)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+          o[I][n] += *(const f32x4*)(other + (((w * 4 + I) * NS + n) * 64 + ln.id) * 4);
+    }
     typedef T Out __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int I = 0; I < 4; ++I)
@@ -706,18 +791,56 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
         for (int n = 0; n < NS; ++n) {
           const uint32_t to = row0 + I * down + 4 * n;
           f32x4 y = o[I][n];
-          if (ps.acc && !ps.first) y += *(const f32x4*)(ps.acc + chunk + to);
-          if (ps.acc && !ps.last)
+          if (flip && ps.acc && !ps.first) y += *(const f32x4*)(ps.acc + chunk + to);
+          if (flip && ps.acc && !ps.last)
             *(f32x4*)(ps.acc + chunk + to) = y;
           else
             *(Out*)((T*)ps.out + chunk + to) = __builtin_convertvector(y, Out);
         }
   }
-  if (ps.fin) S.store(ps.fin, ps.flip, w, ln);
-  if (!ps.x) return;
+  if (!flip && ps.fin) S.store(ps.fin, flip, w, ln);
+  if (!far_rows) return;
   lds_only_barrier();
   write_rows(ch.n - 1);
 }
+
+// The tiles of one pass.
+template <int DK, int DV, int NT, typename T>
+struct PassTiles {
+  Source<DK, NT, T> q, k;
+  Source<DV, NT, T> v;
+  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
+    q.fetch(at, m, rev), k.fetch(at, m, rev), v.fetch(at, m, rev);
+  }
+  __device__ __forceinline__ void store(int m) const { q.store(m), k.store(m), v.store(m); }
+};
+// Two of one kind each: of DA and of DB values a row.
+template <int DA, int DB, int NT, typename T>
+struct TwoAndTwo {
+  Source<DA, NT, T> a0, a1;
+  Source<DB, NT, T> b0, b1;
+  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
+    a0.fetch(at, m, rev), a1.fetch(at, m, rev), b0.fetch(at, m, rev), b1.fetch(at, m, rev);
+  }
+  __device__ __forceinline__ void store(int m) const {
+    a0.store(m), a1.store(m), b0.store(m), b1.store(m);
+  }
+};
+// Those of dQ or dK of two heads, MORE: with x.
+template <int DA, int DB, int NT, typename T, bool MORE>
+struct FourAndMore {
+  Source<DA, NT, T> a0, a1, a2, a3;
+  Source<DB, NT, T> b0, b1;
+  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
+    a0.fetch(at, m, rev), a1.fetch(at, m, rev), a2.fetch(at, m, rev), a3.fetch(at, m, rev);
+    b0.fetch(at, m, rev);
+    if (MORE) b1.fetch(at, m, rev);
+  }
+  __device__ __forceinline__ void store(int m) const {
+    a0.store(m), a1.store(m), a2.store(m), a3.store(m), b0.store(m);
+    if (MORE) b1.store(m);
+  }
+};
 
 // sequences without tokens: the state stays what it was
 __device__ __forceinline__ void copy_state(const LinArgs& a, int s, const float* from, float* to) {
@@ -726,16 +849,23 @@ __device__ __forceinline__ void copy_state(const LinArgs& a, int s, const float*
   a.q.at(s, t0, base, len);
   if (len > 0) return;
   const int64_t n = (int64_t)a.Hv * a.dk * a.dv, at = (int64_t)s * n;
-  for (int64_t e = threadIdx.x * 4; e < n; e += 1024)
+  for (int64_t e = threadIdx.x * 4; e < n; e += 4 * blockDim.x)
     *(f32x4*)(to + at + e) = from ? *(const f32x4*)(from + at + e) : zero4();
 }
 
 }  // namespace
 
-template <int DK, int DV, typename T, int TS, int TO, int TP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_forward(const LinArgs a,
-                                                                            uint32_t n) {
-  __shared__ __attribute__((aligned(16))) PassLds<DK, DV, T, TP> lds;
+// waves a SIMD: two workgroups a CU, with fp32 inputs one
+template <typename T> constexpr int waves_of(int threads) {
+  return threads / 256 * (sizeof(T) == 2 ? 2 : 1);
+}
+
+template <int DK, int DV, int NS, typename T, int TS, int TO, int TP>
+__global__ __launch_bounds__(4 * DV / NS, waves_of<T>(4 * DV / NS)) void k_lin_forward(
+    const LinArgs a, uint32_t n) {
+  constexpr int NT = 4 * DV / NS;
+  __shared__ __attribute__((aligned(16))) T sq[LC * DK], sk[LC * DK], sv[LC * DV];
+  __shared__ __attribute__((aligned(16))) TeamLds<DV / 16 / NS, T, TP> lds;
   const uint32_t blocks = (n + 7) & ~7u;
   if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.S0, a.Sf);
   const uint32_t w = work_item(blockIdx.x, n);
@@ -745,92 +875,206 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_forward(con
   const Segment sg(a.q, slot);
   if (sg.len == 0) return;
   const int64_t size = DK * DV, own = ((int64_t)sg.s * a.Hv + h) * size;
+  const int64_t tk = (sg.t0 * a.Hk + hk) * DK, tv = (sg.t0 * a.Hv + h) * DV;
+  PassTiles<DK, DV, NT, T> tiles{{(const T*)a.Q + tk, a.Hk, sq},
+                                 {(const T*)a.K + tk, a.Hk, sk},
+                                 {(const T*)a.V + tv, a.Hv, sv}};
   Pass ps{};
-  ps.ldq = ps.ldk = (uint32_t)a.Hk * DK, ps.ldv = ps.ldo = (uint32_t)a.Hv * DV;
-  ps.q = (const T*)a.Q + (sg.t0 * a.Hk + hk) * DK;
-  ps.k = (const T*)a.K + (sg.t0 * a.Hk + hk) * DK;
-  ps.v = (const T*)a.V + (sg.t0 * a.Hv + h) * DV;
-  ps.out = (T*)a.O + (sg.t0 * a.Hv + h) * DV;
+  ps.q = sq, ps.k = sk, ps.v = sv;
+  ps.ldo = (uint32_t)a.Hv * DV;
+  ps.out = (T*)a.O + tv;
   ps.start = a.U ? a.U + ((int64_t)slot * a.Hv + h) * size : a.S0 ? a.S0 + own : nullptr;
   ps.fin = a.Sf && sg.j == sg.n - 1 ? a.Sf + own : nullptr;
-  ps.s_out = a.scale, ps.s_in = 1.f;
-  walk<DK, DV, T, TS, TO, TP>(a, sg, h, ps, &lds);
+  walk<DK, DV, NS, T, TS, TO, TP, kO, false, false>(a, sg, h, ps, tiles, &lds);
 }
 
-// Three passes: dQ and dK by key heads (the heads of a group one after the other), dV by
-// value heads.
-template <int DK, int DV, typename T, int TS, int TO, int TP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(const LinArgs a,
-                                                                             uint32_t slots) {
-  union Lds {
-    PassLds<DV, DK, T, TP> qk;
-    PassLds<DK, DV, T, TP> v;
-  };
-  __shared__ __attribute__((aligned(16))) Lds lds;
-  const uint32_t nk = slots * (uint32_t)a.Hk, nv = slots * (uint32_t)a.Hv;
+// ---- the gradients.  A workgroup is two teams of four waves on common tiles (read apart, the
+// tiles of the passes came from HBM each time: they run at different places of a segment):
+// of a group of two heads, or each two of a larger even one, dQ, dK or dV of both (the first
+// team adds up dQ and dK); of one head, or of an odd group's one after the other, dK and dV,
+// and dQ by a team of its own.
+
+namespace {
+
+// What dQ (or dK) of value head h takes and gives.
+template <int DK, int DV, typename T, Kind P, bool DG>
+__device__ __forceinline__ Pass key_pass(const LinArgs& a, const Segment& sg, uint32_t slot, int hk,
+                                         int h) {
+  constexpr bool rev = P == kDK;
+  constexpr int64_t size = DK * DV;
+  const int64_t tk = (sg.t0 * a.Hk + hk) * DK;
+  const int64_t own = ((int64_t)sg.s * a.Hv + h) * size, at = ((int64_t)slot * a.Hv + h) * size;
+  const float* S = a.U ? a.U + at : a.S0 ? a.S0 + own : nullptr;
+  Pass ps{};
+  ps.ldo = (uint32_t)a.Hk * DK;
+  ps.out = (T*)(rev ? a.dK : a.dQ) + tk;
+  ps.start = !rev ? S : a.R ? a.R + at : a.dSf ? a.dSf + own : nullptr;
+  if (DG) {
+    const int64_t tokens = a.q.cu ? (int64_t)a.q.T : (int64_t)a.q.nseq * a.q.T;
+    ps.x = (const T*)(rev ? a.K : a.Q) + tk;
+    ps.rows = (rev ? a.rows_k : a.rows_q) + h * tokens + sg.t0;
+    ps.against = S;
+    ps.anchor = a.anchor + (int64_t)slot * a.Hv + h;
+  }
+  return ps;
+}
+template <int DK, int DV, typename T>
+__device__ __forceinline__ Pass value_pass(const LinArgs& a, const Segment& sg, uint32_t slot,
+                                           int h) {
+  constexpr int64_t size = DK * DV;
+  const int64_t own = ((int64_t)sg.s * a.Hv + h) * size;
+  Pass ps{};
+  ps.ldo = (uint32_t)a.Hv * DV;
+  ps.out = (T*)a.dV + (sg.t0 * a.Hv + h) * DV;
+  ps.start = a.R ? a.R + ((int64_t)slot * a.Hv + h) * size : a.dSf ? a.dSf + own : nullptr;
+  ps.fin = a.dS0 && sg.j == 0 ? a.dS0 + own : nullptr;
+  return ps;
+}
+
+// dQ or dK of a key head with an even group: its value heads two by two
+template <int DK, int DV, typename T, int TS, int TO, int TP, Kind P, bool DG>
+__device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segment& sg,
+                                                    uint32_t slot, int hk, T* s, float* other,
+                                                    TeamLds<4, T, TP>* lds) {
+  constexpr bool rev = P == kDK, more = rev && DG;
+  const int gr = a.Hv / a.Hk, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  constexpr int VT = LC * DV, KT = LC * DK;
+  const int64_t tk = (sg.t0 * a.Hk + hk) * DK;
+  for (int u = 0; u < gr; u += 2) {
+    const int h = hk * gr + u;
+    const T* q = (const T*)(rev ? a.V : a.dO) + (sg.t0 * a.Hv + h) * DV;
+    const T* k = (const T*)(rev ? a.dO : a.V) + (sg.t0 * a.Hv + h) * DV;
+    const T *v = (const T*)(rev ? a.Q : a.K) + tk, *x = (const T*)a.K + tk;
+    FourAndMore<DV, DK, 512, T, more> tiles{{q, a.Hv, s},
+                                            {k, a.Hv, s + VT},
+                                            {q + DV, a.Hv, s + 2 * VT},
+                                            {k + DV, a.Hv, s + 3 * VT},
+                                            {v, a.Hk, s + 4 * VT},
+                                            {x, a.Hk, s + 4 * VT + KT}};
+    Pass ps = key_pass<DK, DV, T, P, DG>(a, sg, slot, hk, h + team);
+    ps.q = s + 2 * team * VT, ps.k = s + (2 * team + 1) * VT, ps.v = s + 4 * VT;
+    if (more) ps.x = s + 4 * VT + KT;
+    ps.acc = gr > 2 ? (rev ? a.acc_k : a.acc_q) + tk : nullptr;
+    ps.first = u == 0, ps.last = u == gr - 2;
+    walk<DV, DK, DK / 64, T, TS, TO, TP, P, DG, more>(a, sg, h + team, ps, tiles, lds + team, other);
+    lds_only_barrier();
+  }
+}
+
+}  // namespace
+
+// groups of even size
+template <int DK, int DV, typename T, int TS, int TO, int TP, bool DG>
+__global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a, uint32_t slots) {
+  // the second team's results go where the tiles of products lie, which the first has done with
+  __shared__ __attribute__((aligned(16))) T s[LC * (4 * DV + (DG ? 2 : 1) * DK)];
+  static_assert(4 * DV * sizeof(T) >= DK * sizeof(float) && 2 * DV >= DK, "what else lies there");
+  float* other = (float*)s;
+  __shared__ __attribute__((aligned(16))) TeamLds<4, T, TP> lds[2];
+  const uint32_t nk = slots * (uint32_t)a.Hk, nv = slots * (uint32_t)(a.Hv / 2);
   const uint32_t bk = (2 * nk + 7) & ~7u, bv = (nv + 7) & ~7u;
-  const int64_t size = DK * DV;
   if (blockIdx.x >= bk + bv) return copy_state(a, (int)(blockIdx.x - bk - bv), a.dSf, a.dS0);
-  const int gr = a.Hv / a.Hk;
-  if (blockIdx.x < bk) {
-    uint32_t w = work_item(blockIdx.x, 2 * nk);
-    if (w >= 2 * nk) return;
-    const bool rev = w >= nk;
-    if (rev) w -= nk;
-    const uint32_t slot = w / (uint32_t)a.Hk;
-    const int hk = (int)(w - slot * (uint32_t)a.Hk);
-    const Segment sg(a.q, slot);
-    if (sg.len == 0) return;
-    const int64_t tk = (sg.t0 * a.Hk + hk) * DK;
-    for (int u = 0; u < gr; ++u) {
-      const int h = hk * gr + u;
-      const int64_t tv = (sg.t0 * a.Hv + h) * DV, own = ((int64_t)sg.s * a.Hv + h) * size;
-      const int64_t at = ((int64_t)slot * a.Hv + h) * size;
-      const int64_t tokens = a.q.cu ? (int64_t)a.q.T : (int64_t)a.q.nseq * a.q.T;
-      const float* dS = a.R ? a.R + at : a.dSf ? a.dSf + own : nullptr;
-      Pass ps{};
-      ps.ldq = ps.ldk = (uint32_t)a.Hv * DV, ps.ldv = ps.ldo = (uint32_t)a.Hk * DK;
-      ps.q = (const T*)(rev ? a.V : a.dO) + tv;
-      ps.k = (const T*)(rev ? a.dO : a.V) + tv;
-      ps.v = (const T*)(rev ? a.Q : a.K) + tk;
-      ps.out = (T*)(rev ? a.dK : a.dQ) + tk;
-      ps.acc = gr > 1 ? (rev ? a.acc_k : a.acc_q) + tk : nullptr;
-      ps.first = u == 0, ps.last = u == gr - 1;
-      ps.flip = true, ps.rev = rev;
-      if (a.want_dg) {
-        ps.x = (const T*)(rev ? a.K : a.Q) + tk;
-        ps.rows = (rev ? a.rows_k : a.rows_q) + h * tokens + sg.t0;
-        ps.pairs = !rev;
-      }
-      if (rev) {
-        ps.start = dS;
-        ps.s_out = 1.f, ps.s_in = a.scale;
-      } else {
-        ps.start = a.U ? a.U + at : a.S0 ? a.S0 + own : nullptr;
-        ps.s_out = a.scale, ps.s_in = 1.f;
-        if (a.want_dg) ps.against = dS, ps.anchor = a.anchor + (int64_t)slot * a.Hv + h;
-      }
-      walk<DV, DK, T, TS, TO, TP>(a, sg, h, ps, &lds.qk);
-      lds_only_barrier();
-    }
+  const bool keys = blockIdx.x < bk;
+  const uint32_t w = keys ? work_item(blockIdx.x, 2 * nk) : work_item(blockIdx.x - bk, nv);
+  if (w >= (keys ? 2 * nk : nv)) return;
+  const uint32_t heads = (uint32_t)(keys ? a.Hk : a.Hv / 2), v = keys && w >= nk ? w - nk : w;
+  const uint32_t slot = v / heads;
+  const int i = (int)(v - slot * heads);
+  const Segment sg(a.q, slot);
+  if (sg.len == 0) return;
+  if (keys && w >= nk) {
+    key_gradient_by_two<DK, DV, T, TS, TO, TP, kDK, DG>(a, sg, slot, i, s, other, lds);
+  } else if (keys) {
+    key_gradient_by_two<DK, DV, T, TS, TO, TP, kDQ, DG>(a, sg, slot, i, s, other, lds);
   } else {
-    const uint32_t w = work_item(blockIdx.x - bk, nv);
-    if (w >= nv) return;
-    const uint32_t slot = w / (uint32_t)a.Hv;
-    const int h = (int)(w - slot * (uint32_t)a.Hv), hk = h / gr;
-    const Segment sg(a.q, slot);
-    if (sg.len == 0) return;
+    const int team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), h = 2 * i;
+    const int64_t tk = (sg.t0 * a.Hk + h / (a.Hv / a.Hk)) * DK, tv = (sg.t0 * a.Hv + h) * DV;
+    constexpr int KT = LC * DK, VT = LC * DV;
+    TwoAndTwo<DK, DV, 512, T> tiles{{(const T*)a.K + tk, a.Hk, s},
+                                    {(const T*)a.Q + tk, a.Hk, s + KT},
+                                    {(const T*)a.dO + tv, a.Hv, s + 2 * KT},
+                                    {(const T*)a.dO + tv + DV, a.Hv, s + 2 * KT + VT}};
+    Pass ps = value_pass<DK, DV, T>(a, sg, slot, h + team);
+    ps.q = s, ps.k = s + KT, ps.v = s + 2 * KT + team * VT;
+    walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles, lds + team);
+  }
+}
+
+// dK and dV of a key head's value heads one after the other
+template <int DK, int DV, typename T, int TS, int TO, int TP, bool DG>
+__global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uint32_t slots) {
+  constexpr int KT = LC * DK, VT = LC * DV;
+  __shared__ __attribute__((aligned(16))) T s[2 * KT + 2 * VT];
+  __shared__ __attribute__((aligned(16))) TeamLds<4, T, TP> lds[2];
+  const uint32_t n = slots * (uint32_t)a.Hk, blocks = (n + 7) & ~7u;
+  if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.dSf, a.dS0);
+  const uint32_t w = work_item(blockIdx.x, n);
+  if (w >= n) return;
+  const uint32_t slot = w / (uint32_t)a.Hk;
+  const int hk = (int)(w - slot * (uint32_t)a.Hk), gr = a.Hv / a.Hk;
+  const int team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const Segment sg(a.q, slot);
+  if (sg.len == 0) return;
+  T *sQ = s, *sK = s + KT, *sV = s + 2 * KT, *sO = s + 2 * KT + VT;
+  for (int u = 0; u < gr; ++u) {
+    const int h = hk * gr + u;
     const int64_t tk = (sg.t0 * a.Hk + hk) * DK, tv = (sg.t0 * a.Hv + h) * DV;
-    const int64_t own = ((int64_t)sg.s * a.Hv + h) * size;
-    Pass ps{};
-    ps.ldq = ps.ldk = (uint32_t)a.Hk * DK, ps.ldv = ps.ldo = (uint32_t)a.Hv * DV;
-    ps.q = (const T*)a.K + tk, ps.k = (const T*)a.Q + tk, ps.v = (const T*)a.dO + tv;
-    ps.out = (T*)a.dV + tv;
-    ps.start = a.R ? a.R + ((int64_t)slot * a.Hv + h) * size : a.dSf ? a.dSf + own : nullptr;
-    ps.fin = a.dS0 && sg.j == 0 ? a.dS0 + own : nullptr;
-    ps.rev = true;
-    ps.s_out = 1.f, ps.s_in = a.scale;
-    walk<DK, DV, T, TS, kOut, TP>(a, sg, h, ps, &lds.v);
+    TwoAndTwo<DK, DV, 512, T> tiles{{(const T*)a.Q + tk, a.Hk, sQ},
+                                    {(const T*)a.K + tk, a.Hk, sK},
+                                    {(const T*)a.V + tv, a.Hv, sV},
+                                    {(const T*)a.dO + tv, a.Hv, sO}};
+    if (team == 0) {
+      Pass ps = key_pass<DK, DV, T, kDK, DG>(a, sg, slot, hk, h);
+      ps.q = sV, ps.k = sO, ps.v = sQ, ps.x = sK;
+      ps.acc = gr > 1 ? a.acc_k + tk : nullptr;
+      ps.first = u == 0, ps.last = u == gr - 1;
+      walk<DV, DK, DK / 64, T, TS, TO, TP, kDK, DG, true>(a, sg, h, ps, tiles, lds);
+    } else {
+      Pass ps = value_pass<DK, DV, T>(a, sg, slot, h);
+      ps.q = sK, ps.k = sQ, ps.v = sO;
+      walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h, ps, tiles, lds + 1);
+      if (DG) lds_only_barrier();  // (the other team's, before its last rows)
+    }
+    lds_only_barrier();
+  }
+}
+
+// one of the gradients by a team of its own
+template <int DK, int DV, typename T, int TS, int TO, int TP, Kind P, bool DG>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(const LinArgs a,
+                                                                             uint32_t n) {
+  constexpr bool keys = kFlipped<P>;
+  constexpr int D0 = keys ? DV : DK, D1 = keys ? DK : DV;  // of the products, of the result
+  __shared__ __attribute__((aligned(16))) T sq[LC * D0], sk[LC * D0], sv[LC * D1];
+  __shared__ __attribute__((aligned(16))) TeamLds<4, T, TP> lds;
+  const uint32_t blocks = (n + 7) & ~7u;
+  if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.dSf, a.dS0);
+  const uint32_t w = work_item(blockIdx.x, n);
+  if (w >= n) return;
+  const uint32_t heads = (uint32_t)(keys ? a.Hk : a.Hv), slot = w / heads;
+  const int i = (int)(w - slot * heads), gr = a.Hv / a.Hk, hk = keys ? i : i / gr;
+  const Segment sg(a.q, slot);
+  if (sg.len == 0) return;
+  const T *Q = (const T*)a.Q, *K = (const T*)a.K, *V = (const T*)a.V, *dO = (const T*)a.dO;
+  for (int u = 0; u < (keys ? gr : 1); ++u) {
+    const int h = keys ? hk * gr + u : i;
+    const int64_t tk = (sg.t0 * a.Hk + hk) * DK, tv = (sg.t0 * a.Hv + h) * DV;
+    const int Hq = keys ? a.Hv : a.Hk, Ho = keys ? a.Hk : a.Hv;
+    PassTiles<D0, D1, 256, T> tiles{
+        {P == kDQ ? dO + tv : P == kDK ? V + tv : K + tk, Hq, sq},
+        {P == kDQ ? V + tv : P == kDK ? dO + tv : Q + tk, Hq, sk},
+        {P == kDQ ? K + tk : P == kDK ? Q + tk : dO + tv, Ho, sv}};
+    Pass ps;
+    if constexpr (keys) {
+      ps = key_pass<DK, DV, T, P, DG>(a, sg, slot, hk, h);
+      ps.acc = gr > 1 ? (P == kDK ? a.acc_k : a.acc_q) + tk : nullptr;
+      ps.first = u == 0, ps.last = u == gr - 1;
+    } else {
+      ps = value_pass<DK, DV, T>(a, sg, slot, h);
+    }
+    ps.q = sq, ps.k = sk, ps.v = sv;
+    walk<D0, D1, D1 / 64, T, TS, TO, TP, P, DG, false>(a, sg, h, ps, tiles, &lds);
+    lds_only_barrier();
   }
 }
 
@@ -855,8 +1099,8 @@ __global__ __launch_bounds__(256) void k_lin_decay(const LinArgs a) {
   __syncthreads();
   float all = 0.f;
   for (int c = w; c < nc; c += 4) {
-    float x = a.anchor[at];  // X of the last chunk, and from there X of this one
-    for (int i = nc - 1; i > c; --i) x += sq[i] - sk[i - 1];
+    float x = a.anchor[at];  // X of the first chunk, and from there X of this one
+    for (int i = 1; i <= c; ++i) x += sk[i - 1] - sq[i];
     const int t = c * LC + l;
     const float q = t < sg.len ? rq[t] : 0.f, k = t < sg.len ? rk[t] : 0.f;
     const double pq = prefix64((double)q), pk = prefix64((double)k);
@@ -927,11 +1171,13 @@ namespace {
 hipError_t launch_states(const LinArgs& a, int dtype, bool both, hipStream_t st) {
   const uint32_t n = (uint32_t)(a.q.slots() * a.Hv), grid = (n * (both ? 2 : 1) + 7) & ~7u;
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
+    constexpr int NS = kStateBlocks * DV / 128 > 0 ? kStateBlocks * DV / 128 : 1;
     if (dtype == 0)
-      hipLaunchKernelGGL((k_lin_state<DK, DV, float, 1>), dim3(grid), dim3(256), 0, st, a, n, both);
+      hipLaunchKernelGGL((k_lin_state<DK, DV, NS, float, 1>), dim3(grid), dim3(4 * DV / NS), 0, st, a,
+                         n, both);
     else
-      hipLaunchKernelGGL((k_lin_state<DK, DV, __bf16, 3>), dim3(grid), dim3(256), 0, st, a, n,
-                         both);
+      hipLaunchKernelGGL((k_lin_state<DK, DV, NS, __bf16, 3>), dim3(grid), dim3(4 * DV / NS), 0, st,
+                         a, n, both);
     if (hipError_t e = hipGetLastError()) return e;
     constexpr int parts = DK * DV / 1024;
     const int64_t heads = std::min<int64_t>((int64_t)a.q.nseq * a.Hv, 16384);
@@ -951,37 +1197,63 @@ hipError_t launch_linear_forward(const LinArgs& a, int dtype, hipStream_t st) {
   const uint32_t grid = ((n + 7) & ~7u) + (a.Sf && (a.q.cu || a.q.T == 0) ? a.q.nseq : 0);
   if (grid == 0) return hipSuccess;
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
+    constexpr int NS = kWalkBlocks * DV / 128 > 0 ? kWalkBlocks * DV / 128 : 1;
     if (dtype == 0)
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, float, 1, 1, 1>), dim3(grid), dim3(256), 0, st, a, n);
-    else
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, __bf16, 3, kOut, kOut>), dim3(grid), dim3(256), 0,
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, DV / 64, float, 1, 1, 1>), dim3(grid), dim3(256), 0,
                          st, a, n);
+    else
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, NS, __bf16, 3, kOut, kOut>), dim3(grid),
+                         dim3(4 * DV / NS), 0, st, a, n);
     return hipGetLastError();
   }))
   return hipErrorNotSupported;
+}
+
+// the gradients' launches
+template <int DK, int DV, bool DG>
+static hipError_t launch_passes(const LinArgs& a, uint32_t slots, int dtype, hipStream_t st) {
+  const uint32_t nk = slots * a.Hk, nv = slots * a.Hv;
+  const uint32_t copies = a.dS0 && (a.q.cu || a.q.T == 0) ? a.q.nseq : 0;
+  auto grid = [](uint32_t n, uint32_t more) { return dim3(((n + 7) & ~7u) + more); };
+  constexpr int TO = DG ? 3 : kOut;
+  if (slots == 0) {
+    if (!copies) return hipSuccess;
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDV, false>), grid(0, copies),
+                       dim3(256), 0, st, a, 0);
+  } else if (dtype == 0) {
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDQ, DG>), grid(nk, 0), dim3(256), 0,
+                       st, a, nk);
+    if (hipError_t e = hipGetLastError()) return e;
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDK, DG>), grid(nk, 0), dim3(256), 0,
+                       st, a, nk);
+    if (hipError_t e = hipGetLastError()) return e;
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDV, false>), grid(nv, copies),
+                       dim3(256), 0, st, a, nv);
+  } else if (a.Hv / a.Hk % 2 == 0) {
+    const uint32_t blocks = ((2 * nk + 7) & ~7u) + ((nv / 2 + 7) & ~7u);
+    hipLaunchKernelGGL((k_lin_backward_by_two<DK, DV, __bf16, 3, TO, kOut, DG>),
+                       dim3(blocks + copies), dim3(512), 0, st, a, slots);
+  } else {
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, TO, kOut, kDQ, DG>), grid(nk, 0),
+                       dim3(256), 0, st, a, nk);
+    if (hipError_t e = hipGetLastError()) return e;
+    hipLaunchKernelGGL((k_lin_backward_kv<DK, DV, __bf16, 3, TO, kOut, DG>), grid(nk, copies),
+                       dim3(512), 0, st, a, slots);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_linear_backward(const LinArgs& a, int dtype, hipStream_t st) {
   if (a.U)
     if (hipError_t e = launch_states(a, dtype, true, st)) return e;
   const uint32_t slots = a.q.T > 0 ? (uint32_t)a.q.slots() : 0;
-  const uint32_t grid = ((2 * slots * a.Hk + 7) & ~7u) + ((slots * a.Hv + 7) & ~7u) +
-                        (a.dS0 && (a.q.cu || a.q.T == 0) ? a.q.nseq : 0);
-  if (grid > 0) {
-    GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
-      if (dtype == 0)
-        hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1>), dim3(grid), dim3(256), 0, st,
-                           a, slots);
-      else if (a.want_dg)
-        hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, 3, kOut>), dim3(grid), dim3(256), 0,
-                           st, a, slots);
-      else
-        hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, kOut, kOut>), dim3(grid), dim3(256),
-                           0, st, a, slots);
-      break;
-    }) break;)
-    if (hipError_t e = hipGetLastError()) return e;
-  }
+  hipError_t e = hipErrorNotSupported;
+  GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
+    e = a.want_dg ? launch_passes<DK, DV, true>(a, slots, dtype, st)
+                  : launch_passes<DK, DV, false>(a, slots, dtype, st);
+    break;
+  }) break;)
+  if (e != hipSuccess) return e;
   if (!a.want_dg) return hipSuccess;
   if (slots > 0) {
     hipLaunchKernelGGL(k_lin_decay, dim3(slots * a.Hv), dim3(256), 0, st, a);

@@ -72,7 +72,7 @@ struct LinArgs {
   float *U, *R;           // [slots, Hv, dk, dv]: states entering, their gradients leaving
   float* dec;             // [slots, Hv]: decay over a segment
   float *rows_q, *rows_k;  // [Hv, tokens]: what dg takes of each token (linear.hip)
-  float *anchor, *part;   // [slots, Hv]: X of a segment's last chunk; sums of dg
+  float *anchor, *part;   // [slots, Hv]: X of a segment's first chunk; sums of dg
   float *acc_q, *acc_k;   // [tokens, Hk, dk]: sums of dQ, dK over a group's first heads
 };
 
