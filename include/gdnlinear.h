@@ -60,8 +60,8 @@ int gdn_linear_forward(const void* Q, const void* K, const void* V, const float*
 
 /* Workspace bytes for nseq sequences of T tokens (packed = 0), or of T tokens
  * in all (packed = 1). */
-int gdn_linear_forward_workspace(int nseq, int T, int Hv, int dk, int dv, int packed,
-                                 int64_t* bytes);
+int gdn_linear_forward_workspace(int nseq, int T, int Hk, int Hv, int dk, int dv, int packed,
+                                 int dtype, int64_t* bytes);
 
 /* Gradients of gdn_linear_forward: from dO and, where given, dS_final (the
  * gradient of the final states; NULL: zero) those of Q, K, V and, where asked
@@ -82,7 +82,7 @@ int gdn_linear_backward(const void* Q, const void* K, const void* V, const float
 
 /* Workspace bytes of gdn_linear_backward, wanting every gradient. */
 int gdn_linear_backward_workspace(int nseq, int T, int Hk, int Hv, int dk, int dv, int packed,
-                                  int64_t* bytes);
+                                  int dtype, int64_t* bytes);
 
 /* The same token by token, for decoding, all of it in fp32 (O rounds once).
  * S0 (nullable: zero states) and S_final (nullable: not written) hold n_states

@@ -17,10 +17,10 @@ _c_int, _c_i64, _c_f, _vp = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes
 _SIGS = {
     "gdn_linear_forward": [_vp] * 4 + [_c_int] + [_vp] * 4 + [_c_i64, _vp] + [_c_int] * 6 +
                           [_c_f, _c_int, _vp],
-    "gdn_linear_forward_workspace": [_c_int] * 6 + [ctypes.POINTER(_c_i64)],
+    "gdn_linear_forward_workspace": [_c_int] * 8 + [ctypes.POINTER(_c_i64)],
     "gdn_linear_backward": [_vp] * 4 + [_c_int] + [_vp] * 9 + [_c_i64, _vp] + [_c_int] * 6 +
                            [_c_f, _c_int, _vp],
-    "gdn_linear_backward_workspace": [_c_int] * 7 + [ctypes.POINTER(_c_i64)],
+    "gdn_linear_backward_workspace": [_c_int] * 8 + [ctypes.POINTER(_c_i64)],
     "gdn_linear_recurrent": [_vp] * 4 + [_c_int] + [_vp] * 4 + [_c_int, _vp] + [_c_int] * 6 +
                             [_c_f, _c_int, _vp],
     "gdn_group_norm_forward": [_vp] * 8 + [_c_i64, _c_i64] + [_c_int] * 3 + [_c_f] +
@@ -66,11 +66,13 @@ def _workspace(fn, args, device):
                                                       device=device)
 
 
-def gdn_linear_forward_workspace(nseq: int, T: int, Hv: int, dk: int, dv: int,
-                                 packed: bool = False) -> int:
+def gdn_linear_forward_workspace(nseq: int, T: int, Hk: int, Hv: int, dk: int, dv: int,
+                                 packed: bool = False,
+                                 dtype: torch.dtype = torch.bfloat16) -> int:
     """Bytes of workspace gdn_linear_forward needs for nseq sequences of T tokens, or with
     packed for nseq sequences of T tokens in all."""
-    return _workspace("gdn_linear_forward_workspace", (nseq, T, Hv, dk, dv, int(packed)), None)
+    return _workspace("gdn_linear_forward_workspace",
+                      (nseq, T, Hk, Hv, dk, dv, int(packed), _FDT[dtype]), None)
 
 
 def gdn_linear_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor,
@@ -94,7 +96,8 @@ def gdn_linear_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: tor
         S_final = torch.empty((nseq, Hv, dk, dv), dtype=_F32, device=K.device)
     if workspace is None:
         workspace = _workspace("gdn_linear_forward_workspace",
-                               (nseq, T, Hv, dk, dv, int(cu_seqlens is not None)), K.device)
+                               (nseq, T, Hk, Hv, dk, dv, int(cu_seqlens is not None), dt),
+                               K.device)
     states = nseq * Hv * dk * dv
     _check("gdn_linear_forward", lib.gdn_linear_forward(
         _dev(Q, "Q", K.dtype, tok * Hk * dk), _dev(K, "K"), _dev(V, "V", K.dtype, tok * Hv * dv),
@@ -107,10 +110,11 @@ def gdn_linear_forward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: tor
 
 
 def gdn_linear_backward_workspace(nseq: int, T: int, Hk: int, Hv: int, dk: int, dv: int,
-                                  packed: bool = False) -> int:
+                                  packed: bool = False,
+                                  dtype: torch.dtype = torch.bfloat16) -> int:
     """Bytes of workspace gdn_linear_backward needs, wanting every gradient."""
-    return _workspace("gdn_linear_backward_workspace", (nseq, T, Hk, Hv, dk, dv, int(packed)),
-                      None)
+    return _workspace("gdn_linear_backward_workspace",
+                      (nseq, T, Hk, Hv, dk, dv, int(packed), _FDT[dtype]), None)
 
 
 def gdn_linear_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor,
@@ -142,7 +146,8 @@ def gdn_linear_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: to
         dS0 = torch.empty((nseq, Hv, dk, dv), dtype=_F32, device=K.device)
     if workspace is None:
         workspace = _workspace("gdn_linear_backward_workspace",
-                               (nseq, T, Hk, Hv, dk, dv, int(cu_seqlens is not None)), K.device)
+                               (nseq, T, Hk, Hv, dk, dv, int(cu_seqlens is not None), dt),
+                               K.device)
     states, gates = nseq * Hv * dk * dv, tok * Hv if per_token else Hv
     _check("gdn_linear_backward", lib.gdn_linear_backward(
         _dev(Q, "Q", K.dtype, tok * Hk * dk), _dev(K, "K"), _dev(V, "V", K.dtype, tok * Hv * dv),

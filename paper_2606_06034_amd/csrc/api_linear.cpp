@@ -17,13 +17,14 @@ namespace {
 
 // the sizes of a call: its segments, and whether its launches and offsets fit
 int set_sizes(gdn::LinArgs& a, const int32_t* cu, bool packed, int nseq, int T, int Hk, int Hv,
-              int dk, int dv, bool backward) {
+              int dk, int dv, bool backward, int dtype) {
   if (nseq < 0 || T < 0 || !valid_heads(Hk, Hv) || !valid_d(dk) || !valid_d(dv))
     return GDN_ERR_SHAPE;
   static const int32_t some = 0;  // (sizes alone are asked for: any offsets)
   a.q.cu = packed ? (cu ? cu : &some) : nullptr;
   a.q.nseq = nseq, a.q.T = T;
-  a.q.seg = gdn::lin_segment(nseq, T, backward ? (2 * Hk + Hv + 1) / 2 : Hv, packed, backward);
+  if (!fdtype(dtype)) return GDN_ERR_DTYPE;
+  a.q.seg = gdn::lin_segment(nseq, T, Hk, Hv, dk, dv, packed, backward, dtype == GDN_F32);
   a.q.nseg = a.q.segments(T);
   a.Hk = Hk, a.Hv = Hv, a.dk = dk, a.dv = dv;
   const int64_t slots = a.q.slots();
@@ -74,11 +75,12 @@ int gdn_linear_recurrent(const void* Q, const void* K, const void* V, const floa
                                             dk, dv, scale, dtype, (hipStream_t)stream));
 }
 
-int gdn_linear_forward_workspace(int nseq, int T, int Hv, int dk, int dv, int packed,
-                                 int64_t* bytes) {
+int gdn_linear_forward_workspace(int nseq, int T, int Hk, int Hv, int dk, int dv, int packed,
+                                 int dtype, int64_t* bytes) {
   if (!bytes) return GDN_ERR_NULL;
   gdn::LinArgs a{};
-  if (int r = set_sizes(a, nullptr, packed != 0, nseq, T, Hv, Hv, dk, dv, false)) return r;
+  if (int r = set_sizes(a, nullptr, packed != 0, nseq, T, Hk, Hv, dk, dv, false, dtype))
+    return r;
   *bytes = 4 * gdn::lin_workspace(a, false, nullptr);
   return GDN_OK;
 }
@@ -88,9 +90,9 @@ int gdn_linear_forward(const void* Q, const void* K, const void* V, const float*
                        int64_t workspace_bytes, const int32_t* cu_seqlens, int nseq, int T, int Hk,
                        int Hv, int dk, int dv, float scale, int dtype, void* stream) {
   gdn::LinArgs a{};
-  if (int r = set_sizes(a, cu_seqlens, cu_seqlens != nullptr, nseq, T, Hk, Hv, dk, dv, false))
+  if (int r = set_sizes(a, cu_seqlens, cu_seqlens != nullptr, nseq, T, Hk, Hv, dk, dv, false,
+                        dtype))
     return r;
-  if (!fdtype(dtype)) return GDN_ERR_DTYPE;
   if (!rows_fit(T, Hk, Hv, dk, dv, dtype)) return GDN_ERR_SHAPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
   const int64_t tok = cu_seqlens ? (int64_t)T : (int64_t)nseq * T, es = esize(dtype);
@@ -118,10 +120,10 @@ int gdn_linear_forward(const void* Q, const void* K, const void* V, const float*
 }
 
 int gdn_linear_backward_workspace(int nseq, int T, int Hk, int Hv, int dk, int dv, int packed,
-                                  int64_t* bytes) {
+                                  int dtype, int64_t* bytes) {
   if (!bytes) return GDN_ERR_NULL;
   gdn::LinArgs a{};
-  if (int r = set_sizes(a, nullptr, packed != 0, nseq, T, Hk, Hv, dk, dv, true)) return r;
+  if (int r = set_sizes(a, nullptr, packed != 0, nseq, T, Hk, Hv, dk, dv, true, dtype)) return r;
   a.want_dg = true;
   *bytes = 4 * gdn::lin_workspace(a, true, nullptr);
   return GDN_OK;
@@ -133,9 +135,9 @@ int gdn_linear_backward(const void* Q, const void* K, const void* V, const float
                         int64_t workspace_bytes, const int32_t* cu_seqlens, int nseq, int T,
                         int Hk, int Hv, int dk, int dv, float scale, int dtype, void* stream) {
   gdn::LinArgs a{};
-  if (int r = set_sizes(a, cu_seqlens, cu_seqlens != nullptr, nseq, T, Hk, Hv, dk, dv, true))
+  if (int r = set_sizes(a, cu_seqlens, cu_seqlens != nullptr, nseq, T, Hk, Hv, dk, dv, true,
+                        dtype))
     return r;
-  if (!fdtype(dtype)) return GDN_ERR_DTYPE;
   if (!rows_fit(T, Hk, Hv, dk, dv, dtype)) return GDN_ERR_SHAPE;
   if (Hv == 0 || (nseq == 0 && (g_per_token || !dg))) return GDN_OK;
   const int64_t tok = cu_seqlens ? (int64_t)T : (int64_t)nseq * T, es = esize(dtype);

@@ -27,6 +27,7 @@
 // Precision.  bf16 inputs are exact operands of the matrix instructions; fp32 factors
 // (states, decayed values, P) enter as sums of bf16 terms (split.hpp).
 #include <algorithm>
+#include <cmath>
 
 #include "lanes.hpp"
 #include "launch.hpp"
@@ -1132,15 +1133,52 @@ __global__ __launch_bounds__(256) void k_lin_decay_sum(const LinArgs a, int64_t 
   if (threadIdx.x == 0) a.dg[h] = (float)s[0];
 }
 
-int lin_segment(int nseq, int T, int heads, bool packed, bool backward) {
-  const int64_t tokens = packed ? (int64_t)T : (int64_t)nseq * T;
-  const int whole = (int)((std::min<int64_t>(T, 0x7fffffff - LC) + LC - 1) / LC * LC);
-  // about 512 workgroups of work: two a CU
-  int64_t seg = tokens * heads / 512 / LC * LC;
-  if (seg < 256) seg = 256;
-  const int64_t most = backward ? LC * kMostChunks : 4096;
-  if (seg > most) seg = most;
-  return seg >= whole ? std::max(whole, LC) : (int)seg;
+// Tokens a segment.  Short ones fill the chip, long ones save launches and states (each is
+// written, carried over the segments and read: 4 times 64 KB, 9 in the backward pass): the one
+// of least time by what the launches took, in us, for heads of 128 by 128 in bf16.  A step
+// of a walk, of 64 tokens, takes 4.6 with one workgroup a CU and 3.6 each with two, forming
+// a segment's state 1.2 and 0.9; 12 to 13 a step of two teams, one workgroup a CU; with fp32
+// inputs 3.8 times as long.  (16 heads of 8192 tokens, forward: 103 us in segments of 128, 78
+// of 256 and 512, 94 of 768, 160 of 1536; 4 of 1000: 25 of 128, 36 of 256, 75 in one.)
+int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bool backward,
+                bool fp32) {
+  const double tokens = packed ? (double)T : (double)nseq * T, gr = Hk ? (double)Hv / Hk : 1;
+  const double size = (0.25 + 0.75 * dk * dv / 16384) * (fp32 ? 3.8 : 1);
+  const int most = backward ? LC * kMostChunks : 4096;
+  const int64_t whole = ((int64_t)T + LC - 1) / LC * LC;
+  int best = LC;
+  double least = 1e300;
+  for (int k = 1;; k += k < 8 ? 1 : k < 16 ? 2 : k < 32 ? 4 : 8) {
+    int64_t seg = std::min<int64_t>((int64_t)k * LC, most);
+    const bool one = seg >= whole;
+    if (one) seg = std::max<int64_t>(whole, LC);
+    const double steps = (double)seg / LC;
+    const double slots = packed ? tokens / seg + 0.5 * nseq : std::ceil((double)T / seg) * nseq;
+    // steps of `work` walkers on 256 CUs (equal ones in whole rounds; of unlike ones the
+    // last begins late)
+    auto time = [&](double work, double alone, double more, bool whole_rounds) {
+      double n = work / 256;
+      if (packed)
+        n *= (tokens / LC + 0.5 * nseq + 0.4 * slots) / (slots * steps);
+      else if (whole_rounds)
+        n = std::ceil(n);
+      const double t = steps * (fp32 ? alone * std::max(1., n) : std::max(alone, more * n));
+      return packed ? t + 0.5 * steps * alone : t;
+    };
+    const double states = slots * Hv;
+    double walk, add = time(backward ? 2 * states : states, 1.2, 0.9, true);
+    if (!backward)
+      walk = time(states, 4.6, 3.6, true);
+    else if (!fp32 && Hk && Hv / Hk % 2 == 0)
+      walk = time(1.5 * states, 12.9, 12.9, false);
+    else
+      walk = gr * (time(slots * Hk, 12, 12, false) + time(slots * Hk, 6, 4.5, true));
+    double cost = size * (walk + (one ? 0 : add)) + (one ? 4 : 12);
+    if (!one) cost += states * (backward ? 0.131 : 0.058) * dk * dv / 16384;
+    if (cost < least) least = cost, best = (int)seg;
+    if (one || k * LC >= most) break;
+  }
+  return best;
 }
 
 int64_t lin_workspace(LinArgs& a, bool backward, float* ws) {

@@ -77,7 +77,8 @@ struct LinArgs {
 };
 
 // Tokens a segment for these sizes.
-int lin_segment(int nseq, int T, int heads, bool packed, bool backward);
+int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bool backward,
+                bool fp32);
 // Floats of workspace; fills in the pointers where ws is given.
 int64_t lin_workspace(LinArgs& a, bool backward, float* ws);
 

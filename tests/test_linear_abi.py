@@ -90,23 +90,26 @@ def test_backward_refusals(change, code):
 
 
 def test_workspaces():
-    # short sequences are one segment: no workspace; the gradient of g takes some
-    assert G.gdn_linear_forward_workspace(300, 256, 4, 128, 128) == 0
-    assert G.gdn_linear_forward_workspace(1, 0, 4, 128, 128) == 0
+    # many short sequences are a segment each: no workspace; the gradient of g takes some
+    assert G.gdn_linear_forward_workspace(300, 256, 4, 4, 128, 128) == 0
+    assert G.gdn_linear_forward_workspace(1, 64, 4, 4, 128, 128) == 0
+    assert G.gdn_linear_forward_workspace(1, 0, 4, 4, 128, 128) == 0
     assert G.gdn_linear_backward_workspace(1, 0, 4, 4, 128, 128) >= 0
     assert 0 < G.gdn_linear_backward_workspace(300, 256, 4, 4, 64, 64) < 300 * 256 * 4 * 16
     n = 8192 * 16 * 128  # a long sequence: fewer states than tokens' values
-    assert 0 < G.gdn_linear_forward_workspace(1, 8192, 16, 128, 128) < 4 * n
-    assert L.gdn_linear_forward_workspace(1, 8192, 16, 128, 128, 0, None) == NULL
-    assert L.gdn_linear_backward_workspace(1, 8192, 16, 16, 128, 128, 0, None) == NULL
+    assert 0 < G.gdn_linear_forward_workspace(1, 8192, 16, 16, 128, 128) < 4 * n
+    assert G.gdn_linear_forward_workspace(1, 8192, 16, 16, 128, 128, dtype=torch.float32) > 0
+    assert L.gdn_linear_forward_workspace(1, 8192, 16, 16, 128, 128, 0, 1, None) == NULL
+    assert L.gdn_linear_backward_workspace(1, 8192, 16, 16, 128, 128, 0, 1, None) == NULL
     n = ctypes.c_int64()
     # lengths near 2^31 are cut into segments in 64 bits
-    for packed in (0, 1):
-        assert L.gdn_linear_forward_workspace(1, 2 ** 31 - 1, 1, 64, 64, packed,
-                                              ctypes.byref(n)) == OK
-        assert n.value > 0
-    assert L.gdn_linear_forward_workspace(2 ** 31 - 1, 2 ** 31 - 1, 1, 64, 64, 0,
-                                          ctypes.byref(n)) == SHAPE
+    for f in (L.gdn_linear_forward_workspace, L.gdn_linear_backward_workspace):
+        for packed in (0, 1):
+            assert f(1, 2 ** 31 - 1, 1, 1, 64, 64, packed, 1, ctypes.byref(n)) == OK
+            assert n.value > 0
+        assert f(2 ** 31 - 1, 2 ** 31 - 1, 1, 1, 64, 64, 0, 1, ctypes.byref(n)) == SHAPE
+        assert f(1, 100, 1, 1, 64, 64, 0, 2, ctypes.byref(n)) == DTYPE
+        assert f(1, 100, 3, 4, 64, 64, 0, 1, ctypes.byref(n)) == SHAPE
     with pytest.raises(G.GdnError):
         G.gdn_linear_backward_workspace(2, 100, 3, 3, 96, 128)
 
