@@ -18,6 +18,7 @@
 #include "lanes.hpp"
 #include "launch.hpp"
 #include "norm.hpp"
+#include "tile16.hpp"
 
 namespace gdn {
 
@@ -49,14 +50,28 @@ __device__ __forceinline__ void put(T* __restrict__ p, const float (&x)[V]) {
     *(typename Vals<T, V>::type*)p = v;
   }
 }
-// a weight or bias in either dtype; `none` where there is none.  (Its rows need no more than
-// an element's alignment.)
+// V values as they lie in memory, and as floats
+template <typename T, int V> struct Raw {
+  typename Vals<T, V>::type v;
+  __device__ __forceinline__ void load(const T* __restrict__ p) {
+    v = *(const typename Vals<T, V>::type*)p;
+  }
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (V == 1) return (float)v; else return (float)v[i];
+  }
+};
+// a weight or bias in either dtype; `none` where there is none
 template <int V>
 __device__ __forceinline__ void get_param(float (&x)[V], const void* p, bool bf, float none,
                                           int at) {
+  if (!p) {
 #pragma unroll
-  for (int i = 0; i < V; ++i)
-    x[i] = !p ? none : bf ? (float)((const __bf16*)p)[at + i] : ((const float*)p)[at + i];
+    for (int i = 0; i < V; ++i) x[i] = none;
+  } else if (bf) {
+    get<__bf16, V>(x, (const __bf16*)p + at);
+  } else {
+    get<float, V>(x, (const float*)p + at);
+  }
 }
 
 __device__ __forceinline__ float silu_grad(float t) {
@@ -64,23 +79,27 @@ __device__ __forceinline__ float silu_grad(float t) {
   return s * __builtin_fmaf(t, 1.f - s, 1.f);
 }
 
+// what follows n: bit 0 SiLU, bit 1 a gate
+constexpr int kAct = 1, kGate = 2;
+
 // the results of one value
-__device__ __forceinline__ float result(const GroupArgs& a, float h, float w, float b, float z) {
+template <int OPS>
+__device__ __forceinline__ float result(float h, float w, float b, float z) {
   float n = __builtin_fmaf(h, w, b);
-  if (a.act) n *= sigmoid(n);
-  if (a.z) n *= z * sigmoid(z);
+  if (OPS & kAct) n *= sigmoid(n);
+  if (OPS & kGate) n *= z * sigmoid(z);
   return n;
 }
 // dn (and dz) of one value
-__device__ __forceinline__ float grad(const GroupArgs& a, float h, float w, float b, float z,
-                                      float dy, float& dz) {
+template <int OPS>
+__device__ __forceinline__ float grad(float h, float w, float b, float z, float dy, float& dz) {
   const float n = __builtin_fmaf(h, w, b);
-  if (a.z) {
+  if (OPS & kGate) {
     const float s = sigmoid(z);
-    dz = dy * (a.act ? n * sigmoid(n) : n) * (s * __builtin_fmaf(z, 1.f - s, 1.f));
+    dz = dy * (OPS & kAct ? n * sigmoid(n) : n) * (s * __builtin_fmaf(z, 1.f - s, 1.f));
     dy *= z * s;
   }
-  return a.act ? dy * silu_grad(n) : dy;
+  return OPS & kAct ? dy * silu_grad(n) : dy;
 }
 
 // sums over the `tpi` neighbouring threads (a power of two) of a group; past a wave they
@@ -88,6 +107,22 @@ __device__ __forceinline__ float grad(const GroupArgs& a, float h, float w, floa
 struct Sums {
   float* red;
   int buf, tpi;
+  __device__ __forceinline__ void operator()(float& a) {
+    if (tpi >= 2) a += lane_moved<0xB1>(a);
+    if (tpi >= 4) a += lane_moved<0x4E>(a);
+    if (tpi >= 8) a += lane_moved<0x141>(a);
+    if (tpi >= 16) a += lane_moved<0x140>(a);
+    if (tpi >= 32) a = sum_apart16(a);
+    if (tpi >= 64) a = sum_apart32(a);
+    if (tpi > 64) {
+      float* r = red + buf * 32;
+      buf ^= 1;
+      if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = a;
+      __syncthreads();
+      a = 0.f;
+      for (int i = 0; i < tpi >> 6; ++i) a += r[i];
+    }
+  }
   __device__ __forceinline__ void operator()(float& a, float& b) {
     if (tpi >= 2) a += lane_moved<0xB1>(a), b += lane_moved<0xB1>(b);
     if (tpi >= 4) a += lane_moved<0x4E>(a), b += lane_moved<0x4E>(b);
@@ -110,9 +145,10 @@ struct Sums {
 }  // namespace
 
 // Groups in registers.  A workgroup has gw groups of nw n's at a time, tpi threads each, and
-// walks the n's; piece k of thread t of a group is its (t + k tpi)-th piece of V values.
-template <typename T, int V, int NV, int B>
-__global__ __launch_bounds__(B) void k_gn_rows(const GroupArgs a) {
+// walks the n's, the next ones asked for ahead; piece k of thread t of a group is its
+// (t + k tpi)-th piece of V values.
+template <typename T, int V, int NV, int OPS>
+__global__ __launch_bounds__(256) void k_gn_rows(const GroupArgs a) {
   __shared__ float red[64];
   Sums sums{red, 0, a.tpi};
   const int slot = (int)threadIdx.x / a.tpi, t = (int)threadIdx.x - slot * a.tpi;
@@ -120,77 +156,72 @@ __global__ __launch_bounds__(B) void k_gn_rows(const GroupArgs a) {
   const int ni = slot / a.gw, g = gb * a.gw + slot - ni * a.gw;
   const bool mine = ni < a.nw;
   const int pr = a.Cg / V, pieces = a.S * pr;
-  constexpr bool HOLD = NV <= 2;  // (weights and gates past that are read where they are used)
-  constexpr int H = HOLD ? NV : 1;
-  float w[H][V], b[H][V];
-  int at[NV], ch[NV];
+  float w[NV][V], b[NV][V];
+  int at[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int p = t + k * a.tpi, s = p / pr;
-    ch[k] = g * a.Cg + (p - s * pr) * V;
-    at[k] = mine && p < pieces ? s * a.C + ch[k] : -1;
-    if constexpr (HOLD) {
-      get_param<V>(w[k], at[k] < 0 ? nullptr : a.w, a.wbf, 1.f, ch[k]);
-      get_param<V>(b[k], at[k] < 0 ? nullptr : a.b, a.wbf, 0.f, ch[k]);
-    }
+    const int p = t + k * a.tpi, s = p / pr, ch = g * a.Cg + (p - s * pr) * V;
+    at[k] = mine && p < pieces ? s * a.C + ch : -1;
+    get_param<V>(w[k], at[k] < 0 ? nullptr : a.w, a.wbf, 1.f, ch);
+    get_param<V>(b[k], at[k] < 0 ? nullptr : a.b, a.wbf, 0.f, ch);
   }
   const float inv = 1.f / (float)(a.S * a.Cg);
-  const int parts = (int)(gridDim.x / blocks);
-  for (int64_t n0 = (int64_t)nb * a.nw; n0 < a.N; n0 += (int64_t)parts * a.nw) {
-    const int64_t n = n0 + ni, base = n * a.S * a.C;
-    const bool live = mine && n < a.N;
-    float x[NV][V], z[H][V], mean = 0.f, var = 0.f, none = 0.f;
+  const int64_t step = (int64_t)(gridDim.x / blocks) * a.nw, size = (int64_t)a.S * a.C;
+  Raw<T, V> x[NV], z[NV];
+  auto fetch = [&](int64_t n) __attribute__((always_inline)) {
+    n = n < a.N ? n : a.N - 1;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[k][i] = 0.f;
-      if (live && at[k] >= 0) {
-        get<T, V>(x[k], (const T*)a.x + base + at[k]);
-        if constexpr (HOLD)
-          if (a.z) get<T, V>(z[k], (const T*)a.z + base + at[k]);
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) mean += x[k][i];
+      const int64_t p = n * size + max(at[k], 0);
+      x[k].load((const T*)a.x + p);
+      if (OPS & kGate) z[k].load((const T*)a.z + p);
     }
-    sums(mean, none);
+  };
+  int64_t n0 = (int64_t)nb * a.nw;
+  fetch(n0 + ni);
+  for (; n0 < a.N; n0 += step) {
+    const int64_t n = n0 + ni;
+    const bool live = mine && n < a.N;
+    float h[NV][V], f[NV][V], mean = 0.f, var = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        h[k][i] = x[k][i];
+        f[k][i] = OPS & kGate ? z[k][i] : 0.f;
+        mean += at[k] >= 0 ? h[k][i] : 0.f;
+      }
+    fetch(n + step);
+    sums(mean);
     mean *= inv;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        x[k][i] = at[k] >= 0 ? x[k][i] - mean : 0.f;
-        var = __builtin_fmaf(x[k][i], x[k][i], var);
+        h[k][i] = at[k] >= 0 ? h[k][i] - mean : 0.f;
+        var = __builtin_fmaf(h[k][i], h[k][i], var);
       }
-    sums(var, none);
+    sums(var);
     const float rstd = 1.f / sqrtf(var * inv + a.eps);
     if (!live) continue;
     if (t == 0) {
       if (a.mean) a.mean[n * a.G + g] = mean;
       if (a.rstd) a.rstd[n * a.G + g] = rstd;
     }
-    const void *wp = a.w, *bp = a.b;
-    if constexpr (!HOLD) asm volatile("" : "+s"(wp), "+s"(bp));  // (not read ahead of the loop)
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (at[k] >= 0) {
-        constexpr int O = HOLD ? 1 : 0;
         float y[V];
-        if constexpr (!HOLD) {
-          get_param<V>(w[0], wp, a.wbf, 1.f, ch[k]);
-          get_param<V>(b[0], bp, a.wbf, 0.f, ch[k]);
-          if (a.z) get<T, V>(z[0], (const T*)a.z + base + at[k]);
-        }
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          y[i] = result(a, x[k][i] * rstd, w[O * k][i], b[O * k][i], a.z ? z[O * k][i] : 0.f);
-        put<T, V>((T*)a.out + base + at[k], y);
+        for (int i = 0; i < V; ++i) y[i] = result<OPS>(h[k][i] * rstd, w[k][i], b[k][i], f[k][i]);
+        put<T, V>((T*)a.out + n * size + at[k], y);
       }
   }
 }
 
 // The gradients where S = 1.  The n's that run side by side add up their dw and db in LDS, the
 // workgroups' sums go to row nb of the workspace: [parts][C], then the same for db.
-template <typename T, int V, int NV, int B>
+template <typename T, int V, int NV, int B, int OPS>
 __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts) {
   extern __shared__ float lds[];  // 64 values of the sums, then [2][gw Cg]
   Sums sums{lds, 0, a.tpi};
@@ -211,47 +242,66 @@ __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts
     for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = 0.f;
   }
   const float inv = 1.f / (float)a.Cg;
-  for (int64_t n0 = (int64_t)nb * a.nw; n0 < a.N; n0 += (int64_t)parts * a.nw) {
-    const int64_t n = n0 + ni, base = n * a.C;
+  const int64_t step = (int64_t)parts * a.nw;
+  struct Row {
+    Raw<T, V> x[NV], dy[NV], z[NV];
+    float mean, rstd;
+  };
+  auto fetch = [&](Row& r, int64_t n) __attribute__((always_inline)) {
+    n = n < a.N ? n : a.N - 1;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int64_t p = n * a.C + max(at[k], 0);
+      r.x[k].load((const T*)a.x + p);
+      r.dy[k].load((const T*)a.dy + p);
+      if (OPS & kGate) r.z[k].load((const T*)a.z + p);
+    }
+    r.mean = a.mean_in[n * a.G + (mine ? g : 0)];
+    r.rstd = a.rstd_in[n * a.G + (mine ? g : 0)];
+  };
+  auto row = [&](const Row& r, int64_t n) __attribute__((always_inline)) {
     const bool live = mine && n < a.N;
-    const float mean = live ? a.mean_in[n * a.G + g] : 0.f;
-    const float rstd = live ? a.rstd_in[n * a.G + g] : 0.f;
     float h[NV][V], dn[NV][V], s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
+      float dz[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[k][i] = dn[k][i] = 0.f;
-      if (live && at[k] >= 0) {
-        float z[V], dz[V];
-        get<T, V>(h[k], (const T*)a.x + base + at[k]);
-        get<T, V>(dn[k], (const T*)a.dy + base + at[k]);
-        if (a.z) get<T, V>(z, (const T*)a.z + base + at[k]);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          h[k][i] = (h[k][i] - mean) * rstd;
-          dn[k][i] = grad(a, h[k][i], w[k][i], b[k][i], a.z ? z[i] : 0.f, dn[k][i], dz[i]);
-          const float dh = dn[k][i] * w[k][i];
-          s1 += dh;
-          s2 = __builtin_fmaf(dh, h[k][i], s2);
-        }
-        if (a.z) put<T, V>((T*)a.dz + base + at[k], dz);
+      for (int i = 0; i < V; ++i) {
+        h[k][i] = ((float)r.x[k][i] - r.mean) * r.rstd;
+        dn[k][i] = grad<OPS>(h[k][i], w[k][i], b[k][i], OPS & kGate ? r.z[k][i] : 0.f, r.dy[k][i], dz[i]);
+        const float dh = at[k] >= 0 ? dn[k][i] * w[k][i] : 0.f;
+        s1 += dh;
+        s2 += at[k] >= 0 ? dh * h[k][i] : 0.f;
       }
+      if ((OPS & kGate) && live && at[k] >= 0) put<T, V>((T*)a.dz + n * a.C + at[k], dz);
     }
     sums(s1, s2);
     s1 *= inv, s2 *= inv;
-    if (!live) continue;
+    if (!live) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (at[k] >= 0) {
         float dx[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          dx[i] = rstd * (dn[k][i] * w[k][i] - s1 - h[k][i] * s2);
+          dx[i] = r.rstd * (dn[k][i] * w[k][i] - s1 - h[k][i] * s2);
           dw[k][i] = __builtin_fmaf(dn[k][i], h[k][i], dw[k][i]);
           db[k][i] += dn[k][i];
         }
-        put<T, V>((T*)a.out + base + at[k], dx);
+        put<T, V>((T*)a.out + n * a.C + at[k], dx);
       }
+  };
+  // two sets in turn, each asked for again when it has been used
+  Row r0, r1;
+  int64_t n0 = (int64_t)nb * a.nw;
+  fetch(r0, n0 + ni);
+  fetch(r1, n0 + step + ni);
+  for (; n0 < a.N; n0 += 2 * step) {
+    row(r0, n0 + ni);
+    fetch(r0, n0 + 2 * step + ni);
+    if (n0 + step >= a.N) break;
+    row(r1, n0 + step + ni);
+    fetch(r1, n0 + 3 * step + ni);
   }
   if (!a.dw && !a.db) return;
   float* sum = lds + 64;
@@ -292,13 +342,14 @@ __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts
 // one.  Thread t has piece t % cols, and every (256 / cols)-th position.
 struct Tile {
   int64_t n, row0;  // row0: n S
-  int part, s0, s1, cols, c0, col, row, step, g0, ng;
+  int part, s0, s1, cols, c0, col, row, step, g0, ng, per, piece;
   bool mine;
-  template <int V> static __device__ __forceinline__ Tile of(const GroupArgs& a) {
+  template <int V>
+  static __device__ __forceinline__ Tile of(const GroupArgs& a, uint32_t block = blockIdx.x) {
     Tile t;
     const uint32_t pn = (uint32_t)a.sparts * (uint32_t)a.cblocks;
-    t.n = blockIdx.x / pn;
-    const int at = (int)(blockIdx.x - (uint32_t)t.n * pn);
+    t.n = block / pn;
+    const int at = (int)(block - (uint32_t)t.n * pn);
     t.part = at / a.cblocks;
     const int cb = at - t.part * a.cblocks, pr = a.Cg / V;
     t.s0 = (int)((int64_t)a.S * t.part / a.sparts);
@@ -309,11 +360,13 @@ struct Tile {
       t.ng = min(most, a.G - t.g0);
       t.cols = t.ng * pr;
       t.c0 = t.g0 * a.Cg;
+      t.per = 1, t.piece = 0;
     } else {
-      const int per = (pr + 255) / 256;  // blocks a group
-      t.g0 = cb / per;
+      t.per = (pr + 255) / 256;  // blocks a group
+      t.g0 = cb / t.per;
       t.ng = 1;
-      const int p0 = (cb - t.g0 * per) * 256;
+      t.piece = cb - t.g0 * t.per;
+      const int p0 = t.piece * 256;
       t.cols = min(256, pr - p0);
       t.c0 = t.g0 * a.Cg + p0 * V;
     }
@@ -324,6 +377,13 @@ struct Tile {
     t.row0 = t.n * a.S;
     return t;
   }
+  // a power of two within a wave, all groups at once where they are few enough
+  __device__ __forceinline__ int threads_a_group() const {
+    return ng <= 4 ? 64 : ng <= 8 ? 32 : ng <= 16 ? 16 : ng <= 32 ? 8 : 4;
+  }
+  // parts of a group, and which one this is (of one in many column blocks too)
+  __device__ __forceinline__ int parts(const GroupArgs& a) const { return a.sparts * per; }
+  __device__ __forceinline__ int at(const GroupArgs& a) const { return part * per + piece; }
   __device__ __forceinline__ int64_t base(const GroupArgs& a, int s) const {
     return (row0 + s) * a.C + col;
   }
@@ -385,43 +445,49 @@ __global__ __launch_bounds__(256) void k_gn_stats(const GroupArgs a) {
   sum_groups(t, [&](int i) { return sc[i]; }, [&](int g, float x) { gn[g] = x; });
   sum_groups(t, [&](int i) { return sc[i] * sm[i]; }, [&](int g, float x) { gm[g] = x; });
   __syncthreads();
-  const int per = t.cols / t.ng, cb = a.Cg / V > 256 ? (t.c0 - t.g0 * a.Cg) / (256 * V) : 0;
-  const int cparts = a.Cg / V > 256 ? (a.Cg / V + 255) / 256 : 1, parts = a.sparts * cparts;
+  const int per = t.cols / t.ng, parts = t.parts(a);
   sum_groups(
       t,
       [&](int i) {
         const int g = i % t.cols / per;
-        const float d = gn[g] > 0.f ? sm[i] - gm[g] / gn[g] : 0.f;
+        const float d = sm[i] - gm[g] / gn[g];
         return sq[i] + sc[i] * d * d;
       },
       [&](int g, float x) {
-        float* to = a.ws + ((t.n * a.G + t.g0 + g) * parts + t.part * cparts + cb) * 4;
-        to[0] = gn[g], to[1] = gn[g] > 0.f ? gm[g] / gn[g] : 0.f, to[2] = x;
+        *(f32x4*)(a.ws + ((t.n * a.G + t.g0 + g) * parts + t.at(a)) * 4) =
+            f32x4{gn[g], gm[g] / gn[g], x, 0.f};
       });
 }
 
-template <typename T, int V>
+template <typename T, int V, int OPS>
 __global__ __launch_bounds__(256) void k_gn_apply(const GroupArgs a) {
   __shared__ float sm[256], sr[256];
   const Tile t = Tile::of<V>(a);
-  const int parts = a.sparts * (a.Cg / V > 256 ? (a.Cg / V + 255) / 256 : 1);
-  for (int g0 = 0; g0 < t.ng; g0 += 16) {  // 16 threads a group join its parts
-    const int g = g0 + (int)(threadIdx.x >> 4), lane = threadIdx.x & 15;
-    const float* p = a.ws + (t.n * a.G + t.g0 + min(g, t.ng - 1)) * parts * 4;
+  const int parts = t.parts(a);
+  const int each = t.threads_a_group(), lane = (int)threadIdx.x % each;
+  for (int g0 = 0; g0 < t.ng; g0 += 256 / each) {  // join the parts: pairwise, then over threads
+    const int g = g0 + (int)threadIdx.x / each;
+    const f32x4* p = (const f32x4*)a.ws + (t.n * a.G + t.g0 + min(g, t.ng - 1)) * parts;
     float c = 0.f, m = 0.f, q = 0.f;
-    for (int i = lane; i < parts; i += 16) c += p[4 * i], m += p[4 * i] * p[4 * i + 1];
-    c = sum_lanes<16>(c);
-    m = sum_lanes<16>(m) / c;
-    for (int i = lane; i < parts; i += 16) {
-      const float d = p[4 * i + 1] - m;
-      q += p[4 * i + 2] + p[4 * i] * d * d;
+#pragma unroll 4
+    for (int i = lane; i < parts; i += each) {
+      const f32x4 v = p[i];
+      const float n = c + v[0], d = v[1] - m;
+      m += d * (v[0] / n);
+      q += v[2] + d * d * (c * v[0] / n);
+      c = n;
     }
-    q = sum_lanes<16>(q) / c;
+    Sums sums{nullptr, 0, each};
+    float n = c, mean = c * m;
+    sums(n, mean);
+    mean /= n;
+    q += c * (m - mean) * (m - mean);
+    sums(q);
     if (lane == 0 && g < t.ng) {
-      sm[g] = m;
-      sr[g] = 1.f / sqrtf(q + a.eps);
-      if (t.part == 0 && t.c0 == t.g0 * a.Cg) {
-        if (a.mean) a.mean[t.n * a.G + t.g0 + g] = m;
+      sm[g] = mean;
+      sr[g] = 1.f / sqrtf(q / n + a.eps);
+      if (t.at(a) == 0) {
+        if (a.mean) a.mean[t.n * a.G + t.g0 + g] = mean;
         if (a.rstd) a.rstd[t.n * a.G + t.g0 + g] = sr[g];
       }
     }
@@ -438,16 +504,17 @@ __global__ __launch_bounds__(256) void k_gn_apply(const GroupArgs a) {
     const int64_t at = t.base(a, s);
     float x[V], z[V], y[V];
     get<T, V>(x, (const T*)a.x + at);
-    if (a.z) get<T, V>(z, (const T*)a.z + at);
+    if (OPS & kGate) get<T, V>(z, (const T*)a.z + at);
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      y[i] = result(a, (x[i] - mean) * rstd, w[i], b[i], a.z ? z[i] : 0.f);
+      y[i] = result<OPS>((x[i] - mean) * rstd, w[i], b[i], OPS & kGate ? z[i] : 0.f);
     put<T, V>((T*)a.out + at, y);
   }
 }
 
-// the sums of dn h and dn of a part of the positions: [N sparts][C], then the same for dn
-template <typename T, int V>
+// The sums of dn h and dn of a part of the positions: [N sparts][C], then the same for dn;
+// behind them what the groups' means need of it, the sums of dh h and dh: [N][G][parts][2].
+template <typename T, int V, int OPS>
 __global__ __launch_bounds__(256) void k_gn_sums(const GroupArgs a) {
   __shared__ float s1[256 * V], s2[256 * V];
   const Tile t = Tile::of<V>(a);
@@ -465,12 +532,12 @@ __global__ __launch_bounds__(256) void k_gn_sums(const GroupArgs a) {
       float x[V], dy[V], z[V];
       get<T, V>(x, (const T*)a.x + at);
       get<T, V>(dy, (const T*)a.dy + at);
-      if (a.z) get<T, V>(z, (const T*)a.z + at);
+      if (OPS & kGate) get<T, V>(z, (const T*)a.z + at);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float dz;
         const float h = (x[i] - mean) * rstd;
-        const float dn = grad(a, h, w[i], b[i], a.z ? z[i] : 0.f, dy[i], dz);
+        const float dn = grad<OPS>(h, w[i], b[i], OPS & kGate ? z[i] : 0.f, dy[i], dz);
         dw[i] = __builtin_fmaf(dn, h, dw[i]);
         db[i] += dn;
       }
@@ -482,46 +549,76 @@ __global__ __launch_bounds__(256) void k_gn_sums(const GroupArgs a) {
   float* to = a.ws + (t.n * a.sparts + t.part) * a.C + t.c0;
   const int64_t half = a.N * a.sparts * a.C;
   for (int c = threadIdx.x; c < t.cols * V; c += 256) {
-    float x = 0.f, y = 0.f;
+    float x = 0.f, y = 0.f, f[1];
     for (int r = 0; r < t.step; ++r) x += s1[r * t.cols * V + c], y += s2[r * t.cols * V + c];
     to[c] = x;
     to[half + c] = y;
+    get_param<1>(f, a.w, a.wbf, 1.f, t.c0 + c);
+    s1[c] = f[0] * x, s2[c] = f[0] * y;  // (read by this thread alone until here)
+  }
+  __syncthreads();
+  const int per = t.cols * V / t.ng, lane = threadIdx.x & 15, parts = t.parts(a);
+  for (int g0 = 0; g0 < t.ng; g0 += 16) {
+    const int g = g0 + (int)(threadIdx.x >> 4);
+    float x = 0.f, y = 0.f;
+    if (g < t.ng)
+      for (int i = lane; i < per; i += 16) x += s1[g * per + i], y += s2[g * per + i];
+    x = sum_lanes<16>(x), y = sum_lanes<16>(y);
+    if (lane == 0 && g < t.ng) {
+      float* m = a.ws + 2 * half + ((t.n * a.G + t.g0 + g) * parts + t.at(a)) * 2;
+      m[0] = x, m[1] = y;
+    }
   }
 }
 
-// what the groups' means need of them: mean(dh h) and mean(dh) of each (n, group), behind the
-// sums in the workspace
-__global__ __launch_bounds__(256) void k_gn_means(const GroupArgs a) {
-  __shared__ float red[64];
-  Sums sums{red, 0, 256};
-  const int64_t n = blockIdx.x / (uint32_t)a.G, half = a.N * a.sparts * a.C;
-  const int g = (int)(blockIdx.x - (uint32_t)n * (uint32_t)a.G);
-  const float* from = a.ws + n * a.sparts * a.C + g * a.Cg;
-  float x = 0.f, y = 0.f;
-  for (int i = threadIdx.x; i < a.Cg * a.sparts; i += 256) {
-    const int p = i / a.Cg, c = i - p * a.Cg;
-    float w[1];
-    get_param<1>(w, a.w, a.wbf, 1.f, g * a.Cg + c);
-    x += w[0] * from[(int64_t)p * a.C + c];
-    y += w[0] * from[half + (int64_t)p * a.C + c];
-  }
-  sums(x, y);
-  if (threadIdx.x == 0) {
-    const float inv = 1.f / ((float)a.S * (float)a.Cg);
-    a.ws[2 * half + 2 * blockIdx.x] = x * inv;
-    a.ws[2 * half + 2 * blockIdx.x + 1] = y * inv;
+// dw[c] (dn h) and db[c]: sums over the parts, 16 threads a column and 16 columns a workgroup
+__device__ __forceinline__ void sum_parts(const GroupArgs& a, int64_t parts, int block) {
+  __shared__ float s[16][17];
+  const int blocks = (a.C + 15) / 16, second = block >= blocks;
+  const float* from = a.ws + (second ? parts * a.C : 0);
+  float* to = second ? a.db : a.dw;
+  if (!to) return;
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, d = (block - second * blocks) * 16 + c;
+  float x = 0.f;
+  if (d < a.C)
+#pragma unroll 8
+    for (int64_t p = r; p < parts; p += 16) x += from[p * a.C + d];
+  s[r][c] = x;
+  __syncthreads();
+  if (r == 0 && d < a.C) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) x += s[i][c];
+    to[d] = x;
   }
 }
+__global__ __launch_bounds__(256) void k_gn_parts(const GroupArgs a, int64_t parts) {
+  sum_parts(a, parts, (int)blockIdx.x);
+}
 
-template <typename T, int V>
-__global__ __launch_bounds__(256) void k_gn_dx(const GroupArgs a) {
-  const Tile t = Tile::of<V>(a);
+// (the first blocks add up dw and db)
+template <typename T, int V, int OPS>
+__global__ __launch_bounds__(256) void k_gn_dx(const GroupArgs a, int adding) {
+  if ((int)blockIdx.x < adding) return sum_parts(a, a.N * a.sparts, (int)blockIdx.x);
+  __shared__ float m1[256], m2[256];
+  const Tile t = Tile::of<V>(a, blockIdx.x - adding);
+  const float* sums = a.ws + 2 * (a.N * a.sparts * a.C);
+  const int parts = t.parts(a);
+  const float inv = 1.f / ((float)a.S * (float)a.Cg);
+  const int each = t.threads_a_group(), lane = (int)threadIdx.x % each;
+  for (int g0 = 0; g0 < t.ng; g0 += 256 / each) {
+    const int g = g0 + (int)threadIdx.x / each;
+    const float* p = sums + (t.n * a.G + t.g0 + min(g, t.ng - 1)) * parts * 2;
+    float x = 0.f, y = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < parts; i += each) x += p[2 * i], y += p[2 * i + 1];
+    Sums{nullptr, 0, each}(x, y);
+    if (lane == 0 && g < t.ng) m2[g] = x * inv, m1[g] = y * inv;
+  }
+  __syncthreads();
   if (!t.mine) return;
   const int g = t.col / a.Cg;
   const int64_t ng = t.n * a.G + g;
-  const float mean = a.mean_in[ng], rstd = a.rstd_in[ng];
-  const float* m = a.ws + 2 * (a.N * a.sparts * a.C) + 2 * ng;
-  const float s2 = m[0], s1 = m[1];
+  const float mean = a.mean_in[ng], rstd = a.rstd_in[ng], s1 = m1[g - t.g0], s2 = m2[g - t.g0];
   float w[V], b[V];
   get_param<V>(w, a.w, a.wbf, 1.f, t.col);
   get_param<V>(b, a.b, a.wbf, 0.f, t.col);
@@ -531,36 +628,15 @@ __global__ __launch_bounds__(256) void k_gn_dx(const GroupArgs a) {
     float x[V], dy[V], z[V], dz[V];
     get<T, V>(x, (const T*)a.x + at);
     get<T, V>(dy, (const T*)a.dy + at);
-    if (a.z) get<T, V>(z, (const T*)a.z + at);
+    if (OPS & kGate) get<T, V>(z, (const T*)a.z + at);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float h = (x[i] - mean) * rstd;
-      const float dn = grad(a, h, w[i], b[i], a.z ? z[i] : 0.f, dy[i], dz[i]);
+      const float dn = grad<OPS>(h, w[i], b[i], OPS & kGate ? z[i] : 0.f, dy[i], dz[i]);
       x[i] = rstd * (dn * w[i] - s1 - h * s2);
     }
     put<T, V>((T*)a.out + at, x);
-    if (a.z) put<T, V>((T*)a.dz + at, dz);
-  }
-}
-
-// dw[c] (dn h) and db[c]: sums over the parts, 16 threads a column and 16 columns a workgroup
-__global__ __launch_bounds__(256) void k_gn_parts(const float* __restrict__ ws, float* dw,
-                                                  float* db, int64_t parts, int C) {
-  __shared__ float s[16][17];
-  const float* from = ws + (blockIdx.y ? parts * C : 0);
-  float* to = blockIdx.y ? db : dw;
-  if (!to) return;
-  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
-  float x = 0.f;
-  if (d < C)
-#pragma unroll 8
-    for (int64_t p = r; p < parts; p += 16) x += from[p * C + d];
-  s[r][c] = x;
-  __syncthreads();
-  if (r == 0 && d < C) {
-#pragma unroll
-    for (int i = 1; i < 16; ++i) x += s[i][c];
-    to[d] = x;
+    if (OPS & kGate) put<T, V>((T*)a.dz + at, dz);
   }
 }
 
@@ -586,15 +662,16 @@ int vec_of(int Cg, int dtype) {
   return Cg % 8 == 0 ? 8 : Cg % 2 == 0 ? 2 : 1;
 }
 
-// pieces a thread holds, threads of a workgroup and of a group; 0 where a group is too long
+// pieces a thread holds, threads of a workgroup and of a group; 0 where a group is read twice.
+// (4 x 4096 positions of 32 groups of 16 channels in bf16, the groups in registers of 1024
+// threads, 32 bytes of a position each: 45 us, read twice 17.)
 struct RowShape { int nv, b, tpi; };
-RowShape row_shape(int64_t pieces, bool grad) {
-  if (pieces <= 64) return {1, 256, pow2_up(pieces)};
+RowShape row_shape(int64_t pieces, int S, bool grad) {
+  if (grad && S > 1) return {0, 0, 0};
+  if (pieces <= 64) return {1, grad ? 1024 : 256, pow2_up(pieces)};
   if (pieces <= 128) return {2, 256, 64};
   if (pieces <= 256) return {4, 256, 64};
-  if (pieces <= 1024) return {4, 256, 256};
-  if (!grad && pieces <= 4096) return {4, 1024, 1024};
-  if (!grad && pieces <= 8192) return {8, 1024, 1024};
+  if (S == 1 && pieces <= 1024) return {4, 256, 256};
   return {0, 0, 0};
 }
 
@@ -605,7 +682,7 @@ int row_parts(GroupArgs& a, const RowShape& r, bool grad) {
   a.gw = largest_divisor(a.G, ipb);
   a.nw = std::max(1, ipb / a.gw);
   const int64_t blocks = a.G / a.gw, rounds = (a.N + a.nw - 1) / a.nw;
-  const int64_t most = std::max<int64_t>(1, (grad ? 1024 : 8192) * 256 / r.b / blocks);
+  const int64_t most = std::max<int64_t>(1, (grad ? 1024 : 2048) * 256 / r.b / blocks);
   return (int)std::max<int64_t>(1, std::min(rounds, most));
 }
 
@@ -614,7 +691,7 @@ void tile_parts(GroupArgs& a, int V) {
   const int64_t pr = a.Cg / V;
   a.cblocks = pr <= 256 ? (int)((a.G + 256 / pr - 1) / (256 / pr)) : (int)(a.G * ((pr + 255) / 256));
   const int step = pr <= 256 ? (int)std::max<int64_t>(1, 256 / (pr * std::min<int64_t>(a.G, 256 / pr))) : 1;
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, a.N * a.cblocks));
+  const int64_t want = std::max<int64_t>(1, 768 / std::max<int64_t>(1, a.N * a.cblocks));
   const int64_t most = std::max<int64_t>(1, a.S / (8ll * step));  // eight positions a thread
   a.sparts = (int)std::min<int64_t>(std::min(want, most), 256);
 }
@@ -627,109 +704,125 @@ GroupArgs sizes(int64_t N, int S, int G, int Cg) {
   a.N = N, a.S = S, a.G = G, a.Cg = Cg, a.C = G * Cg;
   return a;
 }
-bool in_registers(int S, int Cg, int V, bool grad) {
-  return grad ? S == 1 && row_shape(Cg / V, true).nv : row_shape((int64_t)S * (Cg / V), false).nv;
+RowShape shape_of(int S, int Cg, int V, bool grad) {
+  return row_shape((int64_t)S * (Cg / V), S, grad);
+}
+int64_t parts_a_group(const GroupArgs& a, int V) {
+  const int pr = a.Cg / V;
+  return (int64_t)a.sparts * (pr > 256 ? (pr + 255) / 256 : 1);
 }
 }  // namespace
 
 int64_t group_forward_blocks(int64_t N, int S, int G, int Cg, int dtype) {
   GroupArgs a = sizes(N, S, G, Cg);
   const int V = vec_of(Cg, dtype);
-  if (in_registers(S, Cg, V, false)) return 0;
+  if (shape_of(S, Cg, V, false).nv) return 0;
   tile_parts(a, V);
   return N * a.sparts * a.cblocks;
 }
 int64_t group_forward_workspace(int64_t N, int S, int G, int Cg, int dtype) {
   GroupArgs a = sizes(N, S, G, Cg);
-  const int V = vec_of(Cg, dtype), pr = Cg / V;
-  if (in_registers(S, Cg, V, false)) return 0;
+  const int V = vec_of(Cg, dtype);
+  if (shape_of(S, Cg, V, false).nv) return 0;
   tile_parts(a, V);
-  return N * G * a.sparts * (pr > 256 ? (pr + 255) / 256 : 1) * 4;
+  return N * G * parts_a_group(a, V) * 4;
 }
 
 int64_t group_backward_blocks(int64_t N, int S, int G, int Cg, int dtype) {
   GroupArgs a = sizes(N, S, G, Cg);
   const int V = vec_of(Cg, dtype);
-  if (in_registers(S, Cg, V, true)) return 0;
+  if (shape_of(S, Cg, V, true).nv) return 0;
   tile_parts(a, V);
-  return N * std::max<int64_t>((int64_t)a.sparts * a.cblocks, G);
+  return N * a.sparts * a.cblocks + 2 * ((a.C + 15) / 16);
 }
 int64_t group_backward_workspace(int64_t N, int S, int G, int Cg, int dtype) {
   GroupArgs a = sizes(N, S, G, Cg);
   const int V = vec_of(Cg, dtype);
-  if (in_registers(S, Cg, V, true)) return 2ll * row_parts(a, row_shape(Cg / V, true), true) * a.C;
+  const RowShape r = shape_of(S, Cg, V, true);
+  if (r.nv) return 2ll * row_parts(a, r, true) * a.C;
   tile_parts(a, V);
-  return 2 * N * a.sparts * a.C + 2 * N * G;
+  return 2 * N * a.sparts * a.C + 2 * N * G * parts_a_group(a, V);
 }
 
-#define GDN_GN_ROWS(X) X(1, 256) X(2, 256) X(4, 256)
-
-template <typename T, int V>
+template <typename T, int V, int OPS>
 static hipError_t group_forward(GroupArgs a, hipStream_t st) {
-  const RowShape r = row_shape((int64_t)a.S * (a.Cg / V), false);
+  const RowShape r = shape_of(a.S, a.Cg, V, false);
   if (r.nv) {
-    const unsigned grid = (unsigned)(row_parts(a, r, false) * (a.G / a.gw));
-#define GDN_X(NV, B)                                                              \
-  if (r.nv == NV && r.b == B) {                                                   \
-    hipLaunchKernelGGL((k_gn_rows<T, V, NV, B>), dim3(grid), dim3(B), 0, st, a);  \
-    return hipGetLastError();                                                     \
-  }
-    GDN_GN_ROWS(GDN_X) GDN_X(4, 1024) GDN_X(8, 1024)
-#undef GDN_X
-    return hipErrorNotSupported;
+    const dim3 grid((unsigned)(row_parts(a, r, false) * (a.G / a.gw)));
+    if (r.nv == 1)
+      hipLaunchKernelGGL((k_gn_rows<T, V, 1, OPS>), grid, dim3(256), 0, st, a);
+    else if (r.nv == 2)
+      hipLaunchKernelGGL((k_gn_rows<T, V, 2, OPS>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_gn_rows<T, V, 4, OPS>), grid, dim3(256), 0, st, a);
+    return hipGetLastError();
   }
   tile_parts(a, V);
-  const unsigned grid = (unsigned)(a.N * a.sparts * a.cblocks);
-  hipLaunchKernelGGL((k_gn_stats<T, V>), dim3(grid), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)(a.N * a.sparts * a.cblocks));
+  hipLaunchKernelGGL((k_gn_stats<T, V>), grid, dim3(256), 0, st, a);
   if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL((k_gn_apply<T, V>), dim3(grid), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_gn_apply<T, V, OPS>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
-template <typename T, int V>
+template <typename T, int V, int OPS>
 static hipError_t group_backward(GroupArgs a, hipStream_t st) {
+  const RowShape r = shape_of(a.S, a.Cg, V, true);
+  const unsigned adding = a.dw || a.db ? 2 * ((a.C + 15) / 16) : 0;
   int64_t parts = 0;
-  if (a.N == 0) {
-  } else if (in_registers(a.S, a.Cg, V, true)) {
-    const RowShape r = row_shape(a.Cg / V, true);
-    parts = row_parts(a, r, true);
-    const unsigned grid = (unsigned)(parts * (a.G / a.gw));
-    const size_t lds = (64 + (a.nw > 1 ? 2 * (size_t)a.gw * a.Cg : 0)) * sizeof(float);
-#define GDN_X(NV, B)                                                                         \
-  if (r.nv == NV && r.b == B)                                                                \
-    hipLaunchKernelGGL((k_gn_rows_grad<T, V, NV, B>), dim3(grid), dim3(B), lds, st, a, (int)parts);
-    GDN_GN_ROWS(GDN_X)
-#undef GDN_X
-  } else {
+  if (a.N > 0 && !r.nv) {
     tile_parts(a, V);
-    parts = a.N * a.sparts;
-    const unsigned grid = (unsigned)(parts * a.cblocks);
-    hipLaunchKernelGGL((k_gn_sums<T, V>), dim3(grid), dim3(256), 0, st, a);
+    const unsigned grid = (unsigned)(a.N * a.sparts * a.cblocks);
+    hipLaunchKernelGGL((k_gn_sums<T, V, OPS>), dim3(grid), dim3(256), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL(k_gn_means, dim3((unsigned)(a.N * a.G)), dim3(256), 0, st, a);
-    if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((k_gn_dx<T, V>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_gn_dx<T, V, OPS>), dim3(grid + adding), dim3(256), 0, st, a, (int)adding);
+    return hipGetLastError();
   }
-  if (hipError_t e = hipGetLastError()) return e;
-  if (!a.dw && !a.db) return hipSuccess;
-  hipLaunchKernelGGL(k_gn_parts, dim3((unsigned)((a.C + 15) / 16), 2), dim3(256), 0, st, a.ws, a.dw,
-                     a.db, parts, a.C);
+  if (a.N > 0) {
+    parts = row_parts(a, r, true);
+    const dim3 grid((unsigned)(parts * (a.G / a.gw)));
+    const size_t lds = (64 + (a.nw > 1 ? 2 * (size_t)a.gw * a.Cg : 0)) * sizeof(float);
+    if (r.nv == 1)
+      hipLaunchKernelGGL((k_gn_rows_grad<T, V, 1, 1024, OPS>), grid, dim3(1024), lds, st, a, (int)parts);
+    else if (r.nv == 2)
+      hipLaunchKernelGGL((k_gn_rows_grad<T, V, 2, 256, OPS>), grid, dim3(256), lds, st, a, (int)parts);
+    else
+      hipLaunchKernelGGL((k_gn_rows_grad<T, V, 4, 256, OPS>), grid, dim3(256), lds, st, a, (int)parts);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  if (!adding) return hipSuccess;
+  hipLaunchKernelGGL(k_gn_parts, dim3(adding), dim3(256), 0, st, a, parts);
   return hipGetLastError();
+}
+
+// by type, values a piece and what follows n
+template <int OPS>
+static hipError_t by_width(const GroupArgs& a, int dtype, bool grad, hipStream_t st) {
+  const int v = vec_of(a.Cg, dtype);
+#define GDN_X(T, V) return grad ? group_backward<T, V, OPS>(a, st) : group_forward<T, V, OPS>(a, st)
+  if (dtype == 0) {
+    if (v == 4) GDN_X(float, 4);
+    GDN_X(float, 1);
+  }
+  if (v == 8) GDN_X(__bf16, 8);
+  if (v == 2) GDN_X(__bf16, 2);
+  GDN_X(__bf16, 1);
+#undef GDN_X
+}
+static hipError_t by_ops(const GroupArgs& a, int dtype, bool grad, hipStream_t st) {
+  switch ((a.act ? kAct : 0) | (a.z ? kGate : 0)) {
+    case 0: return by_width<0>(a, dtype, grad, st);
+    case kAct: return by_width<kAct>(a, dtype, grad, st);
+    case kGate: return by_width<kGate>(a, dtype, grad, st);
+    default: return by_width<kAct | kGate>(a, dtype, grad, st);
+  }
 }
 
 hipError_t launch_group_forward(const GroupArgs& a, int dtype, hipStream_t st) {
-  const int v = vec_of(a.Cg, dtype);
-  if (dtype == 0) return v == 4 ? group_forward<float, 4>(a, st) : group_forward<float, 1>(a, st);
-  return v == 8   ? group_forward<__bf16, 8>(a, st)
-         : v == 2 ? group_forward<__bf16, 2>(a, st)
-                  : group_forward<__bf16, 1>(a, st);
+  return by_ops(a, dtype, false, st);
 }
 hipError_t launch_group_backward(const GroupArgs& a, int dtype, hipStream_t st) {
-  const int v = vec_of(a.Cg, dtype);
-  if (dtype == 0) return v == 4 ? group_backward<float, 4>(a, st) : group_backward<float, 1>(a, st);
-  return v == 8   ? group_backward<__bf16, 8>(a, st)
-         : v == 2 ? group_backward<__bf16, 2>(a, st)
-                  : group_backward<__bf16, 1>(a, st);
+  return by_ops(a, dtype, true, st);
 }
 
 }  // namespace gdn
