@@ -39,6 +39,14 @@ namespace gdn {
 
 namespace {
 
+// A value that the compiler takes for new at this point.  What a loop derives from it, LDS
+// addresses above all, is formed again each time: kept from outside the loop, they were more
+// registers than there are and came from scratch memory one after the other.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 template <typename T> struct FragFor { typedef f32x4 type; };
 template <> struct FragFor<__bf16> { typedef bf16x4 type; };
 
@@ -130,26 +138,44 @@ struct Tile {
   }
 };
 
-// The same on the way from memory, NT threads.
+// The same on the way from memory, NT threads: thread t has the pieces of one column of rows
+// t / CPR, and NT / CPR further each.
 template <int D, int NT, typename T>
 struct Rows {
   typedef Tile<D, T> L;
-  static constexpr int E = L::E, CPR = L::CPR, N = LC * CPR / NT;
+  static constexpr int E = L::E, CPR = L::CPR, N = LC * CPR / NT, R = NT / CPR;
   typedef T Vec __attribute__((ext_vector_type(E)));
   Vec v[N];
-  // p: the chunk's first token, ld values a token; rows past m repeat one of its own
-  __device__ __forceinline__ void load(const T* __restrict__ p, uint32_t ld, int m, bool rev) {
+  // t: the thread; p: the chunk's first token, ld values a token; rows past m repeat one of its own
+  template <bool REV>
+  __device__ __forceinline__ void load(const T* __restrict__ p, uint32_t ld, int m, int t) {
+    const uint32_t r0 = (uint32_t)t / CPR, c = (uint32_t)t % CPR * E;
+    if (m == LC) {  // one offset a lane, the rest is the wave's
+      const uint32_t off = ((REV ? R - 1 - r0 : r0) * ld + c) * sizeof(T);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + NT * i, r = min(at / CPR, m - 1);
-      v[i] = *(const Vec*)(p + ((uint32_t)(rev ? m - 1 - r : r) * ld + at % CPR * E));
+      for (int i = 0; i < N; ++i) {
+        const T* pi = p + (int64_t)((REV ? N - 1 - i : i) * R) * ld;
+        v[i] = *(const Vec*)((const char*)pi + off);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = min((int)r0 + R * i, m - 1);
+        v[i] = *(const Vec*)(p + ((uint32_t)(REV ? m - 1 - r : r) * ld + c));
+      }
     }
   }
-  __device__ __forceinline__ void store(T* s, int m) const {
+  __device__ __forceinline__ void store(T* s, int m, int t) const {
+    const int r0 = (uint32_t)t / CPR, c = (uint32_t)t % CPR * E;
+    auto to = [&](int i) {  // (rows 16 apart are turned alike)
+      return R % 16 == 0 ? s + L::at(r0, c) + i * R * D : s + L::at(r0 + R * i, c);
+    };
+    if (m == LC) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + NT * i, r = at / CPR;
-      *(Vec*)(s + L::at(r, at % CPR * E)) = r < m ? v[i] : Vec{};
+      for (int i = 0; i < N; ++i) *(Vec*)to(i) = v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) *(Vec*)to(i) = r0 + R * i < m ? v[i] : Vec{};
     }
   }
 };
@@ -367,9 +393,10 @@ __device__ __forceinline__ uint32_t work_item(uint32_t b, uint32_t n) {
 }
 
 // ---- what a segment adds to the state
-template <int DK, int DV, int NS, typename T, int TS>
+template <int DK, int DV, int NS, typename T, int TS, bool REV>
 __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& sg, uint32_t slot,
-                                               int h, bool rev, T* sK, T* sV, Gates* gt) {
+                                               int h, T* sK, T* sV, Gates* gt) {
+  constexpr bool rev = REV;
   const int gr = a.Hv / a.Hk;
   const T* K = (const T*)(rev ? a.Q : a.K) + (sg.t0 * a.Hk + h / gr) * DK;
   const T* V = (const T*)(rev ? a.dO : a.V) + (sg.t0 * a.Hv + h) * DV;
@@ -384,16 +411,16 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
   Rows<DV, NT, T> v;
   auto fetch = [&](int i) __attribute__((always_inline)) {
     const int at = ch.at(i), m = ch.size(i);
-    k.load(K + (int64_t)at * ldk, ldk, m, rev);
-    v.load(V + (int64_t)at * ldv, ldv, m, rev);
+    k.template load<REV>(K + (int64_t)at * ldk, ldk, m, threadIdx.x);
+    v.template load<REV>(V + (int64_t)at * ldv, ldv, m, threadIdx.x);
   };
   GateStream gates(a, sg, ch, h, w == 2, 1.f, rev ? a.scale : 1.f);
   fetch(0);
   gates.form(gt, 0);
   for (int i = 0; i < ch.n; ++i) {
     lds_only_barrier();
-    k.store(sK, ch.size(i));
-    v.store(sV, ch.size(i));
+    k.store(sK, ch.size(i), threadIdx.x);
+    v.store(sV, ch.size(i), threadIdx.x);
     if (i + 1 < ch.n) fetch(i + 1);
     lds_only_barrier();
     gates.form(gt, i + 1);
@@ -421,7 +448,10 @@ __global__ __launch_bounds__(4 * DV / NS) void k_lin_state(const LinArgs a, uint
   const Segment sg(a.q, slot);
   // (the last segment's share ends in S_final, the first one's in dS0: the walks form those)
   if (sg.len == 0 || (rev ? sg.j == 0 : sg.j == sg.n - 1)) return;
-  add_of_segment<DK, DV, NS, T, TS>(a, sg, slot, h, rev, sK, sV, gt);
+  if (rev)
+    add_of_segment<DK, DV, NS, T, TS, true>(a, sg, slot, h, sK, sV, gt);
+  else
+    add_of_segment<DK, DV, NS, T, TS, false>(a, sg, slot, h, sK, sV, gt);
 }
 
 // The states carried over the segments of each sequence, in place: U from what a segment
@@ -508,10 +538,10 @@ struct Source {
   T* s;
   Rows<D, NT, T> r;
   __device__ Source(const T* from, int heads, T* to) : p(from), ld((uint32_t)heads * D), s(to) {}
-  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
-    r.load(p + (int64_t)at * ld, ld, m, rev);
+  template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
+    r.template load<REV>(p + (int64_t)at * ld, ld, m, t);
   }
-  __device__ __forceinline__ void store(int m) const { r.store(s, m); }
+  __device__ __forceinline__ void store(int m, int t) const { r.store(s, m, t); }
 };
 
 // P's fragments of row block I: pair p of column blocks
@@ -534,7 +564,6 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
   constexpr int NQ = DK / 32, NW = DV / 16 / NS, MO = kTerms<F, TO>, MP = kTerms<F, TP>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % NW;
   const Lane ln = lane_here();
-  const int g4 = 4 * ln.g(), c = ln.c();
   constexpr bool rev = kReversed<P>, flip = kFlipped<P>;
   constexpr bool far_rows = DG && flip, pairs = DG && P == kDK;
   const Chunks ch(sg, rev);
@@ -559,7 +588,7 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     ps.rows[ch.token(i, ln.id)] = f;
   };
   GateStream gates(a, sg, ch, h, w == 2, rev ? 1.f : a.scale, rev ? a.scale : 1.f);
-  tiles.fetch(ch.at(0), ch.size(0), rev);
+  tiles.template fetch<rev>(ch.at(0), ch.size(0), threadIdx.x);
   gates.form(lds->gt, 0);
   // P's blocks above the diagonal that share a pair with one on it
   if (w < 2) {
@@ -573,11 +602,13 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     }
   }
   for (int i = 0; i < ch.n; ++i) {
+    const Lane ln{anew(lane_id())};
+    const int g4 = 4 * ln.g(), c = ln.c();
     const int at = ch.at(i), m = ch.size(i);
     const bool end = i == ch.n - 1;
     const Gates* gt = lds->gt + (i & 1);
     lds_only_barrier();
-    tiles.store(m);
+    tiles.store(m, anew(threadIdx.x));
     write_rows(i - 1);
     lds_only_barrier();
     if (pairs && end) {
@@ -595,14 +626,6 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       }
       if (ln.id == 0) lds->part[w] = x;
     }
-    // rows of x at the results' places
-    RunOf<T, 4 * NS> xr[4];
-    if constexpr (far_rows && !XS)
-#pragma unroll
-      for (int I = 0; I < 4; ++I)
-        xr[I] = *(const RunOf<T, 4 * NS>*)((const T*)ps.x +
-                                           (int64_t)ch.token(i, min(16 * I + c, m - 1)) * ps.ldo +
-                                           16 * NS * w + NS * g4);
     // P's blocks in row form: lane (g, c) has columns 16 J + 4g .. of row 16 I + c; two of them
     // at a time
     auto products = [&](int I, int J) __attribute__((always_inline)) {
@@ -688,6 +711,16 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
         finish(p, y, 3, J);
       }
     }
+    // rows of x at the results' places
+    RunOf<T, 4 * NS> xr[4];
+    if constexpr (far_rows && !XS)
+#pragma unroll
+      for (int I = 0; I < 4; ++I) {
+        const T* xc = (const T*)ps.x + (int64_t)at * ps.ldo + 16 * NS * w;
+        const int r = min(16 * I + c, m - 1);
+        const uint32_t off = (uint32_t)(rev ? m - 1 - r : r) * ps.ldo + NS * g4;
+        xr[I] = *(const RunOf<T, 4 * NS>*)((const char*)xc + off * (uint32_t)sizeof(T));
+      }
     gates.form(lds->gt, i + 1);
     // what comes from the state
     f32x4 o[4][NS];
@@ -714,10 +747,11 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
               o[I0 + I][n] = Pair<F>::template mma<true>(x[I], y[n].t[t], o[I0 + I][n]);
       }
     }
-    // lane (g, c): columns 16 NS w + NS g4 .. of row 16 I + c
-    const uint32_t row0 = (uint32_t)(rev ? m - 1 - c : c) * ps.ldo + 16 * NS * w + NS * g4;
-    const uint32_t down = (rev ? -16 : 16) * ps.ldo;
-    const int64_t chunk = (int64_t)at * ps.ldo;
+    // lane (g, c): columns 16 NS w + NS g4 .. of row 16 I + c; one offset a lane
+    const uint32_t place = (uint32_t)(rev ? 15 - c : c) * ps.ldo + NS * g4;
+    auto block = [&](int I) {
+      return ((int64_t)at + (rev ? m - 16 - 16 * I : 16 * I)) * ps.ldo + 16 * NS * w;
+    };
 #pragma unroll
     for (int I = 0; I < 4; ++I) {
       const float f = gt->out[16 * I + c];
@@ -739,7 +773,7 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
         far = sum_apart32(sum_apart16(far));
         if (ln.g() == 0) lds->far[w][16 * I + c] = far;
       }
-    if (!end) tiles.fetch(ch.at(i + 1), ch.size(i + 1), rev);
+    if (!end) tiles.template fetch<rev>(ch.at(i + 1), ch.size(i + 1), anew(threadIdx.x));
     S.template update<TS>(sk, sv, gt, w, ln);
     lds_only_barrier();
     if (pairs && end && w == 0 && ln.id == 0) {
@@ -790,13 +824,14 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       if (16 * I + c < m)
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-          const uint32_t to = row0 + I * down + 4 * n;
           f32x4 y = o[I][n];
-          if (flip && ps.acc && !ps.first) y += *(const f32x4*)(ps.acc + chunk + to);
+          float* acc = (float*)((char*)(ps.acc + block(I)) + place * 4) + 4 * n;
+          if (flip && ps.acc && !ps.first) y += *(const f32x4*)acc;
           if (flip && ps.acc && !ps.last)
-            *(f32x4*)(ps.acc + chunk + to) = y;
+            *(f32x4*)acc = y;
           else
-            *(Out*)((T*)ps.out + chunk + to) = __builtin_convertvector(y, Out);
+            *(Out*)((T*)((char*)((T*)ps.out + block(I)) + place * (uint32_t)sizeof(T)) + 4 * n) =
+                __builtin_convertvector(y, Out);
         }
   }
   if (!flip && ps.fin) S.store(ps.fin, flip, w, ln);
@@ -810,21 +845,21 @@ template <int DK, int DV, int NT, typename T>
 struct PassTiles {
   Source<DK, NT, T> q, k;
   Source<DV, NT, T> v;
-  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
-    q.fetch(at, m, rev), k.fetch(at, m, rev), v.fetch(at, m, rev);
+  template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
+    q.template fetch<REV>(at, m, t), k.template fetch<REV>(at, m, t), v.template fetch<REV>(at, m, t);
   }
-  __device__ __forceinline__ void store(int m) const { q.store(m), k.store(m), v.store(m); }
+  __device__ __forceinline__ void store(int m, int t) const { q.store(m, t), k.store(m, t), v.store(m, t); }
 };
 // Two of one kind each: of DA and of DB values a row.
 template <int DA, int DB, int NT, typename T>
 struct TwoAndTwo {
   Source<DA, NT, T> a0, a1;
   Source<DB, NT, T> b0, b1;
-  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
-    a0.fetch(at, m, rev), a1.fetch(at, m, rev), b0.fetch(at, m, rev), b1.fetch(at, m, rev);
+  template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
+    a0.template fetch<REV>(at, m, t), a1.template fetch<REV>(at, m, t), b0.template fetch<REV>(at, m, t), b1.template fetch<REV>(at, m, t);
   }
-  __device__ __forceinline__ void store(int m) const {
-    a0.store(m), a1.store(m), b0.store(m), b1.store(m);
+  __device__ __forceinline__ void store(int m, int t) const {
+    a0.store(m, t), a1.store(m, t), b0.store(m, t), b1.store(m, t);
   }
 };
 // Those of dQ or dK of two heads, MORE: with x.
@@ -832,14 +867,14 @@ template <int DA, int DB, int NT, typename T, bool MORE>
 struct FourAndMore {
   Source<DA, NT, T> a0, a1, a2, a3;
   Source<DB, NT, T> b0, b1;
-  __device__ __forceinline__ void fetch(int at, int m, bool rev) {
-    a0.fetch(at, m, rev), a1.fetch(at, m, rev), a2.fetch(at, m, rev), a3.fetch(at, m, rev);
-    b0.fetch(at, m, rev);
-    if (MORE) b1.fetch(at, m, rev);
+  template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
+    a0.template fetch<REV>(at, m, t), a1.template fetch<REV>(at, m, t), a2.template fetch<REV>(at, m, t), a3.template fetch<REV>(at, m, t);
+    b0.template fetch<REV>(at, m, t);
+    if (MORE) b1.template fetch<REV>(at, m, t);
   }
-  __device__ __forceinline__ void store(int m) const {
-    a0.store(m), a1.store(m), a2.store(m), a3.store(m), b0.store(m);
-    if (MORE) b1.store(m);
+  __device__ __forceinline__ void store(int m, int t) const {
+    a0.store(m, t), a1.store(m, t), a2.store(m, t), a3.store(m, t), b0.store(m, t);
+    if (MORE) b1.store(m, t);
   }
 };
 
