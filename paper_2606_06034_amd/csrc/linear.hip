@@ -94,14 +94,16 @@ __device__ __forceinline__ float exp2_of(double x) {
 // differences are numbers.
 struct Gates {
   float hi[LC], lo[LC], out[LC], in[LC];  // H in units of log 2; s_out e^H, s_in e^{total - H}
-  float el, pad[3];                       // e^total
+  float el;                               // e^total
+  double sum;                             // of the totals, in units of log 2 (k_lin_state)
 };
 __device__ __forceinline__ double log_decay(float g) {
   return (double)(g < -1e4f ? -1e4f : g) * kLog2e;
 }
 // wave-wide: row l of m, `g` its token's (per_token) or the head's; returns the total
+// (after: what the rows' values decay by past the chunk, as well)
 __device__ __forceinline__ double form_gates(Gates* s, float g, bool per_token, int m, bool rev,
-                                             float s_out, float s_in) {
+                                             float s_out, float s_in, double after = 0.0) {
   const int l = lane_id();
   double H, total;
   if (per_token) {
@@ -118,7 +120,7 @@ __device__ __forceinline__ double form_gates(Gates* s, float g, bool per_token, 
   s->hi[l] = hi;
   s->lo[l] = (float)(H - (double)hi);
   s->out[l] = s_out * exp2_of(H);
-  s->in[l] = s_in * exp2_of(total - H);
+  s->in[l] = s_in * exp2_of((total - H) + after);
   if (l == 0) s->el = exp2_of(total);
   return total;
 }
@@ -290,16 +292,17 @@ struct StateOf {
         }
       }
   }
-  // S <- el S + (diag(in) K)^T V of the chunk in LDS, the factor on V's rows
-  template <int TS, typename T>
-  __device__ __forceinline__ void update(const T* sK, const T* sV, const Gates* gt, int w,
-                                         Lane ln) {
-    typedef typename FragFor<T>::type F;
-    const float el = gt->el;
+  __device__ __forceinline__ void decay(float el) {
 #pragma unroll
     for (int m = 0; m < 2 * NQ; ++m)
 #pragma unroll
       for (int n = 0; n < NS; ++n) b[m][n] *= el;
+  }
+  // S <- S + (diag(in) K)^T V of the chunk in LDS, the factor on V's rows
+  template <int TS, typename T>
+  __device__ __forceinline__ void update(const T* sK, const T* sV, const Gates* gt, int w,
+                                         Lane ln) {
+    typedef typename FragFor<T>::type F;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const f32x4 wl = *(const f32x4*)(gt->in + 32 * p + 4 * ln.g());
@@ -403,8 +406,8 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
   const uint32_t ldk = (uint32_t)a.Hk * DK, ldv = (uint32_t)a.Hv * DV;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane ln = lane_here();
-  const Chunks ch(sg, rev);
   constexpr int NT = 4 * DV / NS;
+  const Chunks ch(sg, rev);
   StateOf<DK, DV, NS> S;
   S.zero();
   Rows<DK, NT, T> k;
@@ -414,22 +417,50 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
     k.template load<REV>(K + (int64_t)at * ldk, ldk, m, threadIdx.x);
     v.template load<REV>(V + (int64_t)at * ldv, ldv, m, threadIdx.x);
   };
-  GateStream gates(a, sg, ch, h, w == 2, 1.f, rev ? a.scale : 1.f);
-  fetch(0);
-  gates.form(gt, 0);
-  for (int i = 0; i < ch.n; ++i) {
+  // From the last chunk to the first, each decayed past those after it, so that nothing is
+  // scaled again; and no further than to where nothing is left of a value (2^-160 of it: fp32
+  // has none below 2^-149).
+  constexpr double kNothing = -160.0;
+  double total = 0.0;  // of the chunks so far: the first wave's
+  auto gates = [&](int i, float g) __attribute__((always_inline)) {
+    if (w != 0) return;
+    total += form_gates(gt + (i & 1), g, a.per_token, ch.size(i), rev, 1.f, rev ? a.scale : 1.f, total);
+    if (ln.id == 0) gt[i & 1].sum = total;
+  };
+  auto decay_of = [&](int i) __attribute__((always_inline)) {
+    if (i < 0 || w != 0) return 0.f;
+    return a.per_token
+               ? a.g[(sg.t0 + ch.token(i, min(ln.id, ch.size(i) - 1))) * (int64_t)a.Hv + h]
+               : a.g[h];
+  };
+  int i = ch.n - 1;
+  float g = decay_of(i);
+  fetch(i);
+  gates(i, g);
+  g = decay_of(i - 1);
+  for (;; --i) {
     lds_only_barrier();
+    const bool more = i > 0 && !(gt[i & 1].sum < kNothing);
     k.store(sK, ch.size(i), threadIdx.x);
     v.store(sV, ch.size(i), threadIdx.x);
-    if (i + 1 < ch.n) fetch(i + 1);
+    if (more) fetch(i - 1);
     lds_only_barrier();
-    gates.form(gt, i + 1);
+    if (more) {
+      gates(i - 1, g);
+      g = decay_of(i - 2);
+    }
     S.template update<TS>(sK, sV, gt + (i & 1), w, ln);
+    if (!more) break;
+  }
+  for (; w == 0 && i > 0; --i) {  // (the decay over all of the segment)
+    const float x = decay_of(i - 1);
+    total += a.per_token ? lane63(prefix64(ln.id < ch.size(i - 1) ? log_decay(x) : 0.0))
+                         : log_decay(x) * ch.size(i - 1);
   }
   float* to = (rev ? a.R : a.U) + ((int64_t)slot * a.Hv + h) * DK * DV;
   S.store(to, false, w, ln);
-  if (threadIdx.x == 128 && (!rev || sg.j == sg.n - 1))  // (once for each segment)
-    a.dec[(int64_t)slot * a.Hv + h] = exp2_of(gates.total);
+  if (threadIdx.x == 0 && (!rev || sg.j == sg.n - 1))  // (once for each segment)
+    a.dec[(int64_t)slot * a.Hv + h] = exp2_of(total);
 }
 
 }  // namespace
@@ -474,7 +505,7 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinArgs a, int parts) {
     f32x4 S = from ? *(const f32x4*)(from + (int64_t)sh * size + e) : zero4();
     float* X = (rev ? a.R : a.U) + (base * a.Hv + h) * size + e;
     const float* d = a.dec + base * a.Hv + h;
-    constexpr int A = 4;  // asked for ahead
+    constexpr int A = 8;  // asked for ahead
     for (int i0 = 0; i0 < n; i0 += A) {
       f32x4 x[A];
       float f[A];
@@ -774,6 +805,7 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
         if (ln.g() == 0) lds->far[w][16 * I + c] = far;
       }
     if (!end) tiles.template fetch<rev>(ch.at(i + 1), ch.size(i + 1), anew(threadIdx.x));
+    S.decay(gt->el);
     S.template update<TS>(sk, sv, gt, w, ln);
     lds_only_barrier();
     if (pairs && end && w == 0 && ln.id == 0) {
@@ -921,7 +953,12 @@ __global__ __launch_bounds__(4 * DV / NS, waves_of<T>(4 * DV / NS)) void k_lin_f
   ps.out = (T*)a.O + tv;
   ps.start = a.U ? a.U + ((int64_t)slot * a.Hv + h) * size : a.S0 ? a.S0 + own : nullptr;
   ps.fin = a.Sf && sg.j == sg.n - 1 ? a.Sf + own : nullptr;
-  walk<DK, DV, NS, T, TS, TO, TP, kO, false, false>(a, sg, h, ps, tiles, &lds);
+  // (a state that goes into outputs in bf16 alone takes up values in as many terms as it gives;
+  // the last segment's is S_final, asked for or not: the outputs are the same either way)
+  if (TS > TO && sg.j != sg.n - 1)
+    walk<DK, DV, NS, T, TO, TO, TP, kO, false, false>(a, sg, h, ps, tiles, &lds);
+  else
+    walk<DK, DV, NS, T, TS, TO, TP, kO, false, false>(a, sg, h, ps, tiles, &lds);
 }
 
 // ---- the gradients.  A workgroup is two teams of four waves on common tiles (read apart, the
@@ -992,7 +1029,7 @@ __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segm
     if (more) ps.x = s + 4 * VT + KT;
     ps.acc = gr > 2 ? (rev ? a.acc_k : a.acc_q) + tk : nullptr;
     ps.first = u == 0, ps.last = u == gr - 2;
-    walk<DV, DK, DK / 64, T, TS, TO, TP, P, DG, more>(a, sg, h + team, ps, tiles, lds + team, other);
+    walk<DV, DK, DK / 64, T, DG ? TS : TO, TO, TP, P, DG, more>(a, sg, h + team, ps, tiles, lds + team, other);
     lds_only_barrier();
   }
 }
@@ -1032,7 +1069,11 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a,
                                     {(const T*)a.dO + tv + DV, a.Hv, s + 2 * KT + VT}};
     Pass ps = value_pass<DK, DV, T>(a, sg, slot, h + team);
     ps.q = s, ps.k = s + KT, ps.v = s + 2 * KT + team * VT;
-    walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles, lds + team);
+    if (sg.j == 0)
+      walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles, lds + team);
+    else
+      walk<DK, DV, DV / 64, T, kOut, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles,
+                                                                 lds + team);
   }
 }
 
@@ -1064,7 +1105,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uin
       ps.q = sV, ps.k = sO, ps.v = sQ, ps.x = sK;
       ps.acc = gr > 1 ? a.acc_k + tk : nullptr;
       ps.first = u == 0, ps.last = u == gr - 1;
-      walk<DV, DK, DK / 64, T, TS, TO, TP, kDK, DG, true>(a, sg, h, ps, tiles, lds);
+      walk<DV, DK, DK / 64, T, DG ? TS : TO, TO, TP, kDK, DG, true>(a, sg, h, ps, tiles, lds);
     } else {
       Pass ps = value_pass<DK, DV, T>(a, sg, slot, h);
       ps.q = sK, ps.k = sQ, ps.v = sO;
@@ -1109,7 +1150,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(co
       ps = value_pass<DK, DV, T>(a, sg, slot, h);
     }
     ps.q = sq, ps.k = sk, ps.v = sv;
-    walk<D0, D1, D1 / 64, T, TS, TO, TP, P, DG, false>(a, sg, h, ps, tiles, &lds);
+    walk<D0, D1, D1 / 64, T, DG || !keys ? TS : TO, TO, TP, P, DG, false>(a, sg, h, ps, tiles, &lds);
     lds_only_barrier();
   }
 }
