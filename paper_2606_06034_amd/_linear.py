@@ -10,7 +10,8 @@ from typing import Optional
 import torch
 
 from ._binding import _FDT, _check, _fdtype, _on_stream, lib
-from ._layer import _dev, _groups, _opt, _params, _stream
+from . import _layer
+from ._layer import _groups, _params, _stream
 
 _c_int, _c_i64, _c_f, _vp = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 
@@ -43,6 +44,28 @@ def linear_abi_symbols():
 
 
 _F32, _I32 = torch.float32, torch.int32
+_device = _layer._device or torch.cuda.current_device
+
+
+def _dev(t: torch.Tensor, name: str, dtype=None, numel: Optional[int] = None) -> int:
+    """Address of a tensor of the current device, where the launches go."""
+    p = _layer._dev(t, name, dtype, numel)
+    if t.get_device() != _device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device (cuda:{_device()}): "
+                         f"call under torch.cuda.device(), or name a stream of {t.device}")
+    return p
+
+
+def _opt(t: Optional[torch.Tensor], name: str, dtype=None, numel: Optional[int] = None):
+    return None if t is None else _dev(t, name, dtype, numel)
+
+
+def _affine(weight, bias, C):
+    """Pointers of weight and bias and their dtype (one dtype for both)."""
+    p = _params(weight, bias, C)
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        _opt(t, name)
+    return p
 
 
 def _sizes(K, V, cu):
@@ -241,7 +264,7 @@ def gdn_group_norm_forward(x: torch.Tensor, groups: int, weight: Optional[torch.
     if want_stats:
         rstd = x.new_empty((N, groups), dtype=torch.float32)
         mean = torch.empty_like(rstd)
-    wp, bp, wdt = _params(weight, bias, C)
+    wp, bp, wdt = _affine(weight, bias, C)
     if workspace is None:
         n = _workspace("gdn_group_norm_forward_workspace", (N, S, C, groups, dt), None)
         workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
@@ -283,7 +306,7 @@ def gdn_group_norm_backward(dy: torch.Tensor, x: torch.Tensor, groups: int,
     if workspace is None:
         workspace = _workspace("gdn_group_norm_backward_workspace", (N, S, C, groups, dt),
                                x.device)
-    wp, bp, wdt = _params(weight, bias, C)
+    wp, bp, wdt = _affine(weight, bias, C)
     _check("gdn_group_norm_backward", lib.gdn_group_norm_backward(
         _dev(dy, "dy", x.dtype, n), _dev(x, "x"), wp, bp, _opt(gate, "gate", x.dtype, n),
         _dev(mean, "mean", f32, N * groups), _dev(rstd, "rstd", f32, N * groups),

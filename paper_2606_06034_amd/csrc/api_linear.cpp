@@ -28,11 +28,10 @@ int set_sizes(gdn::LinArgs& a, const int32_t* cu, bool packed, int nseq, int T, 
   a.q.nseg = a.q.segments(T);
   a.Hk = Hk, a.Hv = Hv, a.dk = dk, a.dv = dv;
   const int64_t slots = a.q.slots();
-  // workgroups of 256 work items: one a segment and head, in the backward pass one for each
-  // gradient, and one a sequence without tokens
-  if (!grid_ok(slots, 256)) return GDN_ERR_SHAPE;
-  if (!grid_ok(slots * Hv + nseq + 16, 256)) return GDN_ERR_SHAPE;
-  if (backward && !grid_ok(slots * (2ll * Hk + Hv) + nseq + 16, 256)) return GDN_ERR_SHAPE;
+  // workgroups of up to 512 work items: one a segment and head, in the backward pass two or
+  // less, one a sequence without tokens, and some left over for each of the 8 XCDs
+  if (!grid_ok(slots, 512)) return GDN_ERR_SHAPE;
+  if (!grid_ok(slots * Hv * (backward ? 2 : 1) + nseq + 16, 512)) return GDN_ERR_SHAPE;
   return GDN_OK;
 }
 
@@ -166,9 +165,11 @@ int gdn_linear_backward(const void* Q, const void* K, const void* V, const float
 }
 
 namespace {
+constexpr int64_t kMostValues = 1ll << 48;  // of a map; no memory holds as many
 int check_group(int64_t N, int S, int C, int G, int dtype) {
   if (N < 0 || N > 0x7fffffffLL || S < 1 || S > 1 << 30 || C < 1 || C > 65536 || G < 1 || C % G)
     return GDN_ERR_SHAPE;
+  if (N > 0 && S > kMostValues / C / N) return GDN_ERR_SHAPE;
   if (!fdtype(dtype)) return GDN_ERR_DTYPE;
   return GDN_OK;
 }

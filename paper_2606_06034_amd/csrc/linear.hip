@@ -505,7 +505,7 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinArgs a, int parts) {
     f32x4 S = from ? *(const f32x4*)(from + (int64_t)sh * size + e) : zero4();
     float* X = (rev ? a.R : a.U) + (base * a.Hv + h) * size + e;
     const float* d = a.dec + base * a.Hv + h;
-    constexpr int A = 8;  // asked for ahead
+    constexpr int A = 16;  // asked for ahead
     for (int i0 = 0; i0 < n; i0 += A) {
       f32x4 x[A];
       float f[A];
@@ -1231,24 +1231,24 @@ int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bo
     const double steps = (double)seg / LC;
     const double slots = packed ? tokens / seg + 0.5 * nseq : std::ceil((double)T / seg) * nseq;
     // steps of `work` walkers on 256 CUs (equal ones in whole rounds; of unlike ones the
-    // last begins late)
-    auto time = [&](double work, double alone, double more, bool whole_rounds) {
+    // last begins late: half a round's more)
+    auto time = [&](double work, double alone, double more, double whole_rounds) {
       double n = work / 256;
       if (packed)
         n *= (tokens / LC + 0.5 * nseq + 0.4 * slots) / (slots * steps);
-      else if (whole_rounds)
-        n = std::ceil(n);
+      else
+        n += whole_rounds * (std::ceil(n) - n);
       const double t = steps * (fp32 ? alone * std::max(1., n) : std::max(alone, more * n));
       return packed ? t + 0.5 * steps * alone : t;
     };
     const double states = slots * Hv;
-    double walk, add = time(backward ? 2 * states : states, 1.2, 0.9, true);
+    double walk, add = time(backward ? 2 * states : states, 1.2, 0.9, 1);
     if (!backward)
-      walk = time(states, 4.6, 3.6, true);
+      walk = time(states, 4.6, 3.6, 1);
     else if (!fp32 && Hk && Hv / Hk % 2 == 0)
-      walk = time(1.5 * states, 12.9, 12.9, false);
+      walk = time(1.5 * states, 11, 11, 0.5);
     else
-      walk = gr * (time(slots * Hk, 12, 12, false) + time(slots * Hk, 6, 4.5, true));
+      walk = gr * (time(slots * Hk, 12, 12, 0) + time(slots * Hk, 6, 4.5, 1));
     double cost = size * (walk + (one ? 0 : add)) + (one ? 4 : 12);
     if (!one) cost += states * (backward ? 0.131 : 0.058) * dk * dv / 16384;
     if (cost < least) least = cost, best = (int)seg;

@@ -110,6 +110,12 @@ def test_workspaces():
         assert f(2 ** 31 - 1, 2 ** 31 - 1, 1, 1, 64, 64, 0, 1, ctypes.byref(n)) == SHAPE
         assert f(1, 100, 1, 1, 64, 64, 0, 2, ctypes.byref(n)) == DTYPE
         assert f(1, 100, 3, 4, 64, 64, 0, 1, ctypes.byref(n)) == SHAPE
+    # launches of 512 work items for each segment and head: 2^32 of them at most, in the backward
+    # pass two workgroups a segment and head
+    for f, most in ((L.gdn_linear_forward_workspace, 1 << 23), (L.gdn_linear_backward_workspace,
+                                                                 1 << 22)):
+        assert f(most // 4 - 8, 1, 2, 4, 64, 64, 0, 1, ctypes.byref(n)) == SHAPE
+        assert f(most // 5 - 8, 1, 2, 4, 64, 64, 0, 1, ctypes.byref(n)) == OK
     with pytest.raises(G.GdnError):
         G.gdn_linear_backward_workspace(2, 100, 3, 3, 96, 128)
 
@@ -118,7 +124,7 @@ GN = dict(x=P[0], w=P[1], b=P[2], z=P[3], y=P[4], mean=P[5], rstd=P[6], ws=P[7],
           S=100, C=96, G=8, eps=1e-6, act=1, dtype=1, wdt=0, stream=None)
 GROUP = [
     (dict(N=-1), SHAPE), (dict(N=1 << 31), SHAPE), (dict(S=0), SHAPE), (dict(S=(1 << 30) + 1), SHAPE),
-    (dict(C=0), SHAPE), (dict(C=65544), SHAPE), (dict(G=0), SHAPE), (dict(G=7), SHAPE),
+    (dict(N=1 << 20, S=1 << 20, C=512), SHAPE), (dict(C=0), SHAPE), (dict(C=65544), SHAPE), (dict(G=0), SHAPE), (dict(G=7), SHAPE),
     (dict(G=-8), SHAPE), (dict(act=2), PARAM), (dict(act=-1), PARAM), (dict(dtype=2), DTYPE),
     (dict(wdt=2), DTYPE)]
 
