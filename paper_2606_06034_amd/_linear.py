@@ -49,11 +49,15 @@ _device = _layer._device or torch.cuda.current_device
 
 def _dev(t: torch.Tensor, name: str, dtype=None, numel: Optional[int] = None) -> int:
     """Address of a tensor of the current device, where the launches go."""
-    p = _layer._dev(t, name, dtype, numel)
-    if t.get_device() != _device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device (cuda:{_device()}): "
-                         f"call under torch.cuda.device(), or name a stream of {t.device}")
-    return p
+    try:
+        if (t.is_cuda and t.get_device() == _device() and t.is_contiguous() and
+                (dtype is None or t.dtype is dtype) and (numel is None or t.numel() == numel)):
+            return t.data_ptr()
+    except AttributeError:  # not a tensor
+        pass
+    _layer._dev(t, name, dtype, numel)
+    raise ValueError(f"{name} is on {t.device}, not on the current device (cuda:{_device()}): "
+                     f"call under torch.cuda.device(), or name a stream of {t.device}")
 
 
 def _opt(t: Optional[torch.Tensor], name: str, dtype=None, numel: Optional[int] = None):
