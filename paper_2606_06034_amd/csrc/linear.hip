@@ -505,14 +505,14 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinArgs a, int parts) {
     f32x4 S = from ? *(const f32x4*)(from + (int64_t)sh * size + e) : zero4();
     float* X = (rev ? a.R : a.U) + (base * a.Hv + h) * size + e;
     const float* d = a.dec + base * a.Hv + h;
-    constexpr int A = 16;  // asked for ahead
+    constexpr int A = 8;  // asked for ahead
     for (int i0 = 0; i0 < n; i0 += A) {
       f32x4 x[A];
       float f[A];
 #pragma unroll
       for (int u = 0; u < A; ++u) {
-        const int i = min(i0 + u, n - 2), j = rev ? n - 1 - i : i;
-        if (n > 1) {
+        const int i = i0 + u, j = rev ? n - 1 - i : i;
+        if (i + 1 < n) {
           x[u] = *(const f32x4*)(X + j * step);
           f[u] = d[(int64_t)j * a.Hv];
         }
