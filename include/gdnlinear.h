@@ -44,15 +44,16 @@ extern "C" {
  * rows of all heads of 64 tokens (of T where that is less) of Q and of V hold
  * 4 GiB at most.
  * With bf16 inputs the states, and the products q . k under the decay, enter
- * the outputs as sums of two bf16 terms (2^-16 of each) and the values under
- * the decay the states as sums of three (2^-24).
+ * the outputs as sums of two bf16 terms (2^-16 of each), and the values under
+ * the decay the states as sums of three (2^-24), of two where only outputs
+ * take the state up.
  * A value that is not finite makes what it reaches not finite either (an
  * infinity NaN), and may do so to other tokens of its 64, counted from the
  * sequence's first; it reaches no other sequence and no other value head that
  * does not read it.
  * workspace: at least gdn_linear_forward_workspace() bytes (may be NULL where
- * that is 0), contents undefined on return.  One launch, or three for long
- * sequences of few heads. */
+ * that is 0), contents undefined on return.  One launch, or three where a
+ * sequence is cut into segments. */
 int gdn_linear_forward(const void* Q, const void* K, const void* V, const float* g,
                        int g_per_token, const float* S0, void* O, float* S_final, void* workspace,
                        int64_t workspace_bytes, const int32_t* cu_seqlens, int nseq, int T, int Hk,
@@ -111,9 +112,11 @@ enum gdn_act { GDN_ACT_NONE = 0, GDN_ACT_SILU = 1 };
  * nullable: what the backward pass takes.  Statistics and products are fp32; y
  * rounds once.  One group a head and S = 1 is the norm of a layer's heads with
  * weights of their own.
- * 0 <= N < 2^31, 1 <= S <= 2^30, 1 <= C <= 65536, any sizes and row alignment;
- * groups that are read twice (those of over 8192 pieces of 16 bytes or less, in
- * the backward pass those of S > 1): N times their parts below 2^24.
+ * 0 <= N < 2^31, 1 <= S <= 2^30, 1 <= C <= 65536, N S C <= 2^48, any sizes and
+ * row alignment.  Groups of more than 256 pieces (of 16 bytes; of a value or two
+ * where a group's channels do not fill such pieces), of more than 1024 where
+ * S = 1, and in the backward pass all with S > 1, are read twice: up to 2^24
+ * workgroups, one for every 256 pieces of the C channels and each n.
  * workspace: at least gdn_group_norm_forward_workspace() bytes (may be NULL
  * where that is 0). */
 int gdn_group_norm_forward(const void* x, const void* w, const void* b, const void* z, void* y,
