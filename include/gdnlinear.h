@@ -50,7 +50,9 @@ extern "C" {
  * A value that is not finite makes what it reaches not finite either (an
  * infinity NaN), and may do so to other tokens of its 64, counted from the
  * sequence's first; it reaches no other sequence and no other value head that
- * does not read it.
+ * does not read it.  A token reaches those after it as far as the decay between
+ * them is not 0 in fp32 (e^-104); whether a value that is not finite reaches
+ * further is not defined.
  * workspace: at least gdn_linear_forward_workspace() bytes (may be NULL where
  * that is 0), contents undefined on return.  One launch, or three where a
  * sequence is cut into segments. */
@@ -71,6 +73,7 @@ int gdn_linear_forward_workspace(int nseq, int T, int Hk, int Hv, int dk, int dv
  * over its group of value heads, those of a head's decay over all its tokens.
  * Everything is formed in fp32 or sums of bf16 terms that make it up and
  * rounded once at the end, in a fixed order: the same call gives the same bits.
+ * The rows of all heads of 64 tokens hold 2^30 values at most.
  * A value that is not finite reaches what it does in the forward pass, and
  * through dQ and dK the key head's other gradients; dg of a token reaches from
  * the tokens after it.

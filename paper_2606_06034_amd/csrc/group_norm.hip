@@ -12,6 +12,9 @@
 // of parts of the positions first, then the results.  A thread has V neighbouring channels
 // of one group all along, so that its weights and its sums of dw and db stay in registers.
 // Everything is added up in a fixed order (no atomics: the same call gives the same bits).
+// (8192 rows of 32 groups of 128 with a gate, bf16: 36.6 us, 5.5 TB/s; gradients 67 and 4 us,
+// 5.1 TB/s.  4 x 4096 positions of 32 groups of 16, SiLU: 8 us for the sums, 12 for the
+// results.  Gradients of 3 x 3001 positions of 8 groups of 41, fp32, a value a load: 10 and 14.)
 #include <algorithm>
 
 #include "group_norm.hpp"
@@ -664,7 +667,7 @@ int vec_of(int Cg, int dtype) {
 
 // pieces a thread holds, threads of a workgroup and of a group; 0 where a group is read twice.
 // (4 x 4096 positions of 32 groups of 16 channels in bf16, the groups in registers of 1024
-// threads, 32 bytes of a position each: 45 us, read twice 17.)
+// threads, 32 bytes of a position each: 45 us, read twice 20.)
 struct RowShape { int nv, b, tpi; };
 RowShape row_shape(int64_t pieces, int S, bool grad) {
   if (grad && S > 1) return {0, 0, 0};

@@ -25,7 +25,15 @@
 // k_lin_scan carries the states over the segments, k_lin_forward / k_lin_backward walk.
 //
 // Precision.  bf16 inputs are exact operands of the matrix instructions; fp32 factors
-// (states, decayed values, P) enter as sums of bf16 terms (split.hpp).
+// (states, decayed values, P) enter as sums of bf16 terms (split.hpp): two, 2^-16 of each, for
+// what goes into bf16 outputs alone, three, 2^-24, for states and dg, which are fp32 results.
+// fp32 inputs go to the fp32 matrix instructions.
+//
+// Bound: a pass's tiles are read once and take 3 TB/s; the rest is the serial step of a chunk,
+// products of at most 128 x 128 x 64 with the splits between them.  A step takes 4.3 us with
+// one workgroup of 256 a CU and 3.6 each with two, 11 with two teams of a gradient.  (8192 tokens,
+// 16 heads: states 22 us, their carry 8, walk 48; gradients: states 34, carry 12, dQ 64,
+// dK and dV 89, dg 10.)
 #include <algorithm>
 #include <cmath>
 
@@ -53,6 +61,9 @@ template <> struct FragFor<__bf16> { typedef bf16x4 type; };
 // Terms of states and of P where they go into outputs in bf16 alone.  (One would add as much
 // again to the outputs' own rounding.)
 constexpr int kOut = 2;
+// Blocks of 16 value columns a wave has, of 128 columns: eight waves form a segment's state (as
+// many loads in flight as there can be), four walk (16 heads of 8192 tokens: 48 us, 47 with
+// eight waves, which take twice the LDS reads of P and leave no room for a second workgroup).
 constexpr int kStateBlocks = 1, kWalkBlocks = 2;
 constexpr int kMostChunks = 16;  // of a segment of the backward pass
 
@@ -418,8 +429,8 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
     v.template load<REV>(V + (int64_t)at * ldv, ldv, m, threadIdx.x);
   };
   // From the last chunk to the first, each decayed past those after it, so that nothing is
-  // scaled again; and no further than to where nothing is left of a value (2^-160 of it: fp32
-  // has none below 2^-149).
+  // scaled again; and no further than to where the decay is 0 as a factor in fp32 (2^-160:
+  // below 2^-149 there is none).
   constexpr double kNothing = -160.0;
   double total = 0.0;  // of the chunks so far: the first wave's
   auto gates = [&](int i, float g) __attribute__((always_inline)) {
@@ -486,7 +497,10 @@ __global__ __launch_bounds__(4 * DV / NS) void k_lin_state(const LinArgs a, uint
 }
 
 // The states carried over the segments of each sequence, in place: U from what a segment
-// adds to the state that enters it, R to the gradient of the state that leaves it.
+// adds to the state that enters it, R to the gradient of the state that leaves it.  Bound: HBM
+// where there are many (4 x 8192 tokens of 32 heads, both: 246 MB in 41 us), else the chain of
+// loads, eight asked for ahead: 22 us for 16384 packed tokens of 16 heads, in sequences of six
+// segments, 28 with sixteen; 7.5 either way for 8192 in one.
 __global__ __launch_bounds__(256) void k_lin_scan(const LinArgs a, int parts) {
   const bool rev = blockIdx.y;
   const int64_t size = (int64_t)a.dk * a.dv, step = a.Hv * size;
@@ -1036,7 +1050,8 @@ __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segm
 
 }  // namespace
 
-// groups of even size
+// groups of even size.  (4 x 8192 tokens, 32 heads in pairs: 0.97 to 1.1 ms, 3 TB/s, vector units
+// busy 44 % and matrix units 28 %.)
 template <int DK, int DV, typename T, int TS, int TO, int TP, bool DG>
 __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a, uint32_t slots) {
   // the second team's results go where the tiles of products lie, which the first has done with
@@ -1077,7 +1092,8 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a,
   }
 }
 
-// dK and dV of a key head's value heads one after the other
+// dK and dV of a key head's value heads one after the other.  (8192 tokens of 16 heads: 89 us,
+// 2.7 TB/s, vector units busy 40 % and matrix units 26 %.)
 template <int DK, int DV, typename T, int TS, int TO, int TP, bool DG>
 __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uint32_t slots) {
   constexpr int KT = LC * DK, VT = LC * DV;
@@ -1155,7 +1171,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(co
   }
 }
 
-// ---- the gradient of g from the rows' sums; a wave takes a chunk
+// ---- the gradient of g from the rows' sums; a wave takes a chunk.  (18 us for 4 x 8192 tokens of
+// 32 heads, one value a head and token written in each line of 128 bytes; 6 and 4 for the sums of
+// a head's decay over 8192 tokens of 16.)
 __global__ __launch_bounds__(256) void k_lin_decay(const LinArgs a) {
   __shared__ float sq[kMostChunks], sk[kMostChunks], wave[4];
   const uint32_t slot = blockIdx.x / (uint32_t)a.Hv;
@@ -1213,9 +1231,11 @@ __global__ __launch_bounds__(256) void k_lin_decay_sum(const LinArgs a, int64_t 
 // written, carried over the segments and read: 4 times 64 KB, 9 in the backward pass): the one
 // of least time by what the launches took, in us, for heads of 128 by 128 in bf16.  A step
 // of a walk, of 64 tokens, takes 4.6 with one workgroup a CU and 3.6 each with two, forming
-// a segment's state 1.2 and 0.9; 12 to 13 a step of two teams, one workgroup a CU; with fp32
-// inputs 3.8 times as long.  (16 heads of 8192 tokens, forward: 103 us in segments of 128, 78
-// of 256 and 512, 94 of 768, 160 of 1536; 4 of 1000: 25 of 128, 36 of 256, 75 in one.)
+// a segment's state 1.2 and 0.9; 11 to 12 a step of two teams, one workgroup a CU; with fp32
+// inputs 3.8 times as long.  (Forward, 16 heads of 8192 tokens: 135 us in segments of 64, 96 of
+// 128, 73 of 256, 71 of 512, 92 of 768, 161 of 1536; 4 of 1000: 23 of 64, 25 of 128, 36 of 256, 73
+// in one, in fp32 35, 49, 85 and 222.  Gradients, 16 heads of 8192: 440 of 64, 215 of 256, 192 of
+// 512, 299 of 1024; 32 of 2 x 8192 with 16 key heads: 821 of 256, 692 of 512, 634 of 1024.)
 int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bool backward,
                 bool fp32) {
   const double tokens = packed ? (double)T : (double)nseq * T, gr = Hk ? (double)Hv / Hk : 1;

@@ -6,7 +6,8 @@
 // in registers, with no exchange between waves: lane l holds dk NCOL / 256 rows of 4 columns,
 // and the sums over the rows end in exchanges between lanes.
 //
-// Bound: HBM, the state is read and written once a call, 8 bytes for 5 flops a token.
+// Bound: HBM, the state is read and written once a call, 8 bytes for 5 flops a token: 198 us
+// for 256 sequences of 32 heads of 128 x 128, 5.4 TB/s; 4.5 us for one of 16.
 #include "lanes.hpp"
 #include "launch.hpp"
 #include "linear.hpp"

@@ -84,7 +84,10 @@ BWD = dict(Q=P[0], K=P[1], V=P[2], g=P[3], per_token=1, dO=P[5], S0=P[6], dSf=P[
     (dict(dS0=P[12] + 4), ALIGN), (dict(cu=P[14] + 4), ALIGN), (dict(dQ=P[0]), ALIAS),
     (dict(dK=P[8]), ALIAS), (dict(dS0=P[7]), ALIAS), (dict(dS0=P[6]), ALIAS),
     (dict(dg=P[3]), ALIAS), (dict(ws=P[2]), ALIAS), (dict(nseq=0), OK),
-    (dict(nseq=0, per_token=0, dg=None), OK)])
+    (dict(nseq=0, per_token=0, dg=None), OK),
+    # sums over a group's heads are fp32: 32 * 2^18 * 128 * 4 bytes are 4 GiB
+    (dict(Hk=(1 << 18) + 1, Hv=(1 << 19) + 2, dv=64, nseq=1, T=32), SHAPE),
+    (dict(Hk=1 << 18, Hv=1 << 19, dv=64, nseq=1, T=32, Q=None), NULL)])
 def test_backward_refusals(change, code):
     assert call(L.gdn_linear_backward, BWD, **change) == code
 
