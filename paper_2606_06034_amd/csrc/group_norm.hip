@@ -222,11 +222,20 @@ __global__ __launch_bounds__(256) void k_gn_rows(const GroupArgs a) {
   }
 }
 
+// the largest power of two below n (0 for one)
+__host__ __device__ inline int half_of(int n) {
+  int h = 0;
+  for (int p = 1; p < n; p *= 2) h = p;
+  return h;
+}
+// most n's whose sums lie in LDS at once
+inline int of_sums(int nw) { return std::max(nw - half_of(nw), half_of(nw) / 2); }
+
 // The gradients where S = 1.  The n's that run side by side add up their dw and db in LDS, the
 // workgroups' sums go to row nb of the workspace: [parts][C], then the same for db.
 template <typename T, int V, int NV, int B, int OPS>
 __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts) {
-  extern __shared__ float lds[];  // 64 values of the sums, then [2][gw Cg]
+  extern __shared__ float lds[];  // 64 values of the sums, then [of_sums][2][gw Cg]
   Sums sums{lds, 0, a.tpi};
   const int slot = (int)threadIdx.x / a.tpi, t = (int)threadIdx.x - slot * a.tpi;
   const int blocks = a.G / a.gw, gb = (int)(blockIdx.x % blocks), nb = (int)(blockIdx.x / blocks);
@@ -310,7 +319,7 @@ __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts
   float* sum = lds + 64;
   const int width = a.gw * a.Cg;
   float* to = a.ws + (int64_t)nb * a.C + (int64_t)gb * width;
-  if (a.nw == 1) {  // the sums are whole
+  auto write = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (at[k] >= 0)
@@ -319,25 +328,28 @@ __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts
           to[at[k] - gb * width + i] = dw[k][i];
           to[(int64_t)parts * a.C + at[k] - gb * width + i] = db[k][i];
         }
-    return;
-  }
-  for (int r = 0; r < a.nw; ++r) {
-    if (mine && ni == r)
+  };
+  // halves of the n's onto each other (one after the other, 128 n's of a small group took 40 us)
+  for (int half = half_of(a.nw); half > 0; half /= 2) {
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (at[k] >= 0)
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const int c = at[k] - gb * width + i;
-            sum[c] = r ? sum[c] + dw[k][i] : dw[k][i];
-            sum[width + c] = r ? sum[width + c] + db[k][i] : db[k][i];
-          }
+          for (int i = 0; i < V; ++i) f(at[k] - gb * width + i, dw[k][i], db[k][i]);
+    };
+    if (mine && ni >= half && ni < 2 * half) {
+      float* x = sum + (ni - half) * 2 * width;
+      each([&](int c, float& u, float& v) { x[c] = u, x[width + c] = v; });
+    }
+    __syncthreads();
+    if (mine && ni < half && ni + half < a.nw) {
+      const float* x = sum + ni * 2 * width;
+      each([&](int c, float& u, float& v) { u += x[c], v += x[width + c]; });
+    }
     __syncthreads();
   }
-  for (int c = threadIdx.x; c < width; c += B) {
-    to[c] = sum[c];
-    to[(int64_t)parts * a.C + c] = sum[width + c];
-  }
+  if (mine && ni == 0) write();
 }
 
 // ---- groups read twice.  A workgroup has the positions s0 .. s1 of one n and a block of
@@ -784,7 +796,7 @@ static hipError_t group_backward(GroupArgs a, hipStream_t st) {
   if (a.N > 0) {
     parts = row_parts(a, r, true);
     const dim3 grid((unsigned)(parts * (a.G / a.gw)));
-    const size_t lds = (64 + (a.nw > 1 ? 2 * (size_t)a.gw * a.Cg : 0)) * sizeof(float);
+    const size_t lds = (64 + (a.nw > 1 ? of_sums(a.nw) * 2 * (size_t)a.gw * a.Cg : 0)) * sizeof(float);
     if (r.nv == 1)
       hipLaunchKernelGGL((k_gn_rows_grad<T, V, 1, 1024, OPS>), grid, dim3(1024), lds, st, a, (int)parts);
     else if (r.nv == 2)
