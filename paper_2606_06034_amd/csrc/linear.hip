@@ -1235,7 +1235,10 @@ __global__ __launch_bounds__(256) void k_lin_decay_sum(const LinArgs a, int64_t 
 // inputs 3.8 times as long.  (Forward, 16 heads of 8192 tokens: 135 us in segments of 64, 96 of
 // 128, 73 of 256, 71 of 512, 92 of 768, 161 of 1536; 4 of 1000: 23 of 64, 25 of 128, 36 of 256, 73
 // in one, in fp32 35, 49, 85 and 222.  Gradients, 16 heads of 8192: 440 of 64, 215 of 256, 192 of
-// 512, 299 of 1024; 32 of 2 x 8192 with 16 key heads: 821 of 256, 692 of 512, 634 of 1024.)
+// 512, 299 of 1024; 32 of 2 x 8192 with 16 key heads: 821 of 256, 692 of 512, 634 of 1024.  Packed,
+// 16384 tokens in 31 sequences, 16 heads: forward 318, 214, 170, 181, 182 of 64, 128, 256, 512, 1024;
+// gradients, 8 key heads: 966, 626, 505, 481, 563.  Over nine packed mixes the segments chosen
+// take 4 % more than the best ones, 1 % for the gradients.)
 int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bool backward,
                 bool fp32) {
   const double tokens = packed ? (double)T : (double)nseq * T, gr = Hk ? (double)Hv / Hk : 1;
@@ -1250,25 +1253,28 @@ int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bo
     if (one) seg = std::max<int64_t>(whole, LC);
     const double steps = (double)seg / LC;
     const double slots = packed ? tokens / seg + 0.5 * nseq : std::ceil((double)T / seg) * nseq;
-    // steps of `work` walkers on 256 CUs (equal ones in whole rounds; of unlike ones the
-    // last begins late: half a round's more)
-    auto time = [&](double work, double alone, double more, double whole_rounds) {
+    // steps of `work` walkers on 256 CUs, `places` on each (equal ones in whole rounds; of unlike
+    // ones the last begins late: half a round's more).  Packed sequences' segments are of all
+    // lengths, some slots empty: the steps there are, and what begins late.
+    auto time = [&](double work, double alone, double more, double whole_rounds, int places) {
       double n = work / 256;
-      if (packed)
-        n *= (tokens / LC + 0.5 * nseq + 0.4 * slots) / (slots * steps);
-      else
+      if (packed) {
+        n *= (tokens / LC + 0.5 * nseq + 0.8 * slots) / (slots * steps);
+        n += 0.5 * (std::ceil(n / places) * places - n);
+      } else {
         n += whole_rounds * (std::ceil(n) - n);
+      }
       const double t = steps * (fp32 ? alone * std::max(1., n) : std::max(alone, more * n));
-      return packed ? t + 0.5 * steps * alone : t;
+      return packed ? t + (backward ? 0.25 : 2) * steps * alone : t;
     };
     const double states = slots * Hv;
-    double walk, add = time(backward ? 2 * states : states, 1.2, 0.9, 1);
+    double walk, add = time(backward ? 2 * states : states, 1.2, 0.9, 1, 2);
     if (!backward)
-      walk = time(states, 4.6, 3.6, 1);
+      walk = time(states, 4.6, 3.6, 1, 2);
     else if (!fp32 && Hk && Hv / Hk % 2 == 0)
-      walk = time(1.5 * states, 11, 11, 0.5);
+      walk = time(1.5 * states, 11, 11, 0.5, 1);
     else
-      walk = gr * (time(slots * Hk, 12, 12, 0) + time(slots * Hk, 6, 4.5, 1));
+      walk = gr * (time(slots * Hk, 12, 12, 0, 1) + time(slots * Hk, 6, 4.5, 1, 2));
     double cost = size * (walk + (one ? 0 : add)) + (one ? 4 : 12);
     if (!one) cost += states * (backward ? 0.131 : 0.058) * dk * dv / 16384;
     if (cost < least) least = cost, best = (int)seg;
