@@ -571,8 +571,8 @@ struct TeamLds {
   T p[6 * kTerms<typename FragFor<T>::type, TP> * 512];
   float far[NW][LC];             // the waves' shares of x . (what came from the state)
   float row[4][LC], col[4][LC];  // sums of M's blocks (I, J): along rows at J, down columns at I
-  float part[NW];
   Gates gt[2];
+  double part[NW];
 };
 
 // The tiles of a workgroup, from where they come to LDS, and the passes that read them.
@@ -656,8 +656,8 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     tiles.store(m, anew(threadIdx.x));
     write_rows(i - 1);
     lds_only_barrier();
-    if (pairs && end) {
-      float x = 0.f;
+    if (pairs && end) {  // (in 64 bits: dk dv products of any sign)
+      double x = 0.0;
       if (ps.against) {
 #pragma unroll
         for (int u = 0; u < 2 * NQ; ++u)
@@ -665,9 +665,9 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
           for (int n = 0; n < NS; ++n) {
             const f32x4 y = StateOf<DK, DV, NS>::block(ps.against, flip, u, n, w, ln);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x = __builtin_fmaf(S.b[u][n][e], y[e], x);
+            for (int e = 0; e < 4; ++e) x = __builtin_fma((double)S.b[u][n][e], (double)y[e], x);
           }
-        x = sum_lanes<64>(x);
+        x = lane63(prefix64(x));
       }
       if (ln.id == 0) lds->part[w] = x;
     }
@@ -823,10 +823,10 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     S.template update<TS>(sk, sv, gt, w, ln);
     lds_only_barrier();
     if (pairs && end && w == 0 && ln.id == 0) {
-      float x = 0.f;
+      double x = 0.0;
 #pragma unroll
       for (int u = 0; u < NW; ++u) x += lds->part[u];
-      *ps.anchor = gt->el * x;
+      *ps.anchor = (float)(gt->el * x);
     }
     // and from the chunk's tokens
 #pragma unroll

@@ -396,3 +396,18 @@ def test_some_gradients_alone():
         assert np.allclose(f64(p), f64(q), rtol=2.0 ** -7, atol=1e-4 * float(q.abs().max()))
     assert np.allclose(f64(one[3]), f64(each[3]).sum((0, 1)), rtol=1e-4,
                        atol=1e-5 * float(each[3].abs().sum()))
+
+
+def test_the_decay_of_one_token():
+    """Its gradient is e^g <S0, dS> where dO is 0: a sum of dk dv products that cancel to a
+    hundredth, taken in 64 bits; e^g, its product and the results' sums are 8 roundings at most."""
+    x = make([1, 1], 4, 32, 128, 128, "bf16", True, True, 19, False)
+    x["dO"].zero_()
+    for odd in (False, True):  # groups of eight, and of one
+        a = [x[k] for k in ("Q", "K", "V", "g", "dO")]
+        S0, dS = x["S0"], x["dS"]
+        if odd:
+            a[0], a[1] = (t.repeat_interleave(8, 2).contiguous() for t in a[:2])
+        dg = G.gdn_linear_backward(*a, S0=S0, dS_final=dS)[3]
+        ref = np.exp(f64(x["g"])) * (f64(S0) * f64(dS)).sum((2, 3))[:, None]
+        assert (np.abs(f64(dg) - ref) <= 8 * 2.0 ** -24 * np.abs(ref)).all()
