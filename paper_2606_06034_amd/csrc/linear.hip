@@ -1272,7 +1272,7 @@ int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bo
     if (!backward)
       walk = time(states, 4.6, 3.6, 1, 2);
     else if (!fp32 && Hk && Hv / Hk % 2 == 0)
-      walk = time(1.5 * states, 11, 11, 0.5, 1);
+      walk = time(1.5 * states, 5.5 * gr, 11, 0.5, 1);  // (a group's pairs one after the other)
     else
       walk = gr * (time(slots * Hk, 12, 12, 0, 1) + time(slots * Hk, 6, 4.5, 1, 2));
     double cost = size * (walk + (one ? 0 : add)) + (one ? 4 : 12);
