@@ -499,8 +499,8 @@ __global__ __launch_bounds__(4 * DV / NS) void k_lin_state(const LinArgs a, uint
 // The states carried over the segments of each sequence, in place: U from what a segment
 // adds to the state that enters it, R to the gradient of the state that leaves it.  Bound: HBM
 // where there are many (4 x 8192 tokens of 32 heads, both: 246 MB in 41 us), else the chain of
-// loads, eight asked for ahead: 22 us for 16384 packed tokens of 16 heads, in sequences of six
-// segments, 28 with sixteen; 7.5 either way for 8192 in one.
+// loads, eight asked for ahead: 22 us for 16384 packed tokens of 16 heads in segments of 512, 28
+// with sixteen (34 in segments of 256); 7.5 either way for 8192 in one.
 __global__ __launch_bounds__(256) void k_lin_scan(const LinArgs a, int parts) {
   const bool rev = blockIdx.y;
   const int64_t size = (int64_t)a.dk * a.dv, step = a.Hv * size;
