@@ -280,7 +280,8 @@ __global__ __launch_bounds__(B) void k_gn_rows_grad(const GroupArgs a, int parts
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         h[k][i] = ((float)r.x[k][i] - r.mean) * r.rstd;
-        dn[k][i] = grad<OPS>(h[k][i], w[k][i], b[k][i], OPS & kGate ? r.z[k][i] : 0.f, r.dy[k][i], dz[i]);
+        dn[k][i] = grad<OPS>(h[k][i], w[k][i], b[k][i], OPS & kGate ? r.z[k][i] : 0.f, r.dy[k][i],
+                             dz[i]);
         const float dh = at[k] >= 0 ? dn[k][i] * w[k][i] : 0.f;
         s1 += dh;
         s2 += at[k] >= 0 ? dh * h[k][i] : 0.f;
@@ -704,10 +705,11 @@ int row_parts(GroupArgs& a, const RowShape& r, bool grad) {
 // groups read twice: column blocks, and parts of the positions
 void tile_parts(GroupArgs& a, int V) {
   const int64_t pr = a.Cg / V;
-  a.cblocks = pr <= 256 ? (int)((a.G + 256 / pr - 1) / (256 / pr)) : (int)(a.G * ((pr + 255) / 256));
-  const int step = pr <= 256 ? (int)std::max<int64_t>(1, 256 / (pr * std::min<int64_t>(a.G, 256 / pr))) : 1;
+  a.cblocks = (int)(pr <= 256 ? (a.G + 256 / pr - 1) / (256 / pr) : a.G * ((pr + 255) / 256));
+  const int64_t cols = pr <= 256 ? pr * std::min<int64_t>(a.G, 256 / pr) : 256;
+  const int64_t step = std::max<int64_t>(1, 256 / cols);
   const int64_t want = std::max<int64_t>(1, 768 / std::max<int64_t>(1, a.N * a.cblocks));
-  const int64_t most = std::max<int64_t>(1, a.S / (8ll * step));  // eight positions a thread
+  const int64_t most = std::max<int64_t>(1, a.S / (8 * step));  // eight positions a thread
   a.sparts = (int)std::min<int64_t>(std::min(want, most), 256);
 }
 

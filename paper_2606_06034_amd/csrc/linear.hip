@@ -435,7 +435,8 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
   double total = 0.0;  // of the chunks so far: the first wave's
   auto gates = [&](int i, float g) __attribute__((always_inline)) {
     if (w != 0) return;
-    total += form_gates(gt + (i & 1), g, a.per_token, ch.size(i), rev, 1.f, rev ? a.scale : 1.f, total);
+    total += form_gates(gt + (i & 1), g, a.per_token, ch.size(i), rev, 1.f, rev ? a.scale : 1.f,
+                        total);
     if (ln.id == 0) gt[i & 1].sum = total;
   };
   auto decay_of = [&](int i) __attribute__((always_inline)) {
@@ -742,7 +743,8 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
     static_assert(NW >= 4, "two blocks a wave and two over");
     {
       const int b1 = w + NW < 10 ? w + NW : w;  // (of eight waves six repeat their block)
-      const int I0 = row_of(w), J0 = w - I0 * (I0 + 1) / 2, I1 = row_of(b1), J1 = b1 - I1 * (I1 + 1) / 2;
+      const int I0 = row_of(w), J0 = w - I0 * (I0 + 1) / 2;
+      const int I1 = row_of(b1), J1 = b1 - I1 * (I1 + 1) / 2;
       const f32x4 p0 = products(I0, J0), p1 = products(I1, J1);
       f32x4 y0 = zero4(), y1 = zero4();
       if constexpr (pairs) y0 = more_products(I0, J0), y1 = more_products(I1, J1);
@@ -892,9 +894,13 @@ struct PassTiles {
   Source<DK, NT, T> q, k;
   Source<DV, NT, T> v;
   template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
-    q.template fetch<REV>(at, m, t), k.template fetch<REV>(at, m, t), v.template fetch<REV>(at, m, t);
+    q.template fetch<REV>(at, m, t);
+    k.template fetch<REV>(at, m, t);
+    v.template fetch<REV>(at, m, t);
   }
-  __device__ __forceinline__ void store(int m, int t) const { q.store(m, t), k.store(m, t), v.store(m, t); }
+  __device__ __forceinline__ void store(int m, int t) const {
+    q.store(m, t), k.store(m, t), v.store(m, t);
+  }
 };
 // Two of one kind each: of DA and of DB values a row.
 template <int DA, int DB, int NT, typename T>
@@ -902,7 +908,8 @@ struct TwoAndTwo {
   Source<DA, NT, T> a0, a1;
   Source<DB, NT, T> b0, b1;
   template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
-    a0.template fetch<REV>(at, m, t), a1.template fetch<REV>(at, m, t), b0.template fetch<REV>(at, m, t), b1.template fetch<REV>(at, m, t);
+    a0.template fetch<REV>(at, m, t), a1.template fetch<REV>(at, m, t);
+    b0.template fetch<REV>(at, m, t), b1.template fetch<REV>(at, m, t);
   }
   __device__ __forceinline__ void store(int m, int t) const {
     a0.store(m, t), a1.store(m, t), b0.store(m, t), b1.store(m, t);
@@ -914,7 +921,8 @@ struct FourAndMore {
   Source<DA, NT, T> a0, a1, a2, a3;
   Source<DB, NT, T> b0, b1;
   template <bool REV> __device__ __forceinline__ void fetch(int at, int m, int t) {
-    a0.template fetch<REV>(at, m, t), a1.template fetch<REV>(at, m, t), a2.template fetch<REV>(at, m, t), a3.template fetch<REV>(at, m, t);
+    a0.template fetch<REV>(at, m, t), a1.template fetch<REV>(at, m, t);
+    a2.template fetch<REV>(at, m, t), a3.template fetch<REV>(at, m, t);
     b0.template fetch<REV>(at, m, t);
     if (MORE) b1.template fetch<REV>(at, m, t);
   }
@@ -1043,7 +1051,8 @@ __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segm
     if (more) ps.x = s + 4 * VT + KT;
     ps.acc = gr > 2 ? (rev ? a.acc_k : a.acc_q) + tk : nullptr;
     ps.first = u == 0, ps.last = u == gr - 2;
-    walk<DV, DK, DK / 64, T, DG ? TS : TO, TO, TP, P, DG, more>(a, sg, h + team, ps, tiles, lds + team, other);
+    walk<DV, DK, DK / 64, T, DG ? TS : TO, TO, TP, P, DG, more>(a, sg, h + team, ps, tiles,
+                                                                lds + team, other);
     lds_only_barrier();
   }
 }
@@ -1085,7 +1094,8 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a,
     Pass ps = value_pass<DK, DV, T>(a, sg, slot, h + team);
     ps.q = s, ps.k = s + KT, ps.v = s + 2 * KT + team * VT;
     if (sg.j == 0)
-      walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles, lds + team);
+      walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles,
+                                                               lds + team);
     else
       walk<DK, DV, DV / 64, T, kOut, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles,
                                                                  lds + team);
