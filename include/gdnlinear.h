@@ -33,7 +33,8 @@ extern "C" {
  * as empty, whichever of the sequences it is, and tokens outside every sequence
  * get no output.  Offsets within range have to be non-decreasing: nothing
  * outside the arrays is touched where they are not, but the results are
- * undefined.
+ * undefined.  Without sequences (nseq = 0) nothing is read, and nothing is
+ * written but the gradients of the heads' decays, 0.
  *
  * dk, dv in {64, 128}; dtype GDN_F32 or GDN_BF16; T >= 0.  Sums, states and
  * decays are fp32 (the sums of g 64-bit) whatever the dtype, O rounds once. */

@@ -95,7 +95,7 @@ int gdn_linear_forward(const void* Q, const void* K, const void* V, const float*
     return r;
   if (!rows_fit(T, Hk, Hv, dk, dv, dtype)) return GDN_ERR_SHAPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
-  const int64_t tok = cu_seqlens ? (int64_t)T : (int64_t)nseq * T, es = esize(dtype);
+  const int64_t tok = a.q.tokens(), es = esize(dtype);
   int64_t need = 4 * gdn::lin_workspace(a, false, nullptr);
   if (tok > 0) {
     if (!Q || !K || !V || !g || !O || (need && !workspace)) return GDN_ERR_NULL;
@@ -140,7 +140,7 @@ int gdn_linear_backward(const void* Q, const void* K, const void* V, const float
     return r;
   if (!rows_fit(T, Hk, Hv, dk, dv, GDN_F32)) return GDN_ERR_SHAPE;
   if (Hv == 0 || (nseq == 0 && (g_per_token || !dg))) return GDN_OK;
-  const int64_t tok = cu_seqlens ? (int64_t)T : (int64_t)nseq * T, es = esize(dtype);
+  const int64_t tok = a.q.tokens(), es = esize(dtype);
   a.per_token = g_per_token != 0, a.want_dg = dg != nullptr, a.scale = scale;
   int64_t need = 4 * gdn::lin_workspace(a, true, nullptr);
   if (tok > 0) {

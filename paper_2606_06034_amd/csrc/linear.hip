@@ -1005,7 +1005,7 @@ __device__ __forceinline__ Pass key_pass(const LinArgs& a, const Segment& sg, ui
   ps.out = (T*)(rev ? a.dK : a.dQ) + tk;
   ps.start = !rev ? S : a.R ? a.R + at : a.dSf ? a.dSf + own : nullptr;
   if (DG) {
-    const int64_t tokens = a.q.cu ? (int64_t)a.q.T : (int64_t)a.q.nseq * a.q.T;
+    const int64_t tokens = a.q.tokens();
     ps.x = (const T*)(rev ? a.K : a.Q) + tk;
     ps.rows = (rev ? a.rows_k : a.rows_q) + h * tokens + sg.t0;
     ps.against = S;
@@ -1191,7 +1191,7 @@ __global__ __launch_bounds__(256) void k_lin_decay(const LinArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane_id();
   const Segment sg(a.q, slot);
   const int64_t at = (int64_t)slot * a.Hv + h;
-  const int64_t tokens = a.q.cu ? (int64_t)a.q.T : (int64_t)a.q.nseq * a.q.T;
+  const int64_t tokens = a.q.tokens();
   const float* rq = a.rows_q + h * tokens + sg.t0;
   const float* rk = a.rows_k + h * tokens + sg.t0;
   const int nc = (sg.len + LC - 1) / LC;
@@ -1295,7 +1295,7 @@ int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bo
 
 int64_t lin_workspace(LinArgs& a, bool backward, float* ws) {
   const int64_t slots = a.q.slots(), size = (int64_t)a.dk * a.dv;
-  const int64_t tokens = a.q.cu ? (int64_t)a.q.T : (int64_t)a.q.nseq * a.q.T;
+  const int64_t tokens = a.q.tokens();
   const bool many = a.q.seg < a.q.T;
   int64_t n = 0;
   auto take = [&](float*& p, int64_t m) {

@@ -19,8 +19,12 @@ struct LinSeqs {
   int nseq, T;    // T: tokens of each sequence, or of all where cu is given
   int seg, nseg;  // nseg: segments a sequence (cu null)
 
+  // (no sequences have neither, whatever T: cu holds one offset then)
   __host__ __device__ int64_t slots() const {
-    return cu ? (int64_t)T / seg + nseq : (int64_t)nseq * nseg;
+    return cu ? (nseq ? (int64_t)T / seg + nseq : 0) : (int64_t)nseq * nseg;
+  }
+  __host__ __device__ int64_t tokens() const {
+    return cu ? (nseq ? T : 0) : (int64_t)nseq * T;
   }
   __host__ __device__ int segments(int len) const { return len > 0 ? (len - 1) / seg + 1 : 0; }
   __device__ void at(int s, int64_t& t0, int64_t& base, int& len) const {
