@@ -74,7 +74,8 @@ int gdn_linear_forward_workspace(int nseq, int T, int Hk, int Hv, int dk, int dv
  * over its group of value heads, those of a head's decay over all its tokens.
  * Everything is formed in fp32 or sums of bf16 terms that make it up and
  * rounded once at the end, in a fixed order: the same call gives the same bits.
- * The rows of all heads of 64 tokens hold 2^30 values at most.
+ * The rows of all heads of 64 tokens (of T where that is less, of 16 at least)
+ * hold 2^30 values at most.
  * A value that is not finite reaches what it does in the forward pass, and
  * through dQ and dK the key head's other gradients; dg of a token reaches from
  * the tokens after it.

@@ -36,10 +36,11 @@ int set_sizes(gdn::LinArgs& a, const int32_t* cu, bool packed, int nseq, int T, 
 }
 
 // rows of a chunk lie at 32-bit offsets from its first (the gradients' sums over the heads of a
-// group are fp32)
-bool rows_fit(int T, int Hk, int Hv, int dk, int dv, int dtype) {
+// group are fp32).  In reversed time a short chunk's rows are placed from the end of a block of
+// 16, which begins before the first: `least` rows.
+bool rows_fit(int T, int Hk, int Hv, int dk, int dv, int dtype, int least) {
   const int64_t row = std::max((int64_t)Hk * dk, (int64_t)Hv * dv) * esize(dtype);
-  return std::min(T, gdn::LC) * row <= 1ll << 32;
+  return T == 0 || std::max(least, std::min(T, gdn::LC)) * row <= 1ll << 32;
 }
 
 }  // namespace
@@ -93,7 +94,7 @@ int gdn_linear_forward(const void* Q, const void* K, const void* V, const float*
   if (int r = set_sizes(a, cu_seqlens, cu_seqlens != nullptr, nseq, T, Hk, Hv, dk, dv, false,
                         dtype))
     return r;
-  if (!rows_fit(T, Hk, Hv, dk, dv, dtype)) return GDN_ERR_SHAPE;
+  if (!rows_fit(T, Hk, Hv, dk, dv, dtype, 1)) return GDN_ERR_SHAPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
   const int64_t tok = a.q.tokens(), es = esize(dtype);
   int64_t need = 4 * gdn::lin_workspace(a, false, nullptr);
@@ -138,7 +139,7 @@ int gdn_linear_backward(const void* Q, const void* K, const void* V, const float
   if (int r = set_sizes(a, cu_seqlens, cu_seqlens != nullptr, nseq, T, Hk, Hv, dk, dv, true,
                         dtype))
     return r;
-  if (!rows_fit(T, Hk, Hv, dk, dv, GDN_F32)) return GDN_ERR_SHAPE;
+  if (!rows_fit(T, Hk, Hv, dk, dv, GDN_F32, 16)) return GDN_ERR_SHAPE;
   if (Hv == 0 || (nseq == 0 && (g_per_token || !dg))) return GDN_OK;
   const int64_t tok = a.q.tokens(), es = esize(dtype);
   a.per_token = g_per_token != 0, a.want_dg = dg != nullptr, a.scale = scale;

@@ -11,3 +11,24 @@ def test_no_sequences_take_no_workspace():
         for dims in ((1, 2, 64, 64), (4, 4, 128, 128), (2, 6, 128, 64)):
             assert G.gdn_linear_forward_workspace(0, T, *dims, packed=True) == 0
             assert G.gdn_linear_backward_workspace(0, T, *dims, packed=True) == 0
+
+
+def test_rows_of_a_short_chunk_in_reversed_time():
+    """dK and dV place a chunk's rows from the end of a block of 16, at 32-bit byte offsets of fp32
+    rows: 16 rows of all heads, however few tokens there are, hold 2^30 values at most."""
+    ptr = [k << 44 for k in range(1, 14)]  # (a tensor of these sizes is under 2^44 bytes)
+
+    def call(T, H, dtype, dk=128, dv=128, Q=ptr[0]):
+        return G.lib.gdn_linear_backward(
+            Q, ptr[1], ptr[2], ptr[3], 0, ptr[4], None, None, ptr[5], ptr[6], ptr[7], ptr[8], None,
+            ptr[9], 1 << 43, None, 1, T, H, H, dk, dv, 1.0, dtype, None)
+
+    SHAPE, NULL = -2, -1
+    most = (1 << 30) // 16 // 128  # heads
+    for dtype in (0, 1):
+        for T in (1, 7, 15, 16):
+            assert call(T, 600_000, dtype) == SHAPE
+            assert call(T, most + 1, dtype) == SHAPE
+            assert call(T, most, dtype, Q=None) == NULL  # past the sizes
+            assert call(T, 2 * most + 2, dtype, 64, 64) == SHAPE
+        assert call(17, most, dtype) == SHAPE
