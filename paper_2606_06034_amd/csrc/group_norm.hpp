@@ -18,7 +18,7 @@ struct GroupArgs {
   bool act, wbf;
   // set by the launchers
   int tpi, gw, nw;      // groups in registers
-  int sparts, cblocks;  // groups read twice
+  int sparts, cblocks, nrows;  // groups read twice
 };
 
 hipError_t launch_group_forward(const GroupArgs& a, int dtype, hipStream_t st);

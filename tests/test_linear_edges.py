@@ -1,6 +1,8 @@
 """Linear attention and group norm at the edges of what their entry points take, on the CPU:
 sizes, workspaces and refusals."""
 
+import torch
+
 import paper_2606_06034_amd as G
 
 
@@ -32,3 +34,16 @@ def test_rows_of_a_short_chunk_in_reversed_time():
             assert call(T, most, dtype, Q=None) == NULL  # past the sizes
             assert call(T, 2 * most + 2, dtype, 64, 64) == SHAPE
         assert call(17, most, dtype) == SHAPE
+
+
+def test_group_norm_gradients_of_many_rows_take_few_sums():
+    """Past some thousand n's, one more takes two sums of each group and part of it (in 256 pieces),
+    and no row of dw and db of its own."""
+    for dtype, dt, V in ((torch.bfloat16, 1, 8), (torch.float32, 0, 4)):
+        for S, C, groups in ((1, 16384, 1), (4, 64, 8), (2, 64, 8), (49, 40, 5), (7, 8192, 2)):
+            parts = max(1, -(-(C // groups // V) // 256))
+            f = lambda N: G.gdn_group_norm_backward_workspace(N, S, C, groups, dtype)  # noqa: E731
+            assert f(20_000) - f(10_000) == 10_000 * groups * parts * 2 * 4
+            x = 20_000 * S * C * (2 if dt else 4)
+            # rows of dw and db: as many as the workgroups that run at a time have channels
+            assert f(20_000) <= x // 3 + 2 * 2048 * 256 * V * 4
