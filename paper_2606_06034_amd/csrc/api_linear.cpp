@@ -55,7 +55,9 @@ int gdn_linear_recurrent(const void* Q, const void* K, const void* V, const floa
   if (nseq < 0 || T < 0 || n_states < 0 || !valid_heads(Hk, Hv)) return GDN_ERR_SHAPE;
   if (!valid_d(dk) || !valid_d(dv)) return GDN_ERR_SHAPE;
   if (!slots && n_states < nseq && (S0 || S_final)) return GDN_ERR_SHAPE;
-  if (!grid_ok(((int64_t)nseq * Hv * (dv / 8) + 3) / 4, 256)) return GDN_ERR_SHAPE;
+  const int64_t heads = (int64_t)nseq * Hv;
+  if (heads > 0x7fffffffLL || !grid_ok((heads * (dv / gdn::kStepColumns) + 3) / 4, 256))
+    return GDN_ERR_SHAPE;
   if (!fdtype(dtype)) return GDN_ERR_DTYPE;
   if ((int64_t)nseq * Hv == 0) return GDN_OK;
   const int64_t tok = cu_seqlens ? (int64_t)T : (int64_t)nseq * T, es = esize(dtype);

@@ -86,6 +86,9 @@ int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bo
 // Floats of workspace; fills in the pointers where ws is given.
 int64_t lin_workspace(LinArgs& a, bool backward, float* ws);
 
+// Value columns a wave of the recurrent form takes; a workgroup has four waves.
+constexpr int kStepColumns = 32;
+
 hipError_t launch_linear_forward(const LinArgs& a, int dtype, hipStream_t st);
 hipError_t launch_linear_backward(const LinArgs& a, int dtype, hipStream_t st);
 hipError_t launch_linear_step(const void* Q, const void* K, const void* V, const float* g,

@@ -115,7 +115,7 @@ hipError_t launch_linear_step(const void* Q, const void* K, const void* V, const
                               const int* slots, int n_states, const int* cu, int nseq, int T,
                               int Hk, int Hv, int dk, int dv, float scale, int dtype,
                               hipStream_t st) {
-  constexpr int NCOL = 32;
+  constexpr int NCOL = kStepColumns;
   const int64_t waves = (int64_t)nseq * Hv * (dv / NCOL);
   const dim3 grid((unsigned)((waves + 3) / 4)), block(256);  // (checked to fit the grid)
   GDN_DK_SWITCH(dk, GDN_DV_SWITCH(dv, {

@@ -47,3 +47,23 @@ def test_group_norm_gradients_of_many_rows_take_few_sums():
             x = 20_000 * S * C * (2 if dt else 4)
             # rows of dw and db: as many as the workgroups that run at a time have channels
             assert f(20_000) <= x // 3 + 2 * 2048 * 256 * V * 4
+
+
+def test_sequences_and_heads_of_the_recurrent_form():
+    """A wave takes 32 value columns of a head, a workgroup of 256 work items four waves: 2^26 waves
+    are past HIP's 2^32 work items, a workgroup less is not."""
+    ptr = [k << 50 for k in range(1, 8)]
+
+    def call(nseq, Hv, dv, Q=None):
+        return G.lib.gdn_linear_recurrent(Q, ptr[1], ptr[2], ptr[3], 0, None, ptr[4], None, None, 0,
+                                          None, nseq, 1, 1, Hv, 64, dv, 1.0, 1, None)
+
+    SHAPE, NULL = -2, -1
+    for dv in (64, 128):
+        waves = 1 << 26
+        heads = waves // (dv // 32)
+        assert call(heads // 4, 4, dv) == SHAPE
+        assert call(heads // 4 - 1, 4, dv) == NULL  # past the sizes
+        assert call(heads // 4 // 4, 4, dv) == NULL
+        assert call(1 << 30, 1 << 30, dv) == SHAPE
+        assert call((1 << 31) - 1, (1 << 31) - 1, dv) == SHAPE
