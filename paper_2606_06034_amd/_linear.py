@@ -302,7 +302,9 @@ def gdn_group_norm_backward(dy: torch.Tensor, x: torch.Tensor, groups: int,
     N, S, C, dt, a = _group_sizes(x, groups, act)
     n, f32 = x.numel(), torch.float32
     dx = torch.empty_like(x) if dx is None else dx
-    if gate is not None and dz is None:
+    if gate is None:
+        dz = None
+    elif dz is None:
         dz = torch.empty_like(gate)
     want_db = bias is not None if want_db is None else want_db
     dw = torch.empty(C, dtype=f32, device=x.device) if want_dw else None

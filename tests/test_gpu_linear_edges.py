@@ -29,3 +29,14 @@ def test_packed_tokens_of_no_sequence(T, dt):
         for f in (G.gdn_linear_forward, G.gdn_linear_recurrent):
             _, S = f(q, k, v, g, cu_seqlens=cu, O=O)
             assert S.shape == (0, 4, 64, 64) and (O == 7).all()
+
+
+def test_group_norm_without_a_gate_has_no_gradient_of_one():
+    x = torch.randn(5, 3, 16, device="cuda")
+    w = torch.ones(16, device="cuda")
+    _, mean, rstd = G.gdn_group_norm_forward(x, 2, w)
+    dz = torch.full_like(x, 7.0)
+    got = G.gdn_group_norm_backward(x, x, 2, w, mean, rstd, dz=dz)
+    assert got[3] is None and (dz == 7).all()
+    got = G.gdn_group_norm_backward(x, x, 2, w, mean, rstd, gate=x, dz=dz)
+    assert got[3] is dz and not (dz == 7).any()
