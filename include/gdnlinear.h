@@ -135,7 +135,8 @@ int gdn_group_norm_forward_workspace(int64_t N, int S, int C, int G, int dtype, 
  * given, dz [N, S, C] in dtype; dw, db [C] fp32, summed over n and positions
  * (each nullable: not formed).  mean and rstd as the forward pass wrote them.
  * The sums are taken in a fixed order: the same call gives the same bits.
- * workspace: at least gdn_group_norm_backward_workspace() bytes. */
+ * workspace: at least gdn_group_norm_backward_workspace() bytes; groups that are
+ * read once take none (NULL) where neither dw nor db is formed. */
 int gdn_group_norm_backward(const void* dy, const void* x, const void* w, const void* b,
                             const void* z, const float* mean, const float* rstd, void* dx,
                             float* dw, float* db, void* dz, void* workspace,

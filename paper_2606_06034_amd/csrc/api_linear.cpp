@@ -228,13 +228,15 @@ int gdn_group_norm_backward(const void* dy, const void* x, const void* w, const 
   if (act != GDN_ACT_NONE && act != GDN_ACT_SILU) return GDN_ERR_PARAM;
   if (!grid_ok(gdn::group_backward_blocks(N, S, G, C / G, dtype), 256)) return GDN_ERR_SHAPE;
   if (N == 0 && !dw && !db) return GDN_OK;
-  int64_t need = 4 * gdn::group_backward_workspace(N, S, G, C / G, dtype);
+  int64_t need = 4 * gdn::group_backward_workspace(N, S, G, C / G, dtype, dw || db);
   if (N > 0) {
-    if (!dy || !x || !mean || !rstd || !dx || (z && !dz) || !workspace) return GDN_ERR_NULL;
+    if (!dy || !x || !mean || !rstd || !dx || (z && !dz) || (need && !workspace))
+      return GDN_ERR_NULL;
     if (workspace_bytes < need) return GDN_ERR_WORKSPACE;
   } else {
-    need = 0, workspace = nullptr;
+    need = 0;
   }
+  if (!need) workspace = nullptr;
   if (!z) dz = nullptr;
   const int64_t n = N * S * C * esize(dtype), wb = (int64_t)C * esize(w_dtype), sb = N * G * 4;
   const Span in[7] = {{dy, n}, {x, n}, {w, wb}, {b, wb}, {z, n}, {mean, sb}, {rstd, sb}};

@@ -772,11 +772,11 @@ int64_t group_backward_blocks(int64_t N, int S, int G, int Cg, int dtype) {
   tile_parts(a, V);
   return N * a.sparts * a.cblocks + 2 * ((a.C + 15) / 16);
 }
-int64_t group_backward_workspace(int64_t N, int S, int G, int Cg, int dtype) {
+int64_t group_backward_workspace(int64_t N, int S, int G, int Cg, int dtype, bool sums) {
   GroupArgs a = sizes(N, S, G, Cg);
   const int V = vec_of(Cg, dtype);
   const RowShape r = shape_of(S, Cg, V, true);
-  if (r.nv) return 2ll * row_parts(a, r, true) * a.C;
+  if (r.nv) return sums ? 2ll * row_parts(a, r, true) * a.C : 0;
   tile_parts(a, V);
   return 2ll * a.nrows * a.sparts * a.C + 2 * N * G * parts_a_group(a, V);
 }

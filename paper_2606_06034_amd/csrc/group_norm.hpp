@@ -26,8 +26,8 @@ hipError_t launch_group_backward(const GroupArgs& a, int dtype, hipStream_t st);
 // workgroups of the largest launch over groups that are read twice (else 0)
 int64_t group_forward_blocks(int64_t N, int S, int G, int Cg, int dtype);
 int64_t group_backward_blocks(int64_t N, int S, int G, int Cg, int dtype);
-// floats of workspace
+// floats of workspace (sums: with dw or db)
 int64_t group_forward_workspace(int64_t N, int S, int G, int Cg, int dtype);
-int64_t group_backward_workspace(int64_t N, int S, int G, int Cg, int dtype);
+int64_t group_backward_workspace(int64_t N, int S, int G, int Cg, int dtype, bool sums = true);
 
 }  // namespace gdn

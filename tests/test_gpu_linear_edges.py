@@ -40,3 +40,17 @@ def test_group_norm_without_a_gate_has_no_gradient_of_one():
     assert got[3] is None and (dz == 7).all()
     got = G.gdn_group_norm_backward(x, x, 2, w, mean, rstd, gate=x, dz=dz)
     assert got[3] is dz and not (dz == 7).any()
+
+
+def test_group_norm_gradient_of_rows_alone():
+    """Without dw and db, and without a workspace, dx is what it is with them."""
+    x, dy, z = (torch.randn(300, 64, device="cuda") for _ in range(3))
+    w = torch.rand(64, device="cuda")
+    _, mean, rstd = G.gdn_group_norm_forward(x, 4, w, gate=z)
+    want = G.gdn_group_norm_backward(dy, x, 4, w, mean, rstd, gate=z)
+    dx, dz = torch.empty_like(x), torch.empty_like(x)
+    code = G.lib.gdn_group_norm_backward(
+        dy.data_ptr(), x.data_ptr(), w.data_ptr(), None, z.data_ptr(), mean.data_ptr(),
+        rstd.data_ptr(), dx.data_ptr(), None, None, dz.data_ptr(), None, 0, 300, 1, 64, 4, 0, 0, 0,
+        torch.cuda.current_stream().cuda_stream)
+    assert code == 0 and torch.equal(dx, want[0]) and torch.equal(dz, want[3])

@@ -67,3 +67,20 @@ def test_sequences_and_heads_of_the_recurrent_form():
         assert call(heads // 4 // 4, 4, dv) == NULL
         assert call(1 << 30, 1 << 30, dv) == SHAPE
         assert call((1 << 31) - 1, (1 << 31) - 1, dv) == SHAPE
+
+
+def test_group_norm_gradients_without_sums_of_rows():
+    """Rows in registers use the workspace for dw and db alone: without these it may be NULL."""
+    ptr = [k << 40 for k in range(1, 10)]
+
+    def call(S, dw, db, ws, wsb=0, dx=ptr[5] + 4, C=96, N=8):
+        return G.lib.gdn_group_norm_backward(ptr[0], ptr[1], ptr[2], None, None, ptr[3], ptr[4], dx,
+                                             dw, db, None, ws, wsb, N, S, C, 8, 0, 1, 0, None)
+
+    NULL, ALIGN, WS = -1, -5, -9
+    assert call(1, None, None, None) == ALIGN  # past the workspace: dx is refused
+    assert call(1, ptr[6], None, None) == NULL
+    assert call(1, None, ptr[6], None) == NULL
+    assert call(1, ptr[6], None, ptr[7], 4) == WS
+    assert call(5, None, None, None) == NULL  # read twice: the groups' sums
+    assert call(1, None, None, None, C=65536) == ALIGN
