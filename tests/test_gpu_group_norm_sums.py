@@ -19,8 +19,9 @@ pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
-def reference(x, w, b, z, dy, groups, act, eps):
-    """(dx, dw, db, dz, sums of magnitudes of dw, of db) in 64 bits"""
+def reference(x, w, b, z, dy, groups, act, eps, means=(1, 1)):
+    """(dx, dw, db, dz, sums of magnitudes of dw, of db) in 64 bits; means: of dh and of dh h, as
+    they are taken out of dx"""
     N, S, C = x.shape
     x, w, b, z, dy = (None if t is None else t.double() for t in (x, w, b, z, dy))
     g = lambda t: t.view(N, S, groups, C // groups)  # noqa: E731
@@ -41,16 +42,17 @@ def reference(x, w, b, z, dy, groups, act, eps):
     if act:
         dn = dn * s * (1 + n * (1 - s))
     dh = dn if w is None else dn * w
-    dx = (rstd * (g(dh) - mean(dh) - g(h) * mean(dh * h))).view(N, S, C)
+    dx = g(dh) - means[0] * mean(dh) - means[1] * g(h) * mean(dh * h)
+    dx = (rstd * dx).view(N, S, C)
     return (dx, (dn * h).sum((0, 1)), dn.sum((0, 1)), dz, (dn * h).abs().sum((0, 1)),
             dn.abs().sum((0, 1)))
 
 
-def make(N, S, C, groups, dt, wdt, bias, gate, seed):
-    r = torch.Generator("cuda").manual_seed(seed)
-    normal = lambda *s: torch.randn(*s, generator=r, device="cuda")  # noqa: E731
+def make(N, S, C, groups, dt, wdt, bias, gate, seed, device="cuda"):
+    r = torch.Generator(device).manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=r, device=device)  # noqa: E731
     size, mean = normal(N, 1, groups, 1).exp(), 2 * torch.rand(N, 1, groups, 1, generator=r,
-                                                              device="cuda") - 1
+                                                              device=device) - 1
     h = normal(N, S, groups, C // groups)
     x = ((h + 2 * mean) * size).view(N, S, C).to(DT[dt])
     dy = (normal(N, S, C) + 1 + h.view(N, S, C)).to(DT[dt])
@@ -90,3 +92,19 @@ MANY = [  # N, S, C, groups: maps of few positions, and rows of long groups
 @pytest.mark.parametrize("N,S,C,groups", MANY)
 def test_many_rows(N, S, C, groups, dt, wdt, act, bias, gate):
     check(N, S, C, groups, dt, wdt, act, bias, gate)
+
+
+SHAPES = [  # groups of 32 values and more: in registers, in parts of positions, in column blocks
+    (33, 1, 512, 4), (9, 1, 4096, 32), (3, 1, 1025, 5), (2, 1, 8190, 3), (700, 1, 2048, 16),
+    (2, 1, 16384, 1), (2, 1, 65536, 1), (3, 7, 24, 3), (2, 49, 40, 4), (4, 100, 96, 8),
+    (2, 1000, 33, 3), (1, 5000, 64, 2), (2, 4096, 32, 2), (1, 30011, 6, 2), (1, 20000, 10, 1),
+    (2, 9, 9216, 2), (1, 3, 30000, 3), (2, 700, 2560, 1), (3, 3001, 328, 8), (60, 300, 640, 32)]
+
+
+@pytest.mark.parametrize("dt,wdt", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"),
+                                    ("f32", "bf16")])
+@pytest.mark.parametrize("N,S,C,groups", SHAPES)
+def test_means_and_sums(N, S, C, groups, dt, wdt):
+    for act, bias, gate in ((None, False, True), ("silu", True, False), ("silu", True, True),
+                            (None, True, False)):
+        check(N, S, C, groups, dt, wdt, act, bias, gate)
