@@ -61,10 +61,10 @@ template <> struct FragFor<__bf16> { typedef bf16x4 type; };
 // Terms of states and of P where they go into outputs in bf16 alone.  (One would add as much
 // again to the outputs' own rounding.)
 constexpr int kOut = 2;
-// Blocks of 16 value columns a wave has, of 128 columns: eight waves form a segment's state (as
-// many loads in flight as there can be), four walk (16 heads of 8192 tokens: 48 us, 47 with
-// eight waves, which take twice the LDS reads of P and leave no room for a second workgroup).
-constexpr int kStateBlocks = 1, kWalkBlocks = 2;
+// Blocks of 16 value columns a wave has where a segment's state is formed: eight waves for 128
+// columns, as many loads in flight as there can be.  Four walk (16 heads of 8192 tokens: 48 us, 47
+// with eight, which take twice the LDS reads of P and leave no room for a second workgroup).
+constexpr int kStateBlocks = 1;
 constexpr int kMostChunks = 16;  // of a segment of the backward pass
 
 constexpr double kLog2e = 1.4426950408889634074;
@@ -289,18 +289,14 @@ struct StateOf {
     if (flip) return *(const f32x4*)(p + c * DK + r);
     return f32x4{p[r * DV + c], p[(r + 1) * DV + c], p[(r + 2) * DV + c], p[(r + 3) * DV + c]};
   }
-  __device__ __forceinline__ void store(float* p, bool flip, int w, Lane ln) const {
+  __device__ __forceinline__ void store(float* p, int w, Lane ln) const {
 #pragma unroll
     for (int m = 0; m < 2 * NQ; ++m)
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
         const int r = row(m, ln), c = col(n, w, ln);
-        if (flip) {
-          *(f32x4*)(p + c * DK + r) = b[m][n];
-        } else {
 #pragma unroll
-          for (int v = 0; v < 4; ++v) p[(r + v) * DV + c] = b[m][n][v];
-        }
+        for (int v = 0; v < 4; ++v) p[(r + v) * DV + c] = b[m][n][v];
       }
   }
   __device__ __forceinline__ void decay(float el) {
@@ -382,7 +378,6 @@ struct GateStream {
   float now;
   bool mine;
   float s_out, s_in;
-  double total = 0.0;
   __device__ GateStream(const LinArgs& a_, const Segment& sg, const Chunks& c, int h, bool m, float so,
                         float si)
       : a(a_), ch(c), g(a_.g + (a_.per_token ? sg.t0 * a_.Hv + h : h)), mine(m), s_out(so), s_in(si) {
@@ -396,7 +391,7 @@ struct GateStream {
   // those of chunk i, at the buffer that chunk i - 2 has left
   __device__ __forceinline__ void form(Gates* two, int i) {
     if (!mine || i >= ch.n) return;
-    total += form_gates(two + (i & 1), now, a.per_token, ch.size(i), ch.rev, s_out, s_in);
+    form_gates(two + (i & 1), now, a.per_token, ch.size(i), ch.rev, s_out, s_in);
     fetch(i + 1);
   }
 };
@@ -470,7 +465,7 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
                          : log_decay(x) * ch.size(i - 1);
   }
   float* to = (rev ? a.R : a.U) + ((int64_t)slot * a.Hv + h) * DK * DV;
-  S.store(to, false, w, ln);
+  S.store(to, w, ln);
   if (threadIdx.x == 0 && (!rev || sg.j == sg.n - 1))  // (once for each segment)
     a.dec[(int64_t)slot * a.Hv + h] = exp2_of(total);
 }
@@ -740,17 +735,17 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       }
     };
     auto row_of = [](int b) { return b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3; };
-    static_assert(NW >= 4, "two blocks a wave and two over");
+    static_assert(NW == 4, "two of the ten blocks a wave, and two over");
     {
-      const int b1 = w + NW < 10 ? w + NW : w;  // (of eight waves six repeat their block)
+      const int b1 = w + NW;
       const int I0 = row_of(w), J0 = w - I0 * (I0 + 1) / 2;
       const int I1 = row_of(b1), J1 = b1 - I1 * (I1 + 1) / 2;
       const f32x4 p0 = products(I0, J0), p1 = products(I1, J1);
       f32x4 y0 = zero4(), y1 = zero4();
       if constexpr (pairs) y0 = more_products(I0, J0), y1 = more_products(I1, J1);
       finish(p0, y0, I0, J0);
-      if (b1 != w) finish(p1, y1, I1, J1);
-      if (NW == 4 && w < 2) {
+      finish(p1, y1, I1, J1);
+      if (w < 2) {
         const int J = w + 2;  // blocks 8 and 9
         f32x4 y = zero4();
         const f32x4 p = products(3, J);
@@ -882,7 +877,7 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
                 __builtin_convertvector(y, Out);
         }
   }
-  if (!flip && ps.fin) S.store(ps.fin, flip, w, ln);
+  if (!flip && ps.fin) S.store(ps.fin, w, ln);
   if (!far_rows) return;
   lds_only_barrier();
   write_rows(ch.n - 1);
@@ -945,15 +940,12 @@ __device__ __forceinline__ void copy_state(const LinArgs& a, int s, const float*
 
 }  // namespace
 
-// waves a SIMD: two workgroups a CU, with fp32 inputs one
-template <typename T> constexpr int waves_of(int threads) {
-  return threads / 256 * (sizeof(T) == 2 ? 2 : 1);
-}
+// workgroups a CU, of a wave a SIMD each
+template <typename T> constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
 
-template <int DK, int DV, int NS, typename T, int TS, int TO, int TP>
-__global__ __launch_bounds__(4 * DV / NS, waves_of<T>(4 * DV / NS)) void k_lin_forward(
-    const LinArgs a, uint32_t n) {
-  constexpr int NT = 4 * DV / NS;
+template <int DK, int DV, typename T, int TS, int TO, int TP>
+__global__ __launch_bounds__(256, kGroups<T>) void k_lin_forward(const LinArgs a, uint32_t n) {
+  constexpr int NS = DV / 64, NT = 256;
   __shared__ __attribute__((aligned(16))) T sq[LC * DK], sk[LC * DK], sv[LC * DV];
   __shared__ __attribute__((aligned(16))) TeamLds<DV / 16 / NS, T, TP> lds;
   const uint32_t blocks = (n + 7) & ~7u;
@@ -1144,8 +1136,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uin
 
 // one of the gradients by a team of its own
 template <int DK, int DV, typename T, int TS, int TO, int TP, Kind P, bool DG>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_lin_backward(const LinArgs a,
-                                                                             uint32_t n) {
+__global__ __launch_bounds__(256, kGroups<T>) void k_lin_backward(const LinArgs a, uint32_t n) {
   constexpr bool keys = kFlipped<P>;
   constexpr int D0 = keys ? DV : DK, D1 = keys ? DK : DV;  // of the products, of the result
   __shared__ __attribute__((aligned(16))) T sq[LC * D0], sk[LC * D0], sv[LC * D1];
@@ -1321,7 +1312,7 @@ namespace {
 hipError_t launch_states(const LinArgs& a, int dtype, bool both, hipStream_t st) {
   const uint32_t n = (uint32_t)(a.q.slots() * a.Hv), grid = (n * (both ? 2 : 1) + 7) & ~7u;
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
-    constexpr int NS = kStateBlocks * DV / 128 > 0 ? kStateBlocks * DV / 128 : 1;
+    constexpr int NS = kStateBlocks;
     if (dtype == 0)
       hipLaunchKernelGGL((k_lin_state<DK, DV, NS, float, 1>), dim3(grid), dim3(4 * DV / NS), 0, st, a,
                          n, both);
@@ -1347,13 +1338,11 @@ hipError_t launch_linear_forward(const LinArgs& a, int dtype, hipStream_t st) {
   const uint32_t grid = ((n + 7) & ~7u) + (a.Sf && (a.q.cu || a.q.T == 0) ? a.q.nseq : 0);
   if (grid == 0) return hipSuccess;
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
-    constexpr int NS = kWalkBlocks * DV / 128 > 0 ? kWalkBlocks * DV / 128 : 1;
     if (dtype == 0)
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, DV / 64, float, 1, 1, 1>), dim3(grid), dim3(256), 0,
-                         st, a, n);
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, float, 1, 1, 1>), dim3(grid), dim3(256), 0, st, a, n);
     else
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, NS, __bf16, 3, kOut, kOut>), dim3(grid),
-                         dim3(4 * DV / NS), 0, st, a, n);
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, __bf16, 3, kOut, kOut>), dim3(grid), dim3(256), 0, st,
+                         a, n);
     return hipGetLastError();
   }))
   return hipErrorNotSupported;

@@ -7,7 +7,7 @@
 
 namespace gdn {
 
-// Tokens a chunk, and the most tokens of a segment, which one workgroup walks.
+// Tokens a chunk, the step of a walk.
 constexpr int LC = 64;
 
 // Sequences, and how they are cut into segments of `seg` tokens (a multiple of LC), which
@@ -72,7 +72,8 @@ struct LinArgs {
   float *Sf, *dS0, *dg;
   int Hk, Hv, dk, dv;
   float scale;
-  // workspace (all null where every sequence is one segment and no dg is wanted)
+  // workspace, each null where it is not needed (U, R, dec: every sequence is one segment; acc_q,
+  // acc_k: one value head a key head; the others: no dg)
   float *U, *R;           // [slots, Hv, dk, dv]: states entering, their gradients leaving
   float* dec;             // [slots, Hv]: decay over a segment
   float *rows_q, *rows_k;  // [Hv, tokens]: what dg takes of each token (linear.hip)
