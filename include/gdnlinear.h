@@ -44,10 +44,8 @@ extern "C" {
  * but must not overlap it otherwise.  An empty sequence keeps its state.  The
  * rows of all heads of 64 tokens (of T where that is less) of Q and of V hold
  * 4 GiB at most.
- * With bf16 inputs the states, and the products q . k under the decay, enter
- * the outputs as sums of two bf16 terms (2^-16 of each), and the values under
- * the decay the states as sums of three (2^-24), of two where only outputs
- * take the state up.
+ * With bf16 inputs the states, the products q . k under the decay and the values
+ * under the decay enter products as sums of three bf16 terms (2^-24 of each).
  * A value that is not finite makes what it reaches not finite either (an
  * infinity NaN), and may do so to other tokens of its 64, counted from the
  * sequence's first; it reaches no other sequence and no other value head that

@@ -25,9 +25,9 @@
 // k_lin_scan carries the states over the segments, k_lin_forward / k_lin_backward walk.
 //
 // Precision.  bf16 inputs are exact operands of the matrix instructions; fp32 factors
-// (states, decayed values, P) enter as sums of bf16 terms (split.hpp): two, 2^-16 of each, for
-// what goes into bf16 outputs alone, three, 2^-24, for states and dg, which are fp32 results.
-// fp32 inputs go to the fp32 matrix instructions.
+// (states, decayed values, P) enter as sums of three bf16 terms (split.hpp), 2^-24 of each.  (Two
+// where a result is in bf16 take 2 to 8 % less time, and are off by several roundings of a
+// result whose terms cancel to a thousandth.)  fp32 inputs go to the fp32 matrix instructions.
 //
 // Bound: a pass's tiles are read once and take 3 TB/s; the rest is the serial step of a chunk,
 // products of at most 128 x 128 x 64 with the splits between them.  A step takes 4.3 us with
@@ -58,9 +58,6 @@ __device__ __forceinline__ int anew(int x) {
 template <typename T> struct FragFor { typedef f32x4 type; };
 template <> struct FragFor<__bf16> { typedef bf16x4 type; };
 
-// Terms of states and of P where they go into outputs in bf16 alone.  (One would add as much
-// again to the outputs' own rounding.)
-constexpr int kOut = 2;
 // Blocks of 16 value columns a wave has where a segment's state is formed: eight waves for 128
 // columns, as many loads in flight as there can be.  Four walk (16 heads of 8192 tokens: 48 us, 47
 // with eight, which take twice the LDS reads of P and leave no room for a second workgroup).
@@ -235,27 +232,6 @@ __device__ __forceinline__ Pair<F> load_run8(const float* p) {
   return Pair<F>{*(const f32x4*)p, *(const f32x4*)(p + 4)};
 }
 
-// The first N terms of a split value (fp32: the value)
-template <typename F, int N> struct Some { Pair<F> t[N]; };
-template <typename F, int N> constexpr int kTerms = TermsOf<F>::N == 1 ? 1 : N;
-template <typename F, int N>
-__device__ __forceinline__ auto some(f32x4 lo, f32x4 hi) {
-  constexpr int M = kTerms<F, N>;
-  Some<F, M> r;
-  if constexpr (TermsOf<F>::N == 1) {
-    r.t[0] = join(lo, hi);
-  } else {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    float a = lo[0], b = lo[1], c = lo[2], d = lo[3], e = hi[0], f = hi[1], x = hi[2], y = hi[3];
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      const uint32_t p = take2(a, b), q = take2(c, d), u = take2(e, f), w = take2(x, y);
-      r.t[i].v = __builtin_bit_cast(bf16x8, u32x4{p, q, u, w});
-    }
-  }
-  return r;
-}
-
 // A wave's part of a [DK, DV] state: all rows, NS blocks of 16 columns.  Block m = 2q + h,
 // block row 4g + v holds state row 32q + 8g + 4h + v, so that two blocks are the pair that
 // meets a run of 8 values of a row; column c of block n of wave w is 16 NS w + 4 NS (c / 4) + 4n +
@@ -306,7 +282,7 @@ struct StateOf {
       for (int n = 0; n < NS; ++n) b[m][n] *= el;
   }
   // S <- S + (diag(in) K)^T V of the chunk in LDS, the factor on V's rows
-  template <int TS, typename T>
+  template <typename T>
   __device__ __forceinline__ void update(const T* sK, const T* sV, const Gates* gt, int w,
                                          Lane ln) {
     typedef typename FragFor<T>::type F;
@@ -314,11 +290,11 @@ struct StateOf {
     for (int p = 0; p < 2; ++p) {
       const f32x4 wl = *(const f32x4*)(gt->in + 32 * p + 4 * ln.g());
       const f32x4 wh = *(const f32x4*)(gt->in + 32 * p + 16 + 4 * ln.g());
-      Some<F, kTerms<F, TS>> y[NS];
+      Terms<F> y[NS];
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
         const Pair<F> x = down_frag<DV, 4 * NS>(sV, 32 * p, 16 * NS * w + 4 * n, ln);
-        y[n] = some<F, TS>(x.lo() * wl, x.hi() * wh);
+        y[n] = split<F>(x.lo() * wl, x.hi() * wh);
       }
 #pragma unroll
       for (int m0 = 0; m0 < 2 * NQ; m0 += 2) {  // 2 NS sums side by side
@@ -327,7 +303,7 @@ struct StateOf {
         for (int m = 0; m < 2; ++m)
           k[m] = down_frag<DK, 8>(sK, 32 * p, 16 * m0 + 4 * m, ln);
 #pragma unroll
-        for (int i = kTerms<F, TS> - 1; i >= 0; --i)
+        for (int i = TermsOf<F>::N - 1; i >= 0; --i)
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -402,7 +378,7 @@ __device__ __forceinline__ uint32_t work_item(uint32_t b, uint32_t n) {
 }
 
 // ---- what a segment adds to the state
-template <int DK, int DV, int NS, typename T, int TS, bool REV>
+template <int DK, int DV, int NS, typename T, bool REV>
 __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& sg, uint32_t slot,
                                                int h, T* sK, T* sV, Gates* gt) {
   constexpr bool rev = REV;
@@ -456,7 +432,7 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
       gates(i - 1, g);
       g = decay_of(i - 2);
     }
-    S.template update<TS>(sK, sV, gt + (i & 1), w, ln);
+    S.update(sK, sV, gt + (i & 1), w, ln);
     if (!more) break;
   }
   for (; w == 0 && i > 0; --i) {  // (the decay over all of the segment)
@@ -473,7 +449,7 @@ __device__ __forceinline__ void add_of_segment(const LinArgs& a, const Segment& 
 }  // namespace
 
 // `both`: the gradients' states too, in the second half of the work items
-template <int DK, int DV, int NS, typename T, int TS>
+template <int DK, int DV, int NS, typename T>
 __global__ __launch_bounds__(4 * DV / NS) void k_lin_state(const LinArgs a, uint32_t n, bool both) {
   __shared__ __attribute__((aligned(16))) T sK[LC * DK], sV[LC * DV];
   __shared__ __attribute__((aligned(16))) Gates gt[2];
@@ -487,9 +463,9 @@ __global__ __launch_bounds__(4 * DV / NS) void k_lin_state(const LinArgs a, uint
   // (the last segment's share ends in S_final, the first one's in dS0: the walks form those)
   if (sg.len == 0 || (rev ? sg.j == 0 : sg.j == sg.n - 1)) return;
   if (rev)
-    add_of_segment<DK, DV, NS, T, TS, true>(a, sg, slot, h, sK, sV, gt);
+    add_of_segment<DK, DV, NS, T, true>(a, sg, slot, h, sK, sV, gt);
   else
-    add_of_segment<DK, DV, NS, T, TS, false>(a, sg, slot, h, sK, sV, gt);
+    add_of_segment<DK, DV, NS, T, false>(a, sg, slot, h, sK, sV, gt);
 }
 
 // The states carried over the segments of each sequence, in place: U from what a segment
@@ -562,9 +538,9 @@ template <Kind P> constexpr bool kReversed = P == kDK || P == kDV;
 template <Kind P> constexpr bool kFlipped = P == kDQ || P == kDK;  // the state, in memory
 
 // What the waves of a pass share, beside its tiles.
-template <int NW, typename T, int TP>
+template <int NW, typename T>
 struct TeamLds {
-  T p[6 * kTerms<typename FragFor<T>::type, TP> * 512];
+  T p[6 * TermsOf<typename FragFor<T>::type>::N * 512];
   float far[NW][LC];             // the waves' shares of x . (what came from the state)
   float row[4][LC], col[4][LC];  // sums of M's blocks (I, J): along rows at J, down columns at I
   Gates gt[2];
@@ -591,18 +567,16 @@ __host__ __device__ constexpr int p_slot(int I, int p) { return (I == 3 ? 4 : I)
 template <typename T, int N> struct RunType { typedef T type __attribute__((ext_vector_type(N))); };
 template <typename T, int N> using RunOf = typename RunType<T, N>::type;
 
-// Terms: TS of the decayed values that the state takes up, TO of the state, TP of P.
 // DG: with the rows that the gradient of g takes (of dQ and dK).  A team of NW waves walks;
 // two teams of a workgroup walk side by side on tiles that all of them bring, with the same
 // barriers.  other: what a second team gives a first one to add to its result (null: none).
 // XS: x is a tile (with dK), else rows in memory.
-template <int DK, int DV, int NS, typename T, int TS, int TO, int TP, Kind P, bool DG, bool XS,
-          typename Tiles>
+template <int DK, int DV, int NS, typename T, Kind P, bool DG, bool XS, typename Tiles>
 __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h, const Pass& ps,
-                                     Tiles& tiles, TeamLds<DV / 16 / NS, T, TP>* lds,
+                                     Tiles& tiles, TeamLds<DV / 16 / NS, T>* lds,
                                      float* other = nullptr) {
   typedef typename FragFor<T>::type F;
-  constexpr int NQ = DK / 32, NW = DV / 16 / NS, MO = kTerms<F, TO>, MP = kTerms<F, TP>;
+  constexpr int NQ = DK / 32, NW = DV / 16 / NS, N = TermsOf<F>::N;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % NW;
   const Lane ln = lane_here();
   constexpr bool rev = kReversed<P>, flip = kFlipped<P>;
@@ -633,9 +607,9 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
   gates.form(lds->gt, 0);
   // P's blocks above the diagonal that share a pair with one on it
   if (w < 2) {
-    T* to = lds->p + p_slot(2 * w, w) * MP * 512;
+    T* to = lds->p + p_slot(2 * w, w) * N * 512;
 #pragma unroll
-    for (int t = 0; t < MP; ++t) {
+    for (int t = 0; t < N; ++t) {
       if constexpr (sizeof(T) == 4)
         *(f32x4*)(to + 256 + 4 * ln.id) = zero4();
       else
@@ -709,14 +683,14 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
         const float d = __builtin_amdgcn_exp2f((hi - hj[u]) + (lo - lj[u]));
         p[u] = 16 * J + g4 + u <= r ? a.scale * p[u] * d : 0.f;
       }
-      T* to = lds->p + p_slot(I, J >> 1) * MP * 512;
+      T* to = lds->p + p_slot(I, J >> 1) * N * 512;
       if constexpr (sizeof(T) == 4) {
         *(f32x4*)(to + 256 * (J & 1) + 4 * ln.id) = p;
       } else {
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
         float p0 = p[0], p1 = p[1], p2 = p[2], p3 = p[3];
 #pragma unroll
-        for (int t = 0; t < MP; ++t) {
+        for (int t = 0; t < N; ++t) {
           const uint32_t x = take2(p0, p1), z = take2(p2, p3);
           *(u32x2*)(to + t * 512 + 8 * ln.id + 4 * (J & 1)) = u32x2{x, z};
         }
@@ -772,16 +746,16 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       for (int n = 0; n < NS; ++n) o[I][n] = zero4();
 #pragma unroll
     for (int s = 0; s < NQ; ++s) {
-      Some<F, MO> y[NS];
+      Terms<F> y[NS];
 #pragma unroll
-      for (int n = 0; n < NS; ++n) y[n] = some<F, TO>(S.b[2 * s][n], S.b[2 * s + 1][n]);
+      for (int n = 0; n < NS; ++n) y[n] = split<F>(S.b[2 * s][n], S.b[2 * s + 1][n]);
 #pragma unroll
       for (int I0 = 0; I0 < 4; I0 += 2) {
         Pair<F> x[2];
 #pragma unroll
         for (int I = 0; I < 2; ++I) x[I] = run_frag<DK>(sq, 16 * (I0 + I), 32 * s, ln);
 #pragma unroll
-        for (int t = MO - 1; t >= 0; --t)
+        for (int t = N - 1; t >= 0; --t)
 #pragma unroll
           for (int I = 0; I < 2; ++I)
 #pragma unroll
@@ -817,7 +791,7 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       }
     if (!end) tiles.template fetch<rev>(ch.at(i + 1), ch.size(i + 1), anew(threadIdx.x));
     S.decay(gt->el);
-    S.template update<TS>(sk, sv, gt, w, ln);
+    S.update(sk, sv, gt, w, ln);
     lds_only_barrier();
     if (pairs && end && w == 0 && ln.id == 0) {
       double x = 0.0;
@@ -833,10 +807,10 @@ __device__ __forceinline__ void walk(const LinArgs& a, const Segment& sg, int h,
       for (int n = 0; n < NS; ++n)
         y[n] = down_frag<DV, 4 * NS>(sv, 32 * p, 16 * NS * w + 4 * n, ln);
 #pragma unroll
-      for (int t = MP - 1; t >= 0; --t)
+      for (int t = N - 1; t >= 0; --t)
 #pragma unroll
         for (int I = 2 * p; I < 4; ++I) {
-          const T* from = lds->p + (p_slot(I, p) * MP + t) * 512;
+          const T* from = lds->p + (p_slot(I, p) * N + t) * 512;
           Pair<F> x;
           if constexpr (sizeof(T) == 4)
             x = join(*(const f32x4*)(from + 4 * ln.id), *(const f32x4*)(from + 256 + 4 * ln.id));
@@ -943,11 +917,11 @@ __device__ __forceinline__ void copy_state(const LinArgs& a, int s, const float*
 // workgroups a CU, of a wave a SIMD each
 template <typename T> constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
 
-template <int DK, int DV, typename T, int TS, int TO, int TP>
+template <int DK, int DV, typename T>
 __global__ __launch_bounds__(256, kGroups<T>) void k_lin_forward(const LinArgs a, uint32_t n) {
   constexpr int NS = DV / 64, NT = 256;
   __shared__ __attribute__((aligned(16))) T sq[LC * DK], sk[LC * DK], sv[LC * DV];
-  __shared__ __attribute__((aligned(16))) TeamLds<DV / 16 / NS, T, TP> lds;
+  __shared__ __attribute__((aligned(16))) TeamLds<DV / 16 / NS, T> lds;
   const uint32_t blocks = (n + 7) & ~7u;
   if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.S0, a.Sf);
   const uint32_t w = work_item(blockIdx.x, n);
@@ -967,12 +941,7 @@ __global__ __launch_bounds__(256, kGroups<T>) void k_lin_forward(const LinArgs a
   ps.out = (T*)a.O + tv;
   ps.start = a.U ? a.U + ((int64_t)slot * a.Hv + h) * size : a.S0 ? a.S0 + own : nullptr;
   ps.fin = a.Sf && sg.j == sg.n - 1 ? a.Sf + own : nullptr;
-  // (a state that goes into outputs in bf16 alone takes up values in as many terms as it gives;
-  // the last segment's is S_final, asked for or not: the outputs are the same either way)
-  if (TS > TO && sg.j != sg.n - 1)
-    walk<DK, DV, NS, T, TO, TO, TP, kO, false, false>(a, sg, h, ps, tiles, &lds);
-  else
-    walk<DK, DV, NS, T, TS, TO, TP, kO, false, false>(a, sg, h, ps, tiles, &lds);
+  walk<DK, DV, NS, T, kO, false, false>(a, sg, h, ps, tiles, &lds);
 }
 
 // ---- the gradients.  A workgroup is two teams of four waves on common tiles (read apart, the
@@ -1019,10 +988,10 @@ __device__ __forceinline__ Pass value_pass(const LinArgs& a, const Segment& sg, 
 }
 
 // dQ or dK of a key head with an even group: its value heads two by two
-template <int DK, int DV, typename T, int TS, int TO, int TP, Kind P, bool DG>
+template <int DK, int DV, typename T, Kind P, bool DG>
 __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segment& sg,
                                                     uint32_t slot, int hk, T* s, float* other,
-                                                    TeamLds<4, T, TP>* lds) {
+                                                    TeamLds<4, T>* lds) {
   constexpr bool rev = P == kDK, more = rev && DG;
   const int gr = a.Hv / a.Hk, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   constexpr int VT = LC * DV, KT = LC * DK;
@@ -1043,8 +1012,7 @@ __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segm
     if (more) ps.x = s + 4 * VT + KT;
     ps.acc = gr > 2 ? (rev ? a.acc_k : a.acc_q) + tk : nullptr;
     ps.first = u == 0, ps.last = u == gr - 2;
-    walk<DV, DK, DK / 64, T, DG ? TS : TO, TO, TP, P, DG, more>(a, sg, h + team, ps, tiles,
-                                                                lds + team, other);
+    walk<DV, DK, DK / 64, T, P, DG, more>(a, sg, h + team, ps, tiles, lds + team, other);
     lds_only_barrier();
   }
 }
@@ -1053,13 +1021,13 @@ __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segm
 
 // groups of even size.  (4 x 8192 tokens, 32 heads in pairs: 0.97 to 1.1 ms, 3 TB/s, vector units
 // busy 44 % and matrix units 28 %.)
-template <int DK, int DV, typename T, int TS, int TO, int TP, bool DG>
+template <int DK, int DV, typename T, bool DG>
 __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a, uint32_t slots) {
   // the second team's results go where the tiles of products lie, which the first has done with
   __shared__ __attribute__((aligned(16))) T s[LC * (4 * DV + (DG ? 2 : 1) * DK)];
   static_assert(4 * DV * sizeof(T) >= DK * sizeof(float) && 2 * DV >= DK, "what else lies there");
   float* other = (float*)s;
-  __shared__ __attribute__((aligned(16))) TeamLds<4, T, TP> lds[2];
+  __shared__ __attribute__((aligned(16))) TeamLds<4, T> lds[2];
   const uint32_t nk = slots * (uint32_t)a.Hk, nv = slots * (uint32_t)(a.Hv / 2);
   const uint32_t bk = (2 * nk + 7) & ~7u, bv = (nv + 7) & ~7u;
   if (blockIdx.x >= bk + bv) return copy_state(a, (int)(blockIdx.x - bk - bv), a.dSf, a.dS0);
@@ -1072,9 +1040,9 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a,
   const Segment sg(a.q, slot);
   if (sg.len == 0) return;
   if (keys && w >= nk) {
-    key_gradient_by_two<DK, DV, T, TS, TO, TP, kDK, DG>(a, sg, slot, i, s, other, lds);
+    key_gradient_by_two<DK, DV, T, kDK, DG>(a, sg, slot, i, s, other, lds);
   } else if (keys) {
-    key_gradient_by_two<DK, DV, T, TS, TO, TP, kDQ, DG>(a, sg, slot, i, s, other, lds);
+    key_gradient_by_two<DK, DV, T, kDQ, DG>(a, sg, slot, i, s, other, lds);
   } else {
     const int team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), h = 2 * i;
     const int64_t tk = (sg.t0 * a.Hk + h / (a.Hv / a.Hk)) * DK, tv = (sg.t0 * a.Hv + h) * DV;
@@ -1085,22 +1053,17 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a,
                                     {(const T*)a.dO + tv + DV, a.Hv, s + 2 * KT + VT}};
     Pass ps = value_pass<DK, DV, T>(a, sg, slot, h + team);
     ps.q = s, ps.k = s + KT, ps.v = s + 2 * KT + team * VT;
-    if (sg.j == 0)
-      walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles,
-                                                               lds + team);
-    else
-      walk<DK, DV, DV / 64, T, kOut, kOut, TP, kDV, false, false>(a, sg, h + team, ps, tiles,
-                                                                 lds + team);
+    walk<DK, DV, DV / 64, T, kDV, false, false>(a, sg, h + team, ps, tiles, lds + team);
   }
 }
 
 // dK and dV of a key head's value heads one after the other.  (8192 tokens of 16 heads: 89 us,
 // 2.7 TB/s, vector units busy 40 % and matrix units 26 %.)
-template <int DK, int DV, typename T, int TS, int TO, int TP, bool DG>
+template <int DK, int DV, typename T, bool DG>
 __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uint32_t slots) {
   constexpr int KT = LC * DK, VT = LC * DV;
   __shared__ __attribute__((aligned(16))) T s[2 * KT + 2 * VT];
-  __shared__ __attribute__((aligned(16))) TeamLds<4, T, TP> lds[2];
+  __shared__ __attribute__((aligned(16))) TeamLds<4, T> lds[2];
   const uint32_t n = slots * (uint32_t)a.Hk, blocks = (n + 7) & ~7u;
   if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.dSf, a.dS0);
   const uint32_t w = work_item(blockIdx.x, n);
@@ -1123,11 +1086,11 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uin
       ps.q = sV, ps.k = sO, ps.v = sQ, ps.x = sK;
       ps.acc = gr > 1 ? a.acc_k + tk : nullptr;
       ps.first = u == 0, ps.last = u == gr - 1;
-      walk<DV, DK, DK / 64, T, DG ? TS : TO, TO, TP, kDK, DG, true>(a, sg, h, ps, tiles, lds);
+      walk<DV, DK, DK / 64, T, kDK, DG, true>(a, sg, h, ps, tiles, lds);
     } else {
       Pass ps = value_pass<DK, DV, T>(a, sg, slot, h);
       ps.q = sK, ps.k = sQ, ps.v = sO;
-      walk<DK, DV, DV / 64, T, TS, kOut, TP, kDV, false, false>(a, sg, h, ps, tiles, lds + 1);
+      walk<DK, DV, DV / 64, T, kDV, false, false>(a, sg, h, ps, tiles, lds + 1);
       if (DG) lds_only_barrier();  // (the other team's, before its last rows)
     }
     lds_only_barrier();
@@ -1135,12 +1098,12 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uin
 }
 
 // one of the gradients by a team of its own
-template <int DK, int DV, typename T, int TS, int TO, int TP, Kind P, bool DG>
+template <int DK, int DV, typename T, Kind P, bool DG>
 __global__ __launch_bounds__(256, kGroups<T>) void k_lin_backward(const LinArgs a, uint32_t n) {
   constexpr bool keys = kFlipped<P>;
   constexpr int D0 = keys ? DV : DK, D1 = keys ? DK : DV;  // of the products, of the result
   __shared__ __attribute__((aligned(16))) T sq[LC * D0], sk[LC * D0], sv[LC * D1];
-  __shared__ __attribute__((aligned(16))) TeamLds<4, T, TP> lds;
+  __shared__ __attribute__((aligned(16))) TeamLds<4, T> lds;
   const uint32_t blocks = (n + 7) & ~7u;
   if (blockIdx.x >= blocks) return copy_state(a, (int)(blockIdx.x - blocks), a.dSf, a.dS0);
   const uint32_t w = work_item(blockIdx.x, n);
@@ -1167,7 +1130,7 @@ __global__ __launch_bounds__(256, kGroups<T>) void k_lin_backward(const LinArgs 
       ps = value_pass<DK, DV, T>(a, sg, slot, h);
     }
     ps.q = sq, ps.k = sk, ps.v = sv;
-    walk<D0, D1, D1 / 64, T, DG || !keys ? TS : TO, TO, TP, P, DG, false>(a, sg, h, ps, tiles, &lds);
+    walk<D0, D1, D1 / 64, T, P, DG, false>(a, sg, h, ps, tiles, &lds);
     lds_only_barrier();
   }
 }
@@ -1314,10 +1277,10 @@ hipError_t launch_states(const LinArgs& a, int dtype, bool both, hipStream_t st)
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
     constexpr int NS = kStateBlocks;
     if (dtype == 0)
-      hipLaunchKernelGGL((k_lin_state<DK, DV, NS, float, 1>), dim3(grid), dim3(4 * DV / NS), 0, st, a,
+      hipLaunchKernelGGL((k_lin_state<DK, DV, NS, float>), dim3(grid), dim3(4 * DV / NS), 0, st, a,
                          n, both);
     else
-      hipLaunchKernelGGL((k_lin_state<DK, DV, NS, __bf16, 3>), dim3(grid), dim3(4 * DV / NS), 0, st,
+      hipLaunchKernelGGL((k_lin_state<DK, DV, NS, __bf16>), dim3(grid), dim3(4 * DV / NS), 0, st,
                          a, n, both);
     if (hipError_t e = hipGetLastError()) return e;
     constexpr int parts = DK * DV / 1024;
@@ -1339,9 +1302,9 @@ hipError_t launch_linear_forward(const LinArgs& a, int dtype, hipStream_t st) {
   if (grid == 0) return hipSuccess;
   GDN_DK_SWITCH(a.dk, GDN_DV_SWITCH(a.dv, {
     if (dtype == 0)
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, float, 1, 1, 1>), dim3(grid), dim3(256), 0, st, a, n);
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, float>), dim3(grid), dim3(256), 0, st, a, n);
     else
-      hipLaunchKernelGGL((k_lin_forward<DK, DV, __bf16, 3, kOut, kOut>), dim3(grid), dim3(256), 0, st,
+      hipLaunchKernelGGL((k_lin_forward<DK, DV, __bf16>), dim3(grid), dim3(256), 0, st,
                          a, n);
     return hipGetLastError();
   }))
@@ -1354,29 +1317,28 @@ static hipError_t launch_passes(const LinArgs& a, uint32_t slots, int dtype, hip
   const uint32_t nk = slots * a.Hk, nv = slots * a.Hv;
   const uint32_t copies = a.dS0 && (a.q.cu || a.q.T == 0) ? a.q.nseq : 0;
   auto grid = [](uint32_t n, uint32_t more) { return dim3(((n + 7) & ~7u) + more); };
-  constexpr int TO = DG ? 3 : kOut;
   if (slots == 0) {
     if (!copies) return hipSuccess;
-    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDV, false>), grid(0, copies),
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, kDV, false>), grid(0, copies),
                        dim3(256), 0, st, a, 0);
   } else if (dtype == 0) {
-    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDQ, DG>), grid(nk, 0), dim3(256), 0,
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, kDQ, DG>), grid(nk, 0), dim3(256), 0,
                        st, a, nk);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDK, DG>), grid(nk, 0), dim3(256), 0,
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, kDK, DG>), grid(nk, 0), dim3(256), 0,
                        st, a, nk);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, 1, 1, 1, kDV, false>), grid(nv, copies),
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, float, kDV, false>), grid(nv, copies),
                        dim3(256), 0, st, a, nv);
   } else if (a.Hv / a.Hk % 2 == 0) {
     const uint32_t blocks = ((2 * nk + 7) & ~7u) + ((nv / 2 + 7) & ~7u);
-    hipLaunchKernelGGL((k_lin_backward_by_two<DK, DV, __bf16, 3, TO, kOut, DG>),
+    hipLaunchKernelGGL((k_lin_backward_by_two<DK, DV, __bf16, DG>),
                        dim3(blocks + copies), dim3(512), 0, st, a, slots);
   } else {
-    hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, 3, TO, kOut, kDQ, DG>), grid(nk, 0),
+    hipLaunchKernelGGL((k_lin_backward<DK, DV, __bf16, kDQ, DG>), grid(nk, 0),
                        dim3(256), 0, st, a, nk);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((k_lin_backward_kv<DK, DV, __bf16, 3, TO, kOut, DG>), grid(nk, copies),
+    hipLaunchKernelGGL((k_lin_backward_kv<DK, DV, __bf16, DG>), grid(nk, copies),
                        dim3(512), 0, st, a, slots);
   }
   return hipGetLastError();
