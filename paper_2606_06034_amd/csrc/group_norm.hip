@@ -12,8 +12,8 @@
 // of parts of the positions first, then the results.  A thread has V neighbouring channels
 // of one group all along, so that its weights and its sums of dw and db stay in registers.
 // Everything is added up in a fixed order (no atomics: the same call gives the same bits).
-// (8192 rows of 32 groups of 128 with a gate, bf16: 36.6 us, 5.5 TB/s; gradients 67 and 4 us,
-// 5.1 TB/s.  4 x 4096 positions of 32 groups of 16, SiLU: 8 us for the sums, 12 for the
+// (8192 rows of 32 groups of 128 with a gate, bf16: 37 us, 5.4 TB/s; gradients 69 and 4 us,
+// 4.9 TB/s.  4 x 4096 positions of 32 groups of 16, SiLU: 8 us for the sums, 12 for the
 // results.  Gradients of 3 x 3001 positions of 8 groups of 41, fp32, a value a load: 10 and 14.)
 #include <algorithm>
 

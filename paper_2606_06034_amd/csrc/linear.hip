@@ -26,14 +26,14 @@
 //
 // Precision.  bf16 inputs are exact operands of the matrix instructions; fp32 factors
 // (states, decayed values, P) enter as sums of three bf16 terms (split.hpp), 2^-24 of each.  (Two
-// where a result is in bf16 take 2 to 8 % less time, and are off by several roundings of a
+// where a result is in bf16 take 2 to 9 % less time, and are off by several roundings of a
 // result whose terms cancel to a thousandth.)  fp32 inputs go to the fp32 matrix instructions.
 //
-// Bound: a pass's tiles are read once and take 3 TB/s; the rest is the serial step of a chunk,
-// products of at most 128 x 128 x 64 with the splits between them.  A step takes 4.3 us with
-// one workgroup of 256 a CU and 3.6 each with two, 11 with two teams of a gradient.  (8192 tokens,
-// 16 heads: states 22 us, their carry 8, walk 48; gradients: states 34, carry 12, dQ 64,
-// dK and dV 89, dg 10.)
+// Bound: a pass's tiles are read once, at 2.8 TB/s; the rest is the serial step of a chunk,
+// products of at most 128 x 128 x 64 with the splits between them.  A step takes 4.6 us with
+// one workgroup of 256 a CU and 3.8 each with two, 12 with two teams of a gradient.  (8192 tokens,
+// 16 heads: states 22 us, their carry 8, walk 54; gradients: states 34, carry 12, dQ 67,
+// dK and dV 99, dg 10.)
 #include <algorithm>
 #include <cmath>
 
@@ -59,8 +59,9 @@ template <typename T> struct FragFor { typedef f32x4 type; };
 template <> struct FragFor<__bf16> { typedef bf16x4 type; };
 
 // Blocks of 16 value columns a wave has where a segment's state is formed: eight waves for 128
-// columns, as many loads in flight as there can be.  Four walk (16 heads of 8192 tokens: 48 us, 47
-// with eight, which take twice the LDS reads of P and leave no room for a second workgroup).
+// columns, as many loads in flight as there can be.  Four walk (eight took as long, 47 and 48 us
+// for 16 heads of 8192 tokens in two terms: they take twice the LDS reads of P and leave no room
+// for a second workgroup).
 constexpr int kStateBlocks = 1;
 constexpr int kMostChunks = 16;  // of a segment of the backward pass
 
@@ -1019,8 +1020,8 @@ __device__ __forceinline__ void key_gradient_by_two(const LinArgs& a, const Segm
 
 }  // namespace
 
-// groups of even size.  (4 x 8192 tokens, 32 heads in pairs: 0.97 to 1.1 ms, 3 TB/s, vector units
-// busy 44 % and matrix units 28 %.)
+// groups of even size.  (4 x 8192 tokens, 32 heads in pairs: 1.1 to 1.3 ms, 2.5 TB/s, vector units
+// busy 45 % and matrix units 30 %.)
 template <int DK, int DV, typename T, bool DG>
 __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a, uint32_t slots) {
   // the second team's results go where the tiles of products lie, which the first has done with
@@ -1057,8 +1058,8 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward_by_two(const LinArgs a,
   }
 }
 
-// dK and dV of a key head's value heads one after the other.  (8192 tokens of 16 heads: 89 us,
-// 2.7 TB/s, vector units busy 40 % and matrix units 26 %.)
+// dK and dV of a key head's value heads one after the other.  (8192 tokens of 16 heads: 99 us,
+// 2.4 TB/s, vector units busy 41 % and matrix units 27 %.)
 template <int DK, int DV, typename T, bool DG>
 __global__ __launch_bounds__(512, 2) void k_lin_backward_kv(const LinArgs a, uint32_t slots) {
   constexpr int KT = LC * DK, VT = LC * DV;
@@ -1194,15 +1195,15 @@ __global__ __launch_bounds__(256) void k_lin_decay_sum(const LinArgs a, int64_t 
 // Tokens a segment.  Short ones fill the chip, long ones save launches and states (each is
 // written, carried over the segments and read: 4 times 64 KB, 9 in the backward pass): the one
 // of least time by what the launches took, in us, for heads of 128 by 128 in bf16.  A step
-// of a walk, of 64 tokens, takes 4.6 with one workgroup a CU and 3.6 each with two, forming
+// of a walk, of 64 tokens, takes 4.6 with one workgroup a CU and 3.6 to 3.8 each with two, forming
 // a segment's state 1.2 and 0.9; 11 to 12 a step of two teams, one workgroup a CU; with fp32
-// inputs 3.8 times as long.  (Forward, 16 heads of 8192 tokens: 135 us in segments of 64, 96 of
-// 128, 73 of 256, 71 of 512, 92 of 768, 161 of 1536; 4 of 1000: 23 of 64, 25 of 128, 36 of 256, 73
-// in one, in fp32 35, 49, 85 and 222.  Gradients, 16 heads of 8192: 440 of 64, 215 of 256, 192 of
-// 512, 299 of 1024; 32 of 2 x 8192 with 16 key heads: 821 of 256, 692 of 512, 634 of 1024.  Packed,
-// 16384 tokens in 31 sequences, 16 heads: forward 318, 214, 170, 181, 182 of 64, 128, 256, 512, 1024;
-// gradients, 8 key heads: 966, 626, 505, 481, 563.  Over nine packed mixes the segments chosen
-// take 4 % more than the best ones, 1 % for the gradients.)
+// inputs 3.8 times as long.  (Forward, 16 heads of 8192 tokens: 128 us in segments of 64, 101 of
+// 128, 79 of 256, 79 to 82 of 512, 98 of 768, 175 of 1536; 4 of 1000: 23 of 64, 26 of 128, 37 of
+// 256, 83 in one, in fp32 34, 49, 85 and 221.  Gradients, 16 heads of 8192: 443 of 64, 226 of 256,
+// 210 of 512, 318 of 1024; 32 of 2 x 8192 with 16 key heads: 866 of 256, 738 of 512, 670 of 1024.
+// Packed, 16384 tokens in 31 sequences, 16 heads: forward 325, 228, 181, 196, 200 of 64, 128, 256,
+// 512, 1024; gradients, 8 key heads: 982, 648, 530, 503, 592.  Over nine packed mixes the segments
+// chosen take 4 % more than the best ones, 2 % for the gradients.)
 int lin_segment(int nseq, int T, int Hk, int Hv, int dk, int dv, bool packed, bool backward,
                 bool fp32) {
   const double tokens = packed ? (double)T : (double)nseq * T, gr = Hk ? (double)Hv / Hk : 1;
