@@ -812,8 +812,8 @@ static hipError_t group_backward(GroupArgs a, hipStream_t st) {
     const unsigned each = (unsigned)(a.sparts * a.cblocks);
     hipLaunchKernelGGL((k_gn_sums<T, V, OPS>), dim3(a.nrows * each), dim3(256), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((k_gn_dx<T, V, OPS>), dim3((unsigned)a.N * each + adding), dim3(256), 0, st, a,
-                       (int)adding);
+    hipLaunchKernelGGL((k_gn_dx<T, V, OPS>), dim3((unsigned)a.N * each + adding), dim3(256), 0, st,
+                       a, (int)adding);
     return hipGetLastError();
   }
   if (a.N > 0) {

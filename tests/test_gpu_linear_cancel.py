@@ -36,7 +36,8 @@ class Inputs:
     def pairs(self, *s):
         """[..., 2 n] of x, -x (1 + d)"""
         x = self.uniform(*s[:-1], s[-1] // 2)
-        return torch.stack([x, -x * (1 + (self.uniform(*x.shape) - 1) * 2.0 ** -11)], -1).flatten(-2)
+        d = (self.uniform(*x.shape) - 1) * 2.0 ** -11
+        return torch.stack([x, -x * (1 + d)], -1).flatten(-2)
 
 
 def held(got, ref, term, what):
